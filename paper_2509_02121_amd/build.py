@@ -37,6 +37,10 @@ HIP_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
+HOST_SOURCES = ["halo_plan.cpp", "halo_forest.cpp"]
+HIP_SOURCES = ["halo_kernels.hip", "halo_pages.hip"]
+PROBE_SOURCES = ["halo_probe.hip"]
+
 
 def _run(cmd):
     print(" ".join(cmd), flush=True)
@@ -47,31 +51,20 @@ def build(verbose=True):
     """Compile every source and link the shared library next to this file."""
     tmp = tempfile.mkdtemp(prefix="halo_build_")
     try:
-        plan_o = os.path.join(tmp, "halo_plan.o")
-        forest_o = os.path.join(tmp, "halo_forest.o")
-        kern_o = os.path.join(tmp, "halo_kernels.o")
-        pages_o = os.path.join(tmp, "halo_pages.o")
-        probe_o = os.path.join(tmp, "halo_probe.o")
-        procs = [
-            subprocess.Popen(["g++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-Wextra",
-                              "-I", INCLUDE, "-c", os.path.join(CSRC, "halo_plan.cpp"), "-o", plan_o]),
-            subprocess.Popen(["g++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-Wextra",
-                              "-I", INCLUDE, "-c", os.path.join(CSRC, "halo_forest.cpp"), "-o", forest_o]),
-            subprocess.Popen([HIPCC] + HIP_FLAGS + ["-I", INCLUDE, "-c",
-                                                   os.path.join(CSRC, "halo_kernels.hip"), "-o", kern_o]),
-            subprocess.Popen([HIPCC] + HIP_FLAGS + ["-I", INCLUDE, "-c",
-                                                   os.path.join(CSRC, "halo_pages.hip"), "-o", pages_o]),
-            subprocess.Popen([HIPCC] + HIP_FLAGS + ["-I", INCLUDE, "-c",
-                                                   os.path.join(CSRC, "halo_probe.hip"), "-o", probe_o]),
-        ]
+        objs, procs = {}, []
+        for src in HOST_SOURCES + HIP_SOURCES + PROBE_SOURCES:
+            objs[src] = os.path.join(tmp, src + ".o")
+            cc = ["g++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-Wextra"] if src in HOST_SOURCES else [HIPCC] + HIP_FLAGS
+            procs.append(subprocess.Popen(cc + ["-I", INCLUDE, "-c", os.path.join(CSRC, src), "-o", objs[src]]))
         rcs = [p.wait() for p in procs]
         if any(rcs):
             raise RuntimeError(f"compilation failed (exit codes {rcs})")
         out_tmp = LIB_PATH + ".tmp"
-        _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", plan_o, forest_o, kern_o, pages_o, "-o", out_tmp])
+        _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC"] + [objs[s] for s in HOST_SOURCES + HIP_SOURCES] +
+             ["-o", out_tmp])
         os.replace(out_tmp, LIB_PATH)
         probe_tmp = PROBE_LIB_PATH + ".tmp"
-        _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", probe_o, "-o", probe_tmp])
+        _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC"] + [objs[s] for s in PROBE_SOURCES] + ["-o", probe_tmp])
         os.replace(probe_tmp, PROBE_LIB_PATH)
         # the C-ABI driver of the tests (host code against the built library)
         _run(["g++", "-std=c++17", "-O2", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE,
