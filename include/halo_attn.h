@@ -347,6 +347,117 @@ halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t* params,
                                 const int32_t* src_pages, const int32_t* dst_pages,
                                 int32_t num_pages, int32_t* error_flag, void* stream);
 
+/* Page lists, positions and slots of one step, built on the GPU from the
+ * lengths of its sequences: the arrays that the scatter and the gather take,
+ * without a copy from the host. Sequence i holds seq_len[i] tokens in the first
+ * ceil(seq_len[i] / page_size) pages of row i of block_table and is about to get
+ * seq_new[i] more (0 allowed). Where these need more pages, the pages
+ * free_pages[free_next], free_pages[free_next + 1], ... are entered in its row:
+ * in the order of the sequences and, in a sequence, of its pages, so that a host
+ * that knows the lengths knows which pages went where.
+ * All pointers but the structs are DEVICE pointers; the outputs are
+ *   seq_page_indptr [num_seqs + 1], page_ids [max_pages]: the sequences' page
+ *     lists with the new pages (page_ids past the last one is left as it was);
+ *   seq_start, seq_count, seq_end [num_seqs]: seq_len, seq_new and their sum;
+ *   in_token_offset [num_seqs] int64: tokens of the sequences before;
+ *   positions [max_tokens] int32, slots [max_tokens] int64: of each new token,
+ *     its place in its sequence, and page * page_size + place in the page (-1
+ *     for a negative page id); behind the last token 0 and -1, as for the
+ *     padding of a captured step. Either may be NULL;
+ *   free_next [1]: the first page that is still free.
+ * A sequence whose lengths are negative or add up to more than table_width *
+ * page_size (or 2^31 - 16) takes part with no pages and no tokens, its seq_end
+ * being its seq_len. A step that does not fit (too few free pages, free_next
+ * outside [0, num_free], more than max_pages pages or max_tokens tokens) is
+ * refused whole: every sequence takes part like that and no page is taken.
+ * Either way 1 is written to error_flag (may be NULL; 0 never is). The call can
+ * be repeated: the same inputs give the same outputs. seq_len, seq_new and
+ * free_next must not overlap the outputs. */
+typedef struct {
+  int32_t num_seqs;
+  int32_t page_size;     /* 16 */
+  int32_t table_width;   /* pages of a row of block_table */
+  int32_t num_free;      /* elements of free_pages */
+  int32_t max_tokens;    /* elements of positions and slots */
+  int32_t max_pages;     /* elements of page_ids */
+} halo_step_sizes_t;
+
+typedef struct {
+  int32_t* seq_page_indptr;
+  int32_t* page_ids;
+  int32_t* seq_start;
+  int32_t* seq_count;
+  int32_t* seq_end;
+  int64_t* in_token_offset;
+  int32_t* positions;
+  int64_t* slots;
+  int32_t* free_next;
+} halo_step_tables_t;
+
+halo_status_t halo_kv_step_tables(const halo_step_sizes_t* sizes, const int32_t* seq_len,
+                                  const int32_t* seq_new, int32_t* block_table,
+                                  const int32_t* free_pages, const int32_t* free_next,
+                                  const halo_step_tables_t* tables, int32_t* error_flag, void* stream);
+
+/* Rotary positions. Pair i of a head's first rotary_dim dims is turned by the
+ * angle position * w_i, and multiplied by the amplitude:
+ *   (x, y) -> amplitude * (x cos - y sin, x sin + y cos),  w_i = base^(-2i / rotary_dim)
+ * The pair is dims (i, i + rotary_dim / 2), or (2i, 2i + 1) if interleaved; the
+ * dims past rotary_dim stay as they are. For positions beyond those a model was
+ * trained on, factor times as many:
+ *   LINEAR  w_i / factor;
+ *   NTK     base * factor^(rotary_dim / (rotary_dim - 2)) for base;
+ *   YARN    pairs that make more than fast_turns turns over original_positions
+ *           keep w_i, those of fewer than slow_turns get w_i / factor, with a
+ *           ramp over i between the two (from the next lower whole i to the next
+ *           higher one); amplitude 0.1 ln(factor) + 1;
+ *   BANDS   the same with the ramp over the turns, and amplitude 1.
+ * fast_turns and slow_turns both 0: 32 and 1 for YARN, 4 and 1 for BANDS. */
+typedef enum {
+  HALO_ROPE_NONE = 0,
+  HALO_ROPE_LINEAR = 1,
+  HALO_ROPE_NTK = 2,
+  HALO_ROPE_YARN = 3,
+  HALO_ROPE_BANDS = 4
+} halo_rope_scaling_t;
+
+typedef struct {
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t rotary_dim;   /* a multiple of 16, <= head_dim */
+  int32_t interleaved;
+  halo_rope_scaling_t scaling;
+  double base;          /* > 1 */
+  double factor;        /* >= 1 */
+  int32_t original_positions;
+  double fast_turns;
+  double slow_turns;
+} halo_rope_params_t;
+
+/* Fill *rope with the defaults: the whole head, pairs a half apart, base 10000,
+ * no scaling, original_positions 8192. */
+void halo_rope_params_default(halo_rope_params_t* rope, int32_t head_dim);
+
+/* The angles of one position (host only): turns[i], i < rotary_dim / 2, is
+ * w_i / (2 pi) with 64 bits after the point, which halo_rope_qk multiplies by the
+ * position exactly. Made once and copied to the GPU by the caller. */
+halo_status_t halo_rope_turns(const halo_rope_params_t* rope, uint64_t* turns, float* amplitude);
+
+/* Turn the queries and keys of num_tokens tokens by their positions, in one
+ * launch. q [num_tokens][num_q_heads][head_dim] with tokens q_stride elements
+ * apart (>= num_q_heads * head_dim: q and k may be parts of the rows of one
+ * projection), k, q_out and k_out likewise; q_out == q and k_out == k turn in
+ * place, any other overlap is not allowed. positions [num_tokens] (negative:
+ * taken as 0) and turns [rotary_dim / 2] are DEVICE arrays. Tensors and tokens
+ * are 16-byte aligned. num_q_heads or num_kv_heads may be 0. Of rope only
+ * head_dim, rotary_dim and interleaved are used. Computed in fp32, rounded once
+ * to dtype. */
+halo_status_t halo_rope_qk(const halo_rope_params_t* rope, float amplitude, const uint64_t* turns,
+                           const int32_t* positions, int32_t num_tokens, int32_t num_q_heads,
+                           int32_t num_kv_heads, halo_dtype_t dtype,
+                           const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                           void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                           void* stream);
+
 /* Prefix forest from token ids (host only, no device work). The prompts of
  * a batch that share prefixes (§2 intra-batch prefix sharing: a shared
  * prefix is computed once and its KV cache reused; §1: recurring prompts are

@@ -37,8 +37,8 @@ HIP_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
-HOST_SOURCES = ["halo_plan.cpp", "halo_forest.cpp"]
-HIP_SOURCES = ["halo_kernels.hip", "halo_pages.hip"]
+HOST_SOURCES = ["halo_plan.cpp", "halo_forest.cpp", "halo_rope.cpp"]
+HIP_SOURCES = ["halo_kernels.hip", "halo_pages.hip", "halo_step.hip"]
 PROBE_SOURCES = ["halo_probe.hip"]
 
 

@@ -87,6 +87,7 @@ EXPORTED_SYMBOLS = (
     "halo_prefix_attn_decode", "halo_prefix_attn_prefill", "halo_prefix_attn_decode_noalloc",
     "halo_kv_page_gather",
     "halo_kv_page_scatter", "halo_kv_page_scatter_kv", "halo_kv_page_copy",
+    "halo_kv_step_tables", "halo_rope_params_default", "halo_rope_turns", "halo_rope_qk",
     "halo_prefix_tree_build", "halo_prefix_tree_get", "halo_prefix_tree_destroy",
     "halo_status_string", "halo_last_error_message",
 )
@@ -96,6 +97,23 @@ class PrefixTreeInfo(ctypes.Structure):
     _fields_ = [("num_segments", ctypes.c_int32), ("num_path_entries", ctypes.c_int32),
                 ("num_pages", ctypes.c_int64), ("prompt_tokens", ctypes.c_int64),
                 ("distinct_tokens", ctypes.c_int64)]
+
+
+class StepSizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_seqs", "page_size", "table_width", "num_free", "max_tokens",
+                                              "max_pages")]
+
+
+class _StepTables(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("seq_page_indptr", "page_ids", "seq_start", "seq_count", "seq_end",
+                                               "in_token_offset", "positions", "slots", "free_next")]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("scaling", ctypes.c_int), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_positions", ctypes.c_int32), ("fast_turns", ctypes.c_double),
+                ("slow_turns", ctypes.c_double)]
 
 
 class HaloError(RuntimeError):
@@ -176,6 +194,17 @@ def load_library(require_gpu=False):
     lib.halo_kv_page_scatter_kv.restype = ctypes.c_int
     lib.halo_kv_page_copy.argtypes = [vp, ctypes.POINTER(AttnParams), vp, vp, ctypes.c_int32, vp, vp]
     lib.halo_kv_page_copy.restype = ctypes.c_int
+    lib.halo_kv_step_tables.argtypes = [ctypes.POINTER(StepSizes), vp, vp, vp, vp, vp, ctypes.POINTER(_StepTables),
+                                        vp, vp]
+    lib.halo_kv_step_tables.restype = ctypes.c_int
+    lib.halo_rope_params_default.argtypes = [ctypes.POINTER(RopeParams), ctypes.c_int32]
+    lib.halo_rope_params_default.restype = None
+    lib.halo_rope_turns.argtypes = [ctypes.POINTER(RopeParams), vp, ctypes.POINTER(ctypes.c_float)]
+    lib.halo_rope_turns.restype = ctypes.c_int
+    lib.halo_rope_qk.argtypes = [ctypes.POINTER(RopeParams), ctypes.c_float, vp, vp, ctypes.c_int32, ctypes.c_int32,
+                                 ctypes.c_int32, ctypes.c_int, vp, ctypes.c_int64, vp, ctypes.c_int64, vp,
+                                 ctypes.c_int64, vp, ctypes.c_int64, vp]
+    lib.halo_rope_qk.restype = ctypes.c_int
     lib.halo_prefix_tree_build.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(vp),
                                            ctypes.POINTER(PrefixTreeInfo)]
     lib.halo_prefix_tree_build.restype = ctypes.c_int
@@ -683,6 +712,184 @@ def bind_kv_page_copy(pool, params, src_pages, dst_pages, error_flag=None, strea
         if st != HALO_OK:
             _check(st)
     return call
+
+
+class StepTables:
+    """The outputs of kv_step_tables (torch tensors on one GPU): the page
+    lists, ranges and offsets that kv_page_scatter_kv and kv_page_gather take,
+    positions and slots of up to max_tokens new tokens, page lists of up to
+    max_pages pages. seq_end is the next step's seq_len and free_next its
+    free_next (copy them there: a call's outputs must not be its inputs)."""
+
+    def __init__(self, num_seqs, max_tokens, max_pages, device="cuda"):
+        import torch
+
+        def ints(n, dtype=torch.int32):
+            return torch.zeros(n, dtype=dtype, device=device)
+
+        self.num_seqs, self.max_tokens, self.max_pages = int(num_seqs), int(max_tokens), int(max_pages)
+        self.seq_page_indptr, self.page_ids = ints(self.num_seqs + 1), ints(self.max_pages)
+        self.seq_start, self.seq_count, self.seq_end = (ints(self.num_seqs) for _ in range(3))
+        self.in_token_offset = ints(self.num_seqs, torch.int64)
+        self.positions, self.slots = ints(self.max_tokens), ints(self.max_tokens, torch.int64)
+        self.free_next = ints(1)
+
+
+def _step_args(tables, seq_len, seq_new, block_table, free_pages, free_next, error_flag, stream):
+    import torch
+    n = tables.num_seqs
+    _gpu(seq_len, "seq_len", torch.int32, n)
+    _gpu(seq_new, "seq_new", torch.int32, n)
+    _gpu(block_table, "block_table", torch.int32)
+    if block_table.dim() != 2 or block_table.shape[0] < n:
+        raise ValueError(f"block_table must be [num_seqs or more, pages], got {tuple(block_table.shape)} for {n}")
+    _gpu(free_pages, "free_pages", torch.int32)
+    _gpu(free_next, "free_next", torch.int32, 1)
+    outs = [("seq_page_indptr", torch.int32, n + 1), ("page_ids", torch.int32, tables.max_pages),
+            ("seq_start", torch.int32, n), ("seq_count", torch.int32, n), ("seq_end", torch.int32, n),
+            ("in_token_offset", torch.int64, n), ("positions", torch.int32, tables.max_tokens),
+            ("slots", torch.int64, tables.max_tokens), ("free_next", torch.int32, 1)]
+    ptrs, used = {}, [seq_len, seq_new, block_table, free_pages, free_next]
+    for name, dtype, numel in outs:
+        t = getattr(tables, name)
+        if t is None and name in ("positions", "slots"):
+            ptrs[name] = None
+            continue
+        _gpu(t, name, dtype, numel)
+        ptrs[name] = t.data_ptr()
+        used.append(t)
+        for other, what in ((seq_len, "seq_len"), (seq_new, "seq_new"), (free_next, "free_next")):
+            if _overlap(t, other):
+                raise ValueError(f"{what} must not overlap the output {name}")
+    if error_flag is not None:
+        used.append(_gpu(error_flag, "error_flag", torch.int32, 1))
+    _one_gpu(used, stream)
+    sizes = StepSizes(n, 16, block_table.shape[1], free_pages.numel(), tables.max_tokens, tables.max_pages)
+    return (ctypes.byref(sizes), seq_len.data_ptr(), seq_new.data_ptr(), block_table.data_ptr(),
+            free_pages.data_ptr(), free_next.data_ptr(), ctypes.byref(_StepTables(**ptrs)),
+            error_flag.data_ptr() if error_flag is not None else None, _stream_handle(stream))
+
+
+def _one_gpu(tensors, stream):
+    """Check that the tensors are on one GPU, the current one and the
+    stream's: a launch goes to the current GPU."""
+    import torch
+    dev = tensors[0].device
+    for t in tensors:
+        if t.device != dev:
+            raise ValueError(f"the tensors of a call must be on one GPU, got {dev} and {t.device}")
+    here = torch.cuda.current_device()
+    if dev.index != here:
+        raise ValueError(f"the tensors are on {dev}, the current GPU is cuda:{here}")
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"the tensors are on {dev}, the stream is on {stream.device}")
+
+
+def _overlap(a, b):
+    """Whether two contiguous tensors share memory."""
+    return (a.numel() > 0 and b.numel() > 0 and a.data_ptr() < b.data_ptr() + _nbytes(b) and
+            b.data_ptr() < a.data_ptr() + _nbytes(a))
+
+
+def kv_step_tables(tables, seq_len, seq_new, block_table, free_pages, free_next, error_flag=None, stream=None):
+    """halo_kv_step_tables on torch tensors: fills `tables` (a StepTables) and
+    enters new pages in block_table [num_seqs, pages]."""
+    load_library()
+    _check(_LIB.halo_kv_step_tables(*_step_args(tables, seq_len, seq_new, block_table, free_pages, free_next,
+                                                error_flag, stream)))
+
+
+def bind_kv_step_tables(tables, seq_len, seq_new, block_table, free_pages, free_next, error_flag=None, stream=None):
+    """kv_step_tables as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kv_step_tables, _step_args(tables, seq_len, seq_new, block_table, free_pages, free_next,
+                                                       error_flag, stream))
+
+
+def _bound(fn, args):
+    def call():
+        st = fn(*args)
+        if st != HALO_OK:
+            _check(st)
+    return call
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+
+
+class Rope:
+    """Rotary positions of one model: halo_rope_params_t, and its angles
+    (halo_rope_turns) on the GPU. fast_turns and slow_turns None: the
+    scaling's defaults."""
+
+    def __init__(self, head_dim, rotary_dim=None, base=10000.0, interleaved=False, scaling="none", factor=1.0,
+                 original_positions=8192, fast_turns=None, slow_turns=None, device="cuda"):
+        import torch
+        lib = load_library()
+        if scaling not in ROPE_SCALINGS:
+            raise ValueError(f"unknown rope scaling {scaling!r}")
+        if (fast_turns is None) != (slow_turns is None):
+            raise ValueError("fast_turns and slow_turns are given together")
+        self.params = RopeParams(head_dim, head_dim if rotary_dim is None else rotary_dim, int(bool(interleaved)),
+                                 ROPE_SCALINGS[scaling], base, factor, original_positions, fast_turns or 0.0,
+                                 slow_turns or 0.0)
+        host = np.zeros(max(self.params.rotary_dim // 2, 1), dtype=np.uint64)
+        amplitude = ctypes.c_float()
+        _check(lib.halo_rope_turns(ctypes.byref(self.params), host.ctypes.data, ctypes.byref(amplitude)))
+        self.amplitude = amplitude.value
+        self.host_turns = host
+        self.turns = torch.from_numpy(host.view(np.int64)).to(device)
+
+
+def _rope_operand(t, name, head_dim, dtype, tokens):
+    """Check a [tokens, heads, head_dim] GPU tensor whose tokens may be any
+    stride apart; returns (heads, token stride in elements)."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dim() != 3 or t.shape[2] != head_dim:
+        raise ValueError(f"{name} must be [tokens, heads, {head_dim}], got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape[0] != tokens:
+        raise ValueError(f"{name} has {t.shape[0]} tokens, expected {tokens}")
+    heads = t.shape[1]
+    if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim)):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    return heads, t.stride(0) if tokens > 1 else heads * head_dim
+
+
+def _rope_args(q, k, positions, rope, q_out, k_out, stream):
+    import torch
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    d, n = rope.params.head_dim, q.shape[0]
+    code = _dtype_code(q.dtype)
+    hq, sq = _rope_operand(q, "q", d, q.dtype, n)
+    hk, sk = _rope_operand(k, "k", d, q.dtype, n)
+    hqo, sqo = _rope_operand(q_out, "q_out", d, q.dtype, n)
+    hko, sko = _rope_operand(k_out, "k_out", d, q.dtype, n)
+    if (hqo, hko) != (hq, hk):
+        raise ValueError("q_out and k_out must have the heads of q and k")
+    _gpu(positions, "positions", torch.int32, n)
+    _one_gpu([q, k, q_out, k_out, positions, rope.turns], stream)
+    return (ctypes.byref(rope.params), rope.amplitude, rope.turns.data_ptr(), positions.data_ptr(), n, hq, hk, code,
+            q.data_ptr(), sq, k.data_ptr(), sk, q_out.data_ptr(), sqo, k_out.data_ptr(), sko, _stream_handle(stream))
+
+
+def rope_qk(q, k, positions, rope, q_out=None, k_out=None, stream=None):
+    """halo_rope_qk on torch tensors: q and k [tokens, heads, head_dim]
+    (tokens any stride apart, as in the rows of one projection) turned by
+    positions, into q_out and k_out (None: in place)."""
+    load_library()
+    _check(_LIB.halo_rope_qk(*_rope_args(q, k, positions, rope, q_out, k_out, stream)))
+
+
+def bind_rope_qk(q, k, positions, rope, q_out=None, k_out=None, stream=None):
+    """rope_qk as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_rope_qk, _rope_args(q, k, positions, rope, q_out, k_out, stream))
 
 
 class PrefixAttention:
