@@ -347,6 +347,54 @@ halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t* params,
                                 const int32_t* src_pages, const int32_t* dst_pages,
                                 int32_t num_pages, int32_t* error_flag, void* stream);
 
+/* The 4-bit cache: pools of 0.53 bytes per element of K and V instead of 2 or 4.
+ * A code is E2M1 (sign; magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 for 0 .. 7), and a
+ * scale is a power of two: of a token's K one for each 32 dims of a head (its
+ * strong channels then cost the others nothing), held as the biased exponent in
+ * a byte; of its V one for the head, held in bf16. A block's exponent is that of
+ * its largest magnitude rounded to two significant bits, less two (at least
+ * 2^-126); its codes are the nearest ones, ties to the even code, magnitudes past
+ * 6 to 6. A block with an infinity or a NaN becomes NaN (scale byte 255, or bf16
+ * NaN). Every value that a code stands for is exact in bf16.
+ * Pools are bytes, [num_pool_pages][num_kv_heads][tile], and a tile (D = head_dim)
+ *   K: codes  [g: 4][token: 16][s: D/32][i: 8], dim 32 s + 8 g + i   (D * 8 bytes)
+ *      scales [token: 16][s: D/32]                                    (D / 2 bytes)
+ *   V: codes  [bq: D/64][h: 2][c: 16][b: 4][j: 8], dim 16 (4 bq + b) + c,
+ *             slot 8 h + j                                            (D * 8 bytes)
+ *      scales [slot: 16] bf16                                         (32 bytes)
+ * with two codes to a byte, the first one low, and the slots of a V tile as in a
+ * v_pool. */
+
+/* Bytes of a 4-bit pool (-1 and an error message for unsupported params). Of
+ * params num_kv_heads, head_dim, page_size and num_pool_pages are used. */
+int64_t halo_kvq_pool_bytes(const halo_attn_params_t* params, halo_pool_kind_t pool_kind);
+
+/* halo_kv_page_scatter_kv into 4-bit pools: the tokens (of kv_dtype) are
+ * quantised on the way, from each token's values alone, so that a token written
+ * by an append and one written by a chunk are the same bits. Arguments and error
+ * rules are those of halo_kv_page_scatter_kv, and two sequences of one call must
+ * not write into the same page (a byte of a V tile holds two tokens). */
+halo_status_t halo_kvq_page_scatter_kv(void* k_pool, void* v_pool, const halo_attn_params_t* params,
+                                       const int32_t* page_ids, const int32_t* seq_page_indptr,
+                                       const int32_t* seq_start, const int32_t* seq_count,
+                                       const int64_t* in_token_offset, int32_t num_seqs,
+                                       const void* k_in, const void* v_in, int32_t* error_flag,
+                                       void* stream);
+
+/* halo_kv_page_gather of both 4-bit pools in one launch: the tokens' values in
+ * kv_dtype (exact), K to k_out and V to v_out, [*][num_kv_heads][head_dim] each.
+ * Arguments and error rules are those of halo_kv_page_gather. */
+halo_status_t halo_kvq_page_gather_kv(const void* k_pool, const void* v_pool, const halo_attn_params_t* params,
+                                      const int32_t* page_ids, const int32_t* seq_page_indptr,
+                                      const int32_t* seq_len, const int64_t* out_token_offset,
+                                      int32_t num_seqs, void* k_out, void* v_out, int32_t* error_flag,
+                                      void* stream);
+
+/* halo_kv_page_copy in a 4-bit pool. */
+halo_status_t halo_kvq_page_copy(void* pool, const halo_attn_params_t* params, halo_pool_kind_t pool_kind,
+                                 const int32_t* src_pages, const int32_t* dst_pages, int32_t num_pages,
+                                 int32_t* error_flag, void* stream);
+
 /* Page lists, positions and slots of one step, built on the GPU from the
  * lengths of its sequences: the arrays that the scatter and the gather take,
  * without a copy from the host. Sequence i holds seq_len[i] tokens in the first

@@ -25,7 +25,8 @@ reads kv head h // (H_q / H_kv)).
 
 ``paged_kv`` holds the reference of the paged-KV write path (token scatter
 into the pool layouts, page copy for copy-on-write); ``forest`` the prefix
-forest of a batch of token-id prompts, by brute force.
+forest of a batch of token-id prompts, by brute force; ``paged_kvq`` the 4-bit
+cache format.
 """
 
 from .attention import (  # noqa: F401
@@ -38,3 +39,4 @@ from .attention import (  # noqa: F401
 )
 from . import paged_kv  # noqa: F401,E402
 from . import forest  # noqa: F401,E402
+from . import paged_kvq  # noqa: F401,E402

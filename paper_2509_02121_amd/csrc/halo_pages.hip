@@ -691,6 +691,17 @@ extern "C" halo_status_t halo_kv_page_scatter_kv(void* k_pool, void* v_pool, con
   return launch_scatter(params, g, 2, stream);
 }
 
+halo_status_t halo::launch_page_copy(void* pool, const int32_t* src_pages, const int32_t* dst_pages, int32_t num_pages,
+                                     int64_t num_pool_pages, int64_t page_bytes, int32_t* error_flag, void* stream) {
+  PageCopyArgs g{pool, src_pages, dst_pages, error_flag, num_pool_pages, page_bytes / 16, num_pages};
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const int64_t want = ((int64_t)num_pages * g.page_vecs + 255) / 256;
+  const int blocks = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 4096);
+  hipLaunchKernelGGL(page_copy_kernel, dim3(blocks), dim3(256), 0, st, g);
+  return hip_check("page copy launch");
+}
+
 extern "C" halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t* params,
                                            const int32_t* src_pages, const int32_t* dst_pages,
                                            int32_t num_pages, int32_t* error_flag, void* stream) {
@@ -710,11 +721,5 @@ extern "C" halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t*
   else return fail(HALO_ERR_UNSUPPORTED, "kv_dtype must be HALO_F32 or HALO_BF16");
   if (!aligned16(pool)) return fail(HALO_ERR_INVALID_ARGUMENT, "pool must be 16-byte aligned");
   const int64_t page_bytes = (int64_t)params->num_kv_heads * 16 * params->head_dim * elt;
-  PageCopyArgs g{pool, src_pages, dst_pages, error_flag, params->num_pool_pages, page_bytes / 16, num_pages};
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  (void)hipGetLastError();
-  const int64_t want = ((int64_t)num_pages * g.page_vecs + 255) / 256;
-  const int blocks = (int)std::min<int64_t>(std::max<int64_t>(want, 1), 4096);
-  hipLaunchKernelGGL(page_copy_kernel, dim3(blocks), dim3(256), 0, st, g);
-  return hip_check("page copy launch");
+  return launch_page_copy(pool, src_pages, dst_pages, num_pages, params->num_pool_pages, page_bytes, error_flag, stream);
 }

@@ -87,6 +87,7 @@ EXPORTED_SYMBOLS = (
     "halo_prefix_attn_decode", "halo_prefix_attn_prefill", "halo_prefix_attn_decode_noalloc",
     "halo_kv_page_gather",
     "halo_kv_page_scatter", "halo_kv_page_scatter_kv", "halo_kv_page_copy",
+    "halo_kvq_pool_bytes", "halo_kvq_page_scatter_kv", "halo_kvq_page_gather_kv", "halo_kvq_page_copy",
     "halo_kv_step_tables", "halo_rope_params_default", "halo_rope_turns", "halo_rope_qk",
     "halo_prefix_tree_build", "halo_prefix_tree_get", "halo_prefix_tree_destroy",
     "halo_status_string", "halo_last_error_message",
@@ -194,6 +195,16 @@ def load_library(require_gpu=False):
     lib.halo_kv_page_scatter_kv.restype = ctypes.c_int
     lib.halo_kv_page_copy.argtypes = [vp, ctypes.POINTER(AttnParams), vp, vp, ctypes.c_int32, vp, vp]
     lib.halo_kv_page_copy.restype = ctypes.c_int
+    lib.halo_kvq_pool_bytes.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_int]
+    lib.halo_kvq_pool_bytes.restype = ctypes.c_int64
+    lib.halo_kvq_page_scatter_kv.argtypes = [vp, vp, ctypes.POINTER(AttnParams), vp, vp, vp, vp, vp, ctypes.c_int32,
+                                             vp, vp, vp, vp]
+    lib.halo_kvq_page_scatter_kv.restype = ctypes.c_int
+    lib.halo_kvq_page_gather_kv.argtypes = [vp, vp, ctypes.POINTER(AttnParams), vp, vp, vp, vp, ctypes.c_int32,
+                                            vp, vp, vp, vp]
+    lib.halo_kvq_page_gather_kv.restype = ctypes.c_int
+    lib.halo_kvq_page_copy.argtypes = [vp, ctypes.POINTER(AttnParams), ctypes.c_int, vp, vp, ctypes.c_int32, vp, vp]
+    lib.halo_kvq_page_copy.restype = ctypes.c_int
     lib.halo_kv_step_tables.argtypes = [ctypes.POINTER(StepSizes), vp, vp, vp, vp, vp, ctypes.POINTER(_StepTables),
                                         vp, vp]
     lib.halo_kv_step_tables.restype = ctypes.c_int
@@ -714,6 +725,119 @@ def bind_kv_page_copy(pool, params, src_pages, dst_pages, error_flag=None, strea
     return call
 
 
+def kvq_pool_bytes(params, pool_kind):
+    """Bytes of a 4-bit pool of params' pages (halo_kvq_pool_bytes)."""
+    n = load_library().halo_kvq_pool_bytes(ctypes.byref(params), int(pool_kind))
+    if n < 0:
+        raise HaloError(HALO_ERR_INVALID_ARGUMENT, _LIB.halo_last_error_message().decode())
+    return n
+
+
+def alloc_kvq_pools(params, device="cuda"):
+    """(k_pool, v_pool): 4-bit pools [pages, kv heads, tile bytes] of zeros."""
+    import torch
+    d = params.head_dim
+    for kind in (HALO_POOL_K, HALO_POOL_V):
+        kvq_pool_bytes(params, kind)   # (refuses what the library does not hold)
+    return tuple(torch.zeros((int(params.num_pool_pages), params.num_kv_heads, n), dtype=torch.uint8, device=device)
+                 for n in (d * 8 + d // 2, d * 8 + 32))
+
+
+def _kvq_pools(k_pool, v_pool, params):
+    import torch
+    for t, name, kind in ((k_pool, "k_pool", HALO_POOL_K), (v_pool, "v_pool", HALO_POOL_V)):
+        _gpu(t, name, torch.uint8, kvq_pool_bytes(params, kind))
+
+
+def _flag(error_flag):
+    import torch
+    return [] if error_flag is None else [_gpu(error_flag, "error_flag", torch.int32, 1)]
+
+
+def _kvq_scatter_args(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_start, seq_count, in_token_offset, k_src,
+                      v_src, error_flag, stream):
+    import torch
+    _kvq_pools(k_pool, v_pool, params)
+    n = _page_lists(page_ids, seq_page_indptr)
+    for t, name in ((seq_start, "seq_start"), (seq_count, "seq_count")):
+        _gpu(t, name, torch.int32, n)
+    _gpu(in_token_offset, "in_token_offset", torch.int64, n)
+    for t, name in ((k_src, "k_src"), (v_src, "v_src")):
+        _gpu(t, name, _torch_dtype(params.kv_dtype))
+    used = [k_pool, v_pool, page_ids, seq_page_indptr, seq_start, seq_count, in_token_offset, k_src, v_src]
+    _one_gpu(used + _flag(error_flag), stream)
+    return (k_pool.data_ptr(), v_pool.data_ptr(), ctypes.byref(params), page_ids.data_ptr(),
+            seq_page_indptr.data_ptr(), seq_start.data_ptr(), seq_count.data_ptr(), in_token_offset.data_ptr(), n,
+            k_src.data_ptr(), v_src.data_ptr(), error_flag.data_ptr() if error_flag is not None else None,
+            _stream_handle(stream))
+
+
+def kvq_page_scatter_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_start, seq_count, in_token_offset,
+                        k_src, v_src, error_flag=None, stream=None):
+    """halo_kvq_page_scatter_kv on torch tensors: tokens of params' kv_dtype
+    quantised into 4-bit pools (uint8, see alloc_kvq_pools)."""
+    load_library()
+    _check(_LIB.halo_kvq_page_scatter_kv(*_kvq_scatter_args(k_pool, v_pool, params, page_ids, seq_page_indptr,
+                                                            seq_start, seq_count, in_token_offset, k_src, v_src,
+                                                            error_flag, stream)))
+
+
+def bind_kvq_page_scatter_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_start, seq_count,
+                             in_token_offset, k_src, v_src, error_flag=None, stream=None):
+    """kvq_page_scatter_kv as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kvq_page_scatter_kv,
+                  _kvq_scatter_args(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_start, seq_count,
+                                    in_token_offset, k_src, v_src, error_flag, stream))
+
+
+def _kvq_gather_args(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, out_token_offset, k_out, v_out,
+                     error_flag, stream):
+    import torch
+    n = _page_lists(page_ids, seq_page_indptr)
+    _gpu(seq_len, "seq_len", torch.int32, n)
+    _gpu(out_token_offset, "out_token_offset", torch.int64, n)
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        _gpu(t, name, _torch_dtype(params.kv_dtype))
+    _kvq_pools(k_pool, v_pool, params)
+    _one_gpu([k_pool, v_pool, page_ids, seq_page_indptr, seq_len, out_token_offset, k_out, v_out] + _flag(error_flag),
+             stream)
+    return (k_pool.data_ptr(), v_pool.data_ptr(), ctypes.byref(params), page_ids.data_ptr(),
+            seq_page_indptr.data_ptr(), seq_len.data_ptr(), out_token_offset.data_ptr(), n, k_out.data_ptr(),
+            v_out.data_ptr(), error_flag.data_ptr() if error_flag is not None else None, _stream_handle(stream))
+
+
+def kvq_page_gather_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, out_token_offset, k_out, v_out,
+                       error_flag=None, stream=None):
+    """halo_kvq_page_gather_kv on torch tensors: the values that 4-bit pages
+    stand for, in params' kv_dtype."""
+    load_library()
+    _check(_LIB.halo_kvq_page_gather_kv(*_kvq_gather_args(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len,
+                                                          out_token_offset, k_out, v_out, error_flag, stream)))
+
+
+def bind_kvq_page_gather_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, out_token_offset, k_out, v_out,
+                            error_flag=None, stream=None):
+    """kvq_page_gather_kv as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kvq_page_gather_kv,
+                  _kvq_gather_args(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, out_token_offset,
+                                   k_out, v_out, error_flag, stream))
+
+
+def kvq_page_copy(pool, params, pool_kind, src_pages, dst_pages, error_flag=None, stream=None):
+    """halo_kvq_page_copy on torch tensors (int arrays on the GPU)."""
+    import torch
+    load_library()
+    _gpu(pool, "pool", torch.uint8, kvq_pool_bytes(params, pool_kind))
+    _gpu(src_pages, "src_pages", torch.int32)
+    _gpu(dst_pages, "dst_pages", torch.int32, src_pages.numel())
+    _one_gpu([pool, src_pages, dst_pages] + _flag(error_flag), stream)
+    _check(_LIB.halo_kvq_page_copy(pool.data_ptr(), ctypes.byref(params), int(pool_kind), src_pages.data_ptr(),
+                                   dst_pages.data_ptr(), int(src_pages.numel()),
+                                   error_flag.data_ptr() if error_flag is not None else None, _stream_handle(stream)))
+
+
 class StepTables:
     """The outputs of kv_step_tables (torch tensors on one GPU): the page
     lists, ranges and offsets that kv_page_scatter_kv and kv_page_gather take,
@@ -761,9 +885,7 @@ def _step_args(tables, seq_len, seq_new, block_table, free_pages, free_next, err
         for other, what in ((seq_len, "seq_len"), (seq_new, "seq_new"), (free_next, "free_next")):
             if _overlap(t, other):
                 raise ValueError(f"{what} must not overlap the output {name}")
-    if error_flag is not None:
-        used.append(_gpu(error_flag, "error_flag", torch.int32, 1))
-    _one_gpu(used, stream)
+    _one_gpu(used + _flag(error_flag), stream)
     sizes = StepSizes(n, 16, block_table.shape[1], free_pages.numel(), tables.max_tokens, tables.max_pages)
     return (ctypes.byref(sizes), seq_len.data_ptr(), seq_new.data_ptr(), block_table.data_ptr(),
             free_pages.data_ptr(), free_next.data_ptr(), ctypes.byref(_StepTables(**ptrs)),
