@@ -395,6 +395,24 @@ halo_status_t halo_kvq_page_copy(void* pool, const halo_attn_params_t* params, h
                                  const int32_t* src_pages, const int32_t* dst_pages, int32_t num_pages,
                                  int32_t* error_flag, void* stream);
 
+/* halo_prefix_attn_decode and halo_prefix_attn_prefill over 4-bit pools, with the
+ * same plans, metadata, workspaces and errors: k_pool and v_pool hold
+ * halo_kvq_pool_bytes each, kv_dtype is the type of q. The result is that of
+ * attention over the values the pools stand for: for bf16 queries as exact as
+ * over bf16 pools, for fp32 queries as over fp32 pools (4-bit values are exact in
+ * bf16, so fp32 queries and softmax weights are multiplied in three bf16 parts).
+ * Slots past a segment's length may hold any bytes. */
+halo_status_t halo_prefix_attn_decode_kvq(const halo_plan_t* plan, const void* device_meta,
+                                          const void* q, const void* k_pool, const void* v_pool,
+                                          void* o, float* lse,
+                                          void* workspace, size_t workspace_bytes,
+                                          void* stream);
+halo_status_t halo_prefix_attn_prefill_kvq(const halo_plan_t* plan, const void* device_meta,
+                                           const void* q, const void* k_pool, const void* v_pool,
+                                           void* o, float* lse,
+                                           void* workspace, size_t workspace_bytes,
+                                           void* stream);
+
 /* Page lists, positions and slots of one step, built on the GPU from the
  * lengths of its sequences: the arrays that the scatter and the gather take,
  * without a copy from the host. Sequence i holds seq_len[i] tokens in the first

@@ -38,7 +38,7 @@ HIP_FLAGS = [
 ]
 
 HOST_SOURCES = ["halo_plan.cpp", "halo_forest.cpp", "halo_rope.cpp"]
-HIP_SOURCES = ["halo_kernels.hip", "halo_pages.hip", "halo_step.hip", "halo_kvq_pages.hip"]
+HIP_SOURCES = ["halo_kernels.hip", "halo_pages.hip", "halo_step.hip", "halo_kvq_attn.hip", "halo_kvq_pages.hip"]
 PROBE_SOURCES = ["halo_probe.hip"]
 
 

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "halo_internal.h"
+#include "halo_kvq_format.h"
 
 namespace halo {
 
@@ -38,6 +39,9 @@ struct AttnArgs {
   int32_t num_kv_heads;
   float scale_log2;   // sm_scale * log2(e)
 };
+
+// The items of a plan over 4-bit pools (halo_kvq_attn.hip).
+void launch_attention_kvq(AttnArgs args, const halo_plan& plan, hipStream_t stream);
 
 }  // namespace halo
 
@@ -283,6 +287,38 @@ struct RecLane {
   int32_t q_row, aux, page;
 };
 
+// The end of a narrow item: lane (col, grp) holds dims 16b + 4grp .. + 3 of row
+// col in acc[b], and its share of the row's sum.
+template <typename T, int D, typename TO>
+__device__ __forceinline__ void finish_item(const AttnArgs& a, const Item& it, const Row& row, int col, int grp,
+                                            f32x4_t (&acc)[D / 16], float m, float lsum) {
+  constexpr int NB = D / 16;
+  lsum = rows_sum(lsum);
+  const bool has_row = col < it.n_rows;
+  const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+  const float lse2 = lsum > 0.f ? m + __log2f(lsum) : kNegInf;
+  if (it.part_base >= 0) {
+    if (sizeof(T) == 4 && has_row && (it.flags & kItemPiece)) {   // (bf16 pieces are wide items)
+      const int64_t prow = (int64_t)it.part_base + col;
+      float* dst = static_cast<float*>(a.part_o) + prow * D + 4 * grp;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) store4(dst + 16 * b, acc[b] * inv);
+      if (grp == 0) reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
+    } else if (has_row) {
+      const int64_t prow = row.slot;
+      TO* dst = static_cast<TO*>(a.part_o) + prow * D + 4 * grp;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) store4_part(dst + 16 * b, acc[b] * inv);
+      if (grp == 0) reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
+    }
+  } else if (has_row) {
+    TO* dst = static_cast<TO*>(a.o) + (int64_t)row.q_row * D + 4 * grp;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) store4(dst + 16 * b, acc[b] * inv);
+    if (grp == 0 && a.lse) a.lse[row.q_row] = lse2 == kNegInf ? kNegInf : lse2 * kLn2;
+  }
+}
+
 // Waves per workgroup: 8 for bf16 (two per SIMD, so one wave's softmax
 // overlaps another's MFMAs), 4 for fp32, whose operand registers allow only
 // one wave per SIMD.
@@ -329,8 +365,27 @@ constexpr float kRescaleLog2 = 8.f;
 // of 1 KB.
 template <int D, int S> constexpr int wide_ring_bytes() { return S * (D / 16 + 2 * (D / 32)) * 1024; }
 
+// 4-bit pools (KVQ). The loads go to registers instead: a wave has one of the
+// step's four tiles (K and V of two pages; with 8 waves, half of one), one or two
+// instructions of it. kKvqStages registers later it converts them to bf16 (one
+// instruction per two values, the K scale included) and writes them into the step
+// image in the form above, which from there on is read as any other; every value
+// is converted once for the workgroup's rows. An image is written two steps before
+// its V is read, so kKvqStages of them are enough, each with the 32 V scales of its
+// step. A V scale varies along the keys of a dim, so it is put on the softmax's
+// weights instead of on V: P V = (P scale) codes, with the sum of the weights taken
+// before.
+constexpr int kKvqStages = 3;
+template <int D> constexpr int kvq_image_bytes() { return (D / 16 + 2 * (D / 32)) * 1024 + 128; }
+
+// What a wave holds of a step's codes, and of its scales.
+template <int ND> struct KvqRegs {
+  uint32_t w[ND];
+  uint32_t scale;
+};
+
 // A workgroup of W waves and an S-stage ring.
-template <int D, typename TO, int W, int S>
+template <int D, typename TO, int W, int S, bool KVQ = false>
 __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_t* smem) {
   using T = __bf16;
   using F = bf16x8_t;
@@ -343,7 +398,10 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   static_assert(S >= 4 && S % 2 == 0, "the ring needs >= 4 stages, an even count keeps tile parity static");
   constexpr int64_t kTile = 16 * D;
   static_assert(S * kStepBytes == (wide_ring_bytes<D, S>()), "ring size");
-  uint8_t (*lds)[kStepBytes] = reinterpret_cast<uint8_t (*)[kStepBytes]>(smem);
+  constexpr int kImageBytes = KVQ ? kvq_image_bytes<D>() : kStepBytes;
+  constexpr int kImages = KVQ ? kKvqStages : S;
+  static_assert(!KVQ || S == 2 * kKvqStages, "images and registers are indexed by the step's stage modulo kKvqStages");
+  uint8_t (*lds)[kImageBytes] = reinterpret_cast<uint8_t (*)[kImageBytes]>(smem);
 
   const int wave = threadIdx.x >> 6;
   const int uwave = __builtin_amdgcn_readfirstlane(wave);   // on the scalar unit, for addresses
@@ -443,6 +501,79 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
           img + (uwave + W * k) * 1024, 16, 0, 0);
     }
   };
+  // ---- 4-bit loads: tile `tile` of the step (K of pages 0 and 1, then V), of
+  // which this wave has part `half`
+  constexpr int ND = KVQ ? NO / (W / 4) : 1;   // dwords of codes per lane
+  using Regs = KvqRegs<ND>;
+  const int q_tile = uwave / (W / 4), q_half = uwave % (W / 4);
+  const bool q_is_k = q_tile < 2;
+  // K: dwords ND half .. of unit (g, token) = lane. V: unit (bq, h, c) = lane
+  // modulo their number, dwords ND sub .. of its four
+  constexpr int kUnits = D / 2;
+  const int q_unit = q_is_k ? lane : lane % kUnits;
+  const int q_sub = q_is_k ? q_half : lane / kUnits + 64 / kUnits * q_half;
+  const int q_bytes = q_is_k ? kvq_k_tile<D>() : kvq_v_tile<D>();
+  const uint32_t q_off = q_unit * (q_is_k ? D / 8 : 16) + q_sub * ND * 4;
+  const uint32_t q_scale_off = D * 8 + (q_is_k ? (lane & 15) * NO + q_half * ND : 2 * (lane & 15));
+  const uint8_t* q_base = static_cast<const uint8_t*>(q_is_k ? a.k_pool : a.v_pool) + (int64_t)it.kv_head * q_bytes;
+  const int64_t q_stride = (int64_t)a.num_kv_heads * q_bytes;
+  // where the first dword's 8 values go in an image (the others: K 1 KB on, V
+  // by the dim blocks below)
+  const int q_v_blk = 4 * (q_unit / 32) + q_sub * ND;   // 16-dim block of the first dword
+  const uint32_t q_to = q_is_k ? (q_tile & 1) * (NK / 2) * 1024 + (4 * q_sub * ND + (lane >> 4)) * 256 + (lane & 15) * 16
+                               : (NK + (q_tile & 1) * NO) * 1024 + ((q_unit >> 4) & 1) * 512 + (q_unit & 15) * 16;
+  auto q_fetch = [&](const StepPos& p, Regs& r) {
+    const int64_t page = uniform64((int64_t)(uint32_t)(q_tile & 1 ? p.pid1 : p.pid0) * q_stride);
+    const uint8_t* base = reinterpret_cast<const uint8_t*>(uniform64(reinterpret_cast<int64_t>(q_base) + page));
+    if constexpr (ND == 4) {
+      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(base + q_off);
+#pragma unroll
+      for (int k = 0; k < ND; ++k) r.w[k] = x[k];
+    } else if constexpr (ND == 2) {
+      const u32x2_t x = *reinterpret_cast<const u32x2_t*>(base + q_off);
+#pragma unroll
+      for (int k = 0; k < ND; ++k) r.w[k] = x[k];
+    } else {
+      r.w[0] = *reinterpret_cast<const uint32_t*>(base + q_off);
+    }
+    // K: the ND scale bytes of this lane's dwords; V: the scale of slot lane % 16
+    if (q_is_k) {
+      if constexpr (ND == 4) r.scale = *reinterpret_cast<const uint32_t*>(base + q_scale_off);
+      else if constexpr (ND == 2) r.scale = *reinterpret_cast<const uint16_t*>(base + q_scale_off);
+      else r.scale = base[q_scale_off];
+    } else {
+      r.scale = *reinterpret_cast<const uint16_t*>(base + q_scale_off);
+    }
+  };
+  auto q_store = [&](const StepPos& p, const Regs& r, uint8_t* img) {
+    if (q_is_k) {
+#pragma unroll
+      for (int k = 0; k < ND; ++k)
+        *reinterpret_cast<bf16x8_t*>(img + q_to + k * 1024) =
+            kvq_decode_bf16(r.w[k], kvq_scale((r.scale >> (8 * k)) & 0xff));
+    } else {
+#pragma unroll
+      for (int k = 0; k < ND; ++k) {
+        const int b = q_v_blk + k;
+        *reinterpret_cast<bf16x8_t*>(img + q_to + (b >> 1) * 1024 + (b & 1) * 256) = kvq_decode_bf16(r.w[k], 1.f);
+      }
+      if (q_half == 0 && lane < 16) {
+        // slot order to token order; keys past the span may have any scale
+        const int key = 16 * (q_tile & 1) + ((lane & 3) | (lane & 4) << 1 | (lane & 8) >> 1);
+        reinterpret_cast<uint32_t*>(img + kStepBytes)[key] = p.t0 + key < p.key_end ? r.scale << 16 : 0u;
+      }
+    }
+  };
+  // The V scales of this lane's 16 keys of a step.
+  auto read_scales = [&](const uint8_t* img, float (&sc)[16]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(img + kStepBytes + (8 * q + 4 * h) * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[4 * q + i] = x[i];
+    }
+  };
+
   // K fragment s of a step image: this lane's key and units 2s + h.
   const int k_rd = (c >> 4) * (NK / 2) * 1024 + h * 256 + (c & 15) * 16;
   auto k_at = [&](const uint8_t* img, int s) { return img + k_rd + s / 2 * 1024 + s % 2 * 512; };
@@ -504,7 +635,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 
   // Online softmax of one step's scores into P (bf16, RNE), one operand per
   // page of the step (registers 0-7: page 0, 8-15: page 1).
-  auto softmax = [&](const StepPos& p, const f32x16_t& sacc, F (&pf)[2]) {
+  auto softmax = [&](const StepPos& p, const f32x16_t& sacc, const uint8_t* img, F (&pf)[2]) {
     // raw scores (masked ones -inf); the scale is applied inside the exponent
     // with one FMA (scale > 0, so it commutes with the max)
     float sv[16];
@@ -536,6 +667,14 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
     for (int i = 0; i < 16; i += 4) ps += (pr[i] + pr[i + 1]) + (pr[i + 2] + pr[i + 3]);
     lsum += ps;
+    if constexpr (KVQ) {
+      float sc[16];
+      read_scales(img, sc);
+      // (a hidden key of the chunk may have a NaN scale)
+      const int lim = (p.causal ? min(p.key_end, row.qpos + 1) : p.key_end) - p.t0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) pr[i] = skey(i) < lim ? pr[i] * sc[i] : 0.f;
+    }
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       float half[8];
@@ -567,6 +706,8 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
     for (int s = 0; s < NK; ++s) sn = mma32(kf[s], qf[s], sn);
     read_v(img_v, vf);
+    float sc[16];
+    if constexpr (KVQ) read_scales(img_v, sc);
     // softmax of step t (no masks: full step); the max as a tree of
     // three-input maxima (v_max3_f32, 8 instructions for 16 scores)
     auto max3 = [](float x, float y, float z) { return fmaxf(fmaxf(x, y), z); };
@@ -589,7 +730,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     for (int g = 0; g < 2; ++g) {
       float half[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) half[j] = pr[8 * g + j];
+      for (int j = 0; j < 8; ++j) half[j] = KVQ ? pr[8 * g + j] * sc[8 * g + j] : pr[8 * g + j];
       pf_cur[g] = to_frag(half, (F*)nullptr);
     }
     float ps = 0.f;
@@ -614,7 +755,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * NO, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * NO + (KVQ ? 4 : 0), 0);
 #pragma unroll
     for (int k = 0; k < NK - 1; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -636,15 +777,26 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   StepPos ps[S];
   ps[0] = advance();
   if (ps[0].valid) {
+    Regs qr[KVQ ? kKvqStages : 1];
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) {
       if (i > 0) ps[i] = advance();
-      issue(pick(ps[i].valid, ps[i], ps[0]), lds[i]);
+      if constexpr (KVQ) {
+        q_fetch(pick(ps[i].valid, ps[i], ps[0]), qr[i % kKvqStages]);
+        if (i < 2) q_store(ps[i], qr[i], lds[i]);
+      } else {
+        issue(pick(ps[i].valid, ps[i], ps[0]), lds[i]);
+      }
     }
     f32x16_t sacc[2];
     F pf[2][2];
     F vf[2][NO];
-    wait_vmcnt<(S - 3) * kLoadsPerWave>();
+    if constexpr (KVQ) {
+      asm volatile("" ::: "memory");
+      wait_lgkmcnt0();
+    } else {
+      wait_vmcnt<(S - 3) * kLoadsPerWave>();
+    }
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (computes) qk(lds[0], sacc[0]);
@@ -654,32 +806,40 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
       for (int st = 0; st < S; ++st) {
         const int cur_p = st & 1, nxt_p = cur_p ^ 1;
         const int nx = (st + 1) % S, pv_st = (st + S - 1) % S;
-        wait_vmcnt<(S - 3) * kLoadsPerWave>();
+        if constexpr (KVQ) asm volatile("" ::: "memory");
+        else wait_vmcnt<(S - 3) * kLoadsPerWave>();
         wait_lgkmcnt0();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const StepPos prev = ps[pv_st];   // step t-1, whose V is in vf
         ps[pv_st] = advance();
-        issue(pick(ps[pv_st].valid, ps[pv_st], ps[st]), lds[pv_st]);
+        if constexpr (KVQ) {
+          // step t+2 into the image of step t-1; step t+S-1 into its registers
+          constexpr int R = kKvqStages;
+          q_store(ps[(st + 2) % S], qr[(st + 2) % R], lds[(st + 2) % R]);
+          q_fetch(pick(ps[pv_st].valid, ps[pv_st], ps[st]), qr[(st + 2) % R]);
+        } else {
+          issue(pick(ps[pv_st].valid, ps[pv_st], ps[st]), lds[pv_st]);
+        }
         const bool more = ps[nx].valid;
         const bool fast = !first && more && ps[st].full && prev.full;
         if (computes && fast) {
           float alpha;
-          fast_iter(vf, lds[nx], lds[st], pf[nxt_p], sacc[cur_p], sacc[nxt_p], pf[cur_p], alpha);
+          fast_iter(vf, lds[nx % kImages], lds[st % kImages], pf[nxt_p], sacc[cur_p], sacc[nxt_p], pf[cur_p], alpha);
           if (__any(alpha != 1.f)) {
 #pragma unroll
             for (int b = 0; b < NO; ++b) acc[b] *= alpha;
           }
         } else if (computes) {
           if (!first) {
-            mask_v(prev, vf);
+            if constexpr (!KVQ) mask_v(prev, vf);   // (4-bit codes are finite, and the weights 0)
             pv(vf, pf[nxt_p]);
           }
-          if (more) qk(lds[nx], sacc[nxt_p]);
-          softmax(ps[st], sacc[cur_p], pf[cur_p]);
-          read_v(lds[st], vf);
+          if (more) qk(lds[nx % kImages], sacc[nxt_p]);
+          softmax(ps[st], sacc[cur_p], lds[st % kImages], pf[cur_p]);
+          read_v(lds[st % kImages], vf);
           if (!more) {
-            mask_v(ps[st], vf);
+            if constexpr (!KVQ) mask_v(ps[st], vf);
             pv(vf, pf[cur_p]);
           }
         }
@@ -726,6 +886,35 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
           store4(dst + 32 * b + 8 * q, f32x4_t{acc[b][4 * q], acc[b][4 * q + 1], acc[b][4 * q + 2], acc[b][4 * q + 3]} * inv);
       if (h == 0 && a.lse) a.lse[row.q_row] = lse2 == kNegInf ? kNegInf : lse2 * kLn2;
     }
+  }
+}
+
+// ---------------------------------------------------------------- host side
+
+int pad_to(int n, int m) { return (n + m - 1) / m * m; }
+
+// Share (percent) of the narrow rounds interleaved with the wide ones; the
+// rest run after the last wide round.
+constexpr int kWideSpanNarrowPct = 80;
+
+int lcm_int(int a, int b) {
+  int x = a, y = b;
+  while (y) {
+    const int t = x % y;
+    x = y;
+    y = t;
+  }
+  return a / x * b;
+}
+
+// The wide role's blocks: whole dispatch cycles of wide rounds, each a multiple
+// of wide_group rounds.
+void lay_out_rounds(AttnArgs& args, bool wide) {
+  args.wide_blocks =
+      (wide && args.n_wide > 0) ? pad_to(args.n_wide, 8 * lcm_int(args.wide_group, kSeCycle)) : 0;
+  {
+    const int ws = args.wide_blocks / (8 * kSeCycle), ns = args.narrow_blocks / (8 * kSeCycle);
+    args.wide_span = ws + (int)((int64_t)ns * kWideSpanNarrowPct / 100);
   }
 }
 

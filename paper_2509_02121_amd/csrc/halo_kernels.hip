@@ -303,30 +303,7 @@ __device__ __forceinline__ void run_item(const AttnArgs& a, const Item& it, cons
     }
   }
 
-  lsum = rows_sum(lsum);
-  const bool has_row = col < it.n_rows;
-  const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-  const float lse2 = lsum > 0.f ? m + __log2f(lsum) : kNegInf;
-  if (it.part_base >= 0) {
-    if (sizeof(T) == 4 && has_row && (it.flags & kItemPiece)) {   // (bf16 pieces are wide items)
-      const int64_t prow = (int64_t)it.part_base + col;
-      float* dst = static_cast<float*>(a.part_o) + prow * D + 4 * grp;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) store4(dst + 16 * b, acc[b] * inv);
-      if (grp == 0) reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
-    } else if (has_row) {
-      const int64_t prow = row.slot;
-      TO* dst = static_cast<TO*>(a.part_o) + prow * D + 4 * grp;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) store4_part(dst + 16 * b, acc[b] * inv);
-      if (grp == 0) reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
-    }
-  } else if (has_row) {
-    TO* dst = static_cast<TO*>(a.o) + (int64_t)row.q_row * D + 4 * grp;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) store4(dst + 16 * b, acc[b] * inv);
-    if (grp == 0 && a.lse) a.lse[row.q_row] = lse2 == kNegInf ? kNegInf : lse2 * kLn2;
-  }
+  finish_item<T, D, TO>(a, it, row, col, grp, acc, m, lsum);
 }
 
 // Narrow workgroup `block` runs the items in its narrow_slots slots (dealt
@@ -746,38 +723,16 @@ halo_status_t hip_check(const char* what) {
   return HALO_OK;
 }
 
-int pad_to(int n, int m) { return (n + m - 1) / m * m; }
-
-// Share (percent) of the narrow rounds interleaved with the wide ones; the
-// rest run after the last wide round.
-constexpr int kWideSpanNarrowPct = 80;
-
 // A workgroup merges one row where there are more than kMergeK0 partials per
 // row (fewer take one round anyway) and at most kMergeRowMax rows: two rounds
 // of workgroups on the chip (1024 rows of 10 partials: 103 us both ways; 2048
 // of 31: 194.5 -> 192.7 us; 256 of 15: 24.1 -> 22.5 us; whole calls).
 constexpr int kMergeRowMax = 4096;
 
-int lcm_int(int a, int b) {
-  int x = a, y = b;
-  while (y) {
-    const int t = x % y;
-    x = y;
-    y = t;
-  }
-  return a / x * b;
-}
-
 template <typename T, int D, typename TO>
-void launch_attention(AttnArgs args, const MergeArgs& margs, int wide_rb, bool small_wide, hipStream_t stream) {
+void launch_attention(AttnArgs args, int wide_rb, bool small_wide, hipStream_t stream) {
   const int rb = sizeof(T) == 2 ? wide_rb : 0;
-  // whole dispatch cycles of wide rounds, each a multiple of wide_group rounds
-  args.wide_blocks =
-      (rb > 0 && args.n_wide > 0) ? pad_to(args.n_wide, 8 * lcm_int(args.wide_group, kSeCycle)) : 0;
-  {
-    const int ws = args.wide_blocks / (8 * kSeCycle), ns = args.narrow_blocks / (8 * kSeCycle);
-    args.wide_span = ws + (int)((int64_t)ns * kWideSpanNarrowPct / 100);
-  }
+  lay_out_rounds(args, rb > 0);
   constexpr int W = block_waves<T>();
   const int grid = args.wide_blocks + args.narrow_blocks;
   if (grid > 0) {
@@ -793,6 +748,10 @@ void launch_attention(AttnArgs args, const MergeArgs& margs, int wide_rb, bool s
       hipLaunchKernelGGL((attn_kernel<T, D, TO, 0>), dim3(grid), dim3(64 * W), 0, stream, args);
     }
   }
+}
+
+template <int D, typename TO>
+void launch_merge(const MergeArgs& margs, hipStream_t stream) {
   if (margs.n_merge > 0 && margs.n_merge <= kMergeRowMax && margs.n_parts > kMergeK0 * (int64_t)margs.n_merge) {
     hipLaunchKernelGGL((merge_row_kernel<D, TO>), dim3(margs.n_merge), dim3(256), 0, stream, margs);
   } else if (margs.n_merge > 0) {
@@ -815,7 +774,8 @@ void launch_merge_items(MergeItemArgs args, int n_items, int most_rows, int64_t 
   hipLaunchKernelGGL((merge_items_kernel<D, TO>), dim3(n_items * args.blocks_per_item), dim3(256), 0, stream, args);
 }
 
-halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, const void* device_meta,
+// kvq: k_pool and v_pool are 4-bit ones.
+halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq, const void* device_meta,
                             const void* q, const void* k_pool, const void* v_pool, void* o, float* lse,
                             void* workspace, size_t workspace_bytes, void* stream) {
   clear_error();
@@ -873,17 +833,26 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, const vo
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();   // clear any stale error of the caller
   const bool out_f32 = p.out_dtype == HALO_F32;
-  if (p.kv_dtype == HALO_BF16) {
+  if (kvq) {
+    launch_attention_kvq(args, *plan, st);
+  } else if (p.kv_dtype == HALO_BF16) {
     if (D == 128) {
-      if (out_f32) launch_attention<__bf16, 128, float>(args, margs, plan->wide_rb, plan->small_wide, st);
-      else launch_attention<__bf16, 128, __bf16>(args, margs, plan->wide_rb, plan->small_wide, st);
+      if (out_f32) launch_attention<__bf16, 128, float>(args, plan->wide_rb, plan->small_wide, st);
+      else launch_attention<__bf16, 128, __bf16>(args, plan->wide_rb, plan->small_wide, st);
     } else {
-      if (out_f32) launch_attention<__bf16, 64, float>(args, margs, plan->wide_rb, plan->small_wide, st);
-      else launch_attention<__bf16, 64, __bf16>(args, margs, plan->wide_rb, plan->small_wide, st);
+      if (out_f32) launch_attention<__bf16, 64, float>(args, plan->wide_rb, plan->small_wide, st);
+      else launch_attention<__bf16, 64, __bf16>(args, plan->wide_rb, plan->small_wide, st);
     }
   } else {
-    if (D == 128) launch_attention<float, 128, float>(args, margs, plan->wide_rb, plan->small_wide, st);
-    else launch_attention<float, 64, float>(args, margs, plan->wide_rb, plan->small_wide, st);
+    if (D == 128) launch_attention<float, 128, float>(args, plan->wide_rb, plan->small_wide, st);
+    else launch_attention<float, 64, float>(args, plan->wide_rb, plan->small_wide, st);
+  }
+  if (D == 128) {
+    if (out_f32) launch_merge<128, float>(margs, st);
+    else launch_merge<128, __bf16>(margs, st);
+  } else {
+    if (out_f32) launch_merge<64, float>(margs, st);
+    else launch_merge<64, __bf16>(margs, st);
   }
   if (plan->n_merge_items > 0 && !whole) {
     const MergeItemArgs ma{static_cast<const float*>(part_o), part_lse,
@@ -1029,7 +998,7 @@ extern "C" halo_status_t halo_prefix_attn_decode(const halo_plan_t* plan, const 
                                                  const void* q, const void* k_pool, const void* v_pool,
                                                  void* o, float* lse, void* workspace,
                                                  size_t workspace_bytes, void* stream) {
-  return run_attention(plan, false, device_meta, q, k_pool, v_pool, o, lse, workspace, workspace_bytes,
+  return run_attention(plan, false, false, device_meta, q, k_pool, v_pool, o, lse, workspace, workspace_bytes,
                        stream);
 }
 
@@ -1037,8 +1006,22 @@ extern "C" halo_status_t halo_prefix_attn_prefill(const halo_plan_t* plan, const
                                                   const void* q, const void* k_pool, const void* v_pool,
                                                   void* o, float* lse, void* workspace,
                                                   size_t workspace_bytes, void* stream) {
-  return run_attention(plan, true, device_meta, q, k_pool, v_pool, o, lse, workspace, workspace_bytes,
+  return run_attention(plan, true, false, device_meta, q, k_pool, v_pool, o, lse, workspace, workspace_bytes,
                        stream);
+}
+
+extern "C" halo_status_t halo_prefix_attn_decode_kvq(const halo_plan_t* plan, const void* device_meta,
+                                                     const void* q, const void* k_pool, const void* v_pool,
+                                                     void* o, float* lse, void* workspace,
+                                                     size_t workspace_bytes, void* stream) {
+  return run_attention(plan, false, true, device_meta, q, k_pool, v_pool, o, lse, workspace, workspace_bytes, stream);
+}
+
+extern "C" halo_status_t halo_prefix_attn_prefill_kvq(const halo_plan_t* plan, const void* device_meta,
+                                                      const void* q, const void* k_pool, const void* v_pool,
+                                                      void* o, float* lse, void* workspace,
+                                                      size_t workspace_bytes, void* stream) {
+  return run_attention(plan, true, true, device_meta, q, k_pool, v_pool, o, lse, workspace, workspace_bytes, stream);
 }
 
 // ---------------------------------------------------------------- no-alloc decode
@@ -1093,6 +1076,6 @@ extern "C" halo_status_t halo_prefix_attn_decode_noalloc(const halo_plan_t* plan
     halo_status_t st = scratch_of_current_device(&ws);
     if (st != HALO_OK) return st;
   }
-  return run_attention(plan, false, device_meta, q, k_pool, v_pool, o, lse, ws,
+  return run_attention(plan, false, false, device_meta, q, k_pool, v_pool, o, lse, ws,
                        ws ? (size_t)HALO_NOALLOC_SCRATCH_BYTES : 0, stream);
 }

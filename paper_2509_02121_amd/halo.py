@@ -87,6 +87,7 @@ EXPORTED_SYMBOLS = (
     "halo_prefix_attn_decode", "halo_prefix_attn_prefill", "halo_prefix_attn_decode_noalloc",
     "halo_kv_page_gather",
     "halo_kv_page_scatter", "halo_kv_page_scatter_kv", "halo_kv_page_copy",
+    "halo_prefix_attn_decode_kvq", "halo_prefix_attn_prefill_kvq",
     "halo_kvq_pool_bytes", "halo_kvq_page_scatter_kv", "halo_kvq_page_gather_kv", "halo_kvq_page_copy",
     "halo_kv_step_tables", "halo_rope_params_default", "halo_rope_turns", "halo_rope_qk",
     "halo_prefix_tree_build", "halo_prefix_tree_get", "halo_prefix_tree_destroy",
@@ -178,7 +179,8 @@ def load_library(require_gpu=False):
     lib.halo_plan_get_stats.restype = ctypes.c_int
     lib.halo_plan_inspect.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(PlanLayout)]
     lib.halo_plan_inspect.restype = ctypes.c_int
-    for name in ("halo_prefix_attn_decode", "halo_prefix_attn_prefill"):
+    for name in ("halo_prefix_attn_decode", "halo_prefix_attn_prefill", "halo_prefix_attn_decode_kvq",
+                 "halo_prefix_attn_prefill_kvq"):
         fn = getattr(lib, name)
         fn.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         fn.restype = ctypes.c_int
@@ -487,7 +489,7 @@ def _nbytes(t):
     return t.numel() * t.element_size()
 
 
-def _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, library_workspace=False):
+def _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, library_workspace=False, kvq=False):
     """Every buffer a run call reads or writes is checked against the plan's
     sizes before any launch: the kernels index q, o and lse by the plan's
     query rows and the pools by its page ids, so an undersized tensor would
@@ -497,8 +499,12 @@ def _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, library_
     p = plan.params
     kv = _torch_dtype(p.kv_dtype)
     rows = plan.num_query_rows * p.num_q_heads
-    need = [(device_meta, "device_meta", plan.device_meta_bytes, "bytes"),
-            (k_pool, "k_pool", _pool_elems(p), "elements"), (v_pool, "v_pool", _pool_elems(p), "elements"),
+    if kvq:
+        pools = [(k_pool, "k_pool", kvq_pool_bytes(p, HALO_POOL_K), "bytes"),
+                 (v_pool, "v_pool", kvq_pool_bytes(p, HALO_POOL_V), "bytes")]
+    else:
+        pools = [(k_pool, "k_pool", _pool_elems(p), "elements"), (v_pool, "v_pool", _pool_elems(p), "elements")]
+    need = [(device_meta, "device_meta", plan.device_meta_bytes, "bytes"), *pools,
             (o, "o", rows * p.head_dim, "elements")]
     if lse is not None:
         need.append((lse, "lse", rows, "elements"))
@@ -514,8 +520,8 @@ def _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, library_
         raise ValueError(f"workspace has {ws} bytes, the plan needs {plan.workspace_bytes}")
     _gpu(device_meta, "device_meta")
     _gpu(q, "q", kv)
-    _gpu(k_pool, "k_pool", kv)
-    _gpu(v_pool, "v_pool", kv)
+    _gpu(k_pool, "k_pool", torch.uint8 if kvq else kv)
+    _gpu(v_pool, "v_pool", torch.uint8 if kvq else kv)
     _gpu(o, "o", _torch_dtype(p.out_dtype))
     if lse is not None:
         _gpu(lse, "lse", torch.float32)
@@ -523,8 +529,8 @@ def _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, library_
         _gpu(workspace, "workspace")
 
 
-def _run(fn, plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream):
-    _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace)
+def _run(fn, plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream, kvq=False):
+    _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, kvq=kvq)
     ws_ptr = workspace.data_ptr() if workspace is not None else None
     ws_bytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
     _check(fn(plan._handle, device_meta.data_ptr(), q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
@@ -540,6 +546,16 @@ def prefix_attn_decode(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, 
 def prefix_attn_prefill(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream=None):
     """halo_prefix_attn_prefill on torch tensors (all on one GPU)."""
     _run(_LIB.halo_prefix_attn_prefill, plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream)
+
+
+def prefix_attn_decode_kvq(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream=None):
+    """halo_prefix_attn_decode_kvq on torch tensors: 4-bit pools (uint8)."""
+    _run(_LIB.halo_prefix_attn_decode_kvq, plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream, True)
+
+
+def prefix_attn_prefill_kvq(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream=None):
+    """halo_prefix_attn_prefill_kvq on torch tensors: 4-bit pools (uint8)."""
+    _run(_LIB.halo_prefix_attn_prefill_kvq, plan, device_meta, q, k_pool, v_pool, o, lse, workspace, stream, True)
 
 
 # Largest workspace the no-alloc decode entry point serves (HALO_NOALLOC_SCRATCH_BYTES).
@@ -1014,11 +1030,18 @@ def bind_rope_qk(q, k, positions, rope, q_out=None, k_out=None, stream=None):
     return _bound(_LIB.halo_rope_qk, _rope_args(q, k, positions, rope, q_out, k_out, stream))
 
 
+def _kvq_pair(k_pool, v_pool):
+    """Whether the pools are 4-bit ones (both or neither)."""
+    import torch
+    return k_pool.dtype == torch.uint8 and v_pool.dtype == torch.uint8
+
+
 class PrefixAttention:
     """Plan + uploaded metadata + workspace for one forest on one GPU.
 
     run() enqueues the whole path (attention items, then the merge) on the
-    current stream and returns (o, lse).
+    current stream and returns (o, lse). Pools of uint8 are 4-bit ones
+    (alloc_kvq_pools), any other are of params' kv_dtype.
 
     The device metadata is double-buffered. update() uploads the next batch
     step's plan into the buffer the current step does not use, after every
@@ -1220,12 +1243,14 @@ class PrefixAttention:
         is being captured, one from the graph's own pool: the graph may then
         replay on any stream, beside any other call of this object."""
         import torch
-        fn = _LIB.halo_prefix_attn_prefill if self.plan.is_prefill else _LIB.halo_prefix_attn_decode
+        kvq = _kvq_pair(k_pool, v_pool)
+        fn = getattr(_LIB, ("halo_prefix_attn_prefill" if self.plan.is_prefill else "halo_prefix_attn_decode") +
+                     ("_kvq" if kvq else ""))
         capturing = torch.cuda.is_current_stream_capturing
         n = self.plan.workspace_bytes
         # (bound during a capture: the graph's memory is not for eager calls)
         ws = None if capturing() else self._workspace_on(stream)
-        _check_run(self.plan, self.meta, q, k_pool, v_pool, o, lse, ws, library_workspace=ws is None)
+        _check_run(self.plan, self.meta, q, k_pool, v_pool, o, lse, ws, library_workspace=ws is None, kvq=kvq)
         s = self._before_run(stream)
         self._bound[self._cur].add(s)
         tensors = (self.plan._handle, self.meta.data_ptr(), q.data_ptr(), k_pool.data_ptr(),
@@ -1268,7 +1293,10 @@ class PrefixAttention:
         if o is None:
             o, lse_new = self.alloc_outputs(q)
             lse = lse if lse is not None else lse_new
-        fn = prefix_attn_prefill if self.plan.is_prefill else prefix_attn_decode
+        if _kvq_pair(k_pool, v_pool):
+            fn = prefix_attn_prefill_kvq if self.plan.is_prefill else prefix_attn_decode_kvq
+        else:
+            fn = prefix_attn_prefill if self.plan.is_prefill else prefix_attn_decode
         s = self._before_run(stream)
         ws = self._current_workspace(s) if stream is None else self._workspace_on(s)
         with self._enqueue:

@@ -152,3 +152,54 @@ def test_arguments(lib):
             halo.kvq_page_gather_kv(*args)
     with pytest.raises(ValueError):
         halo.kvq_page_copy(k, p, halo.HALO_POOL_K, i32, one)
+
+
+@pytest.mark.parametrize("kind", [0, 1])
+@pytest.mark.parametrize("D", [64, 128])
+def test_vectorised_reading(kind, D):
+    """The helper that the GPU tests read whole pools with."""
+    from kvq_helpers import values
+    rng = np.random.default_rng(kind + D)
+    tiles = rng.integers(0, 256, (3, 2, paged_kvq.tile_bytes(kind, D)), dtype=np.uint8)
+    got = values(tiles, kind, D)
+    for n in range(3):
+        for h in range(2):
+            for t in range(16):
+                with np.errstate(all="ignore"):
+                    assert np.array_equal(got[n, t, h], paged_kvq.read_token(tiles[n, h], kind, D, t), equal_nan=True)
+
+
+def test_attention_arguments(lib):
+    """Pools too small, of another type than the other one, or on the host."""
+    from workloads import build_workload
+    w = build_workload("args", 1, 4, 2, 64, torch.bfloat16, [20, 5], [[0, 1]])
+    p = halo.make_params(4, 2, 64, torch.bfloat16, w.num_pool_pages, w.scale)
+    plan = halo.Plan.from_csr(p, w.forest_csr())
+    k, v = halo.alloc_kvq_pools(p, "cpu")
+    meta = torch.zeros(plan.device_meta_bytes, dtype=torch.uint8)
+    o, lse = torch.zeros_like(w.q), torch.zeros(w.q.shape[:2])
+    ws = torch.zeros(max(plan.workspace_bytes, 1), dtype=torch.uint8)
+    for bad in ((k[:-1], v), (k, v[:, :, :-1]), (k, v.view(torch.int8)), (w.k_pool, v), (k, v)):
+        with pytest.raises(ValueError):
+            halo.prefix_attn_decode_kvq(plan, meta, w.q, *bad, o, lse, ws)
+
+
+@pytest.mark.parametrize("name,prefill", [("halo_prefix_attn_decode_kvq", False), ("halo_prefix_attn_prefill_kvq", True)])
+def test_attention_refusals(lib, name, prefill):
+    from workloads import build_workload
+    w = build_workload("args", 1, 4, 2, 64, torch.bfloat16, [300, 5], [[0, 1]], [5] if prefill else None)
+    p = halo.make_params(4, 2, 64, torch.bfloat16, w.num_pool_pages, w.scale)
+    csr = w.forest_csr()
+    plan = halo.Plan.from_csr(p, csr)
+    other = halo.Plan.from_csr(p, {**csr, "q_len": None if prefill else np.array([5], np.int32)})
+    keep, at = _address()
+    at = (at + 255) // 256 * 256
+    fn = getattr(lib, name)
+    good = [plan._handle, at, at, at, at, at, at, at, 1 << 40, None]
+    for i, bad in ((0, None), (0, other._handle), (1, None), (2, None), (3, None), (4, None), (5, None), (1, at + 16),
+                   (2, at + 4), (3, at + 8), (4, at + 2), (5, at + 1)):
+        args = list(good)
+        args[i] = bad
+        assert fn(*args) == halo.HALO_ERR_INVALID_ARGUMENT, i
+    if not prefill and plan.workspace_bytes:
+        assert fn(*good[:8], 0, None) == halo.HALO_ERR_WORKSPACE_TOO_SMALL
