@@ -366,22 +366,23 @@ constexpr float kRescaleLog2 = 8.f;
 template <int D, int S> constexpr int wide_ring_bytes() { return S * (D / 16 + 2 * (D / 32)) * 1024; }
 
 // 4-bit pools (KVQ). The loads go to registers instead: a wave has one of the
-// step's four tiles (K and V of two pages; with 8 waves, half of one), one or two
-// instructions of it. kKvqStages registers later it converts them to bf16 (one
-// instruction per two values, the K scale included) and writes them into the step
-// image in the form above, which from there on is read as any other; every value
-// is converted once for the workgroup's rows. An image is written two steps before
-// its V is read, so kKvqStages of them are enough, each with the 32 V scales of its
-// step. A V scale varies along the keys of a dim, so it is put on the softmax's
-// weights instead of on V: P V = (P scale) codes, with the sum of the weights taken
-// before.
-constexpr int kKvqStages = 3;
+// step's four tiles (K and V of two pages; with 8 waves, half of one), two
+// instructions of it. An iteration later it converts them to bf16, scales
+// included, and writes them into the step image in the form above, which from
+// there on is read as any other; every value is converted once for the
+// workgroup's rows. K is one conversion per two values. V scales run along the
+// keys of a dim: see kvq_decode_keys. (On the softmax's weights instead, 16 products
+// and 4 LDS reads a step for every wave, they took registers that had to be
+// spilled: chunked prefill 1765 us.) Only in a step with masked keys, whose scales
+// may be NaN, are they put on the weights, with the masked ones at 0.
+constexpr int kKvqStages = 4;
 template <int D> constexpr int kvq_image_bytes() { return (D / 16 + 2 * (D / 32)) * 1024 + 128; }
 
-// What a wave holds of a step's codes, and of its scales.
+// What a lane holds of a step: ND dwords of codes; of K their scale bytes, of V
+// the scales of the 8 keys in bf16.
 template <int ND> struct KvqRegs {
   uint32_t w[ND];
-  uint32_t scale;
+  u32x4_t scale;
 };
 
 // A workgroup of W waves and an S-stage ring.
@@ -400,7 +401,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   static_assert(S * kStepBytes == (wide_ring_bytes<D, S>()), "ring size");
   constexpr int kImageBytes = KVQ ? kvq_image_bytes<D>() : kStepBytes;
   constexpr int kImages = KVQ ? kKvqStages : S;
-  static_assert(!KVQ || S == 2 * kKvqStages, "images and registers are indexed by the step's stage modulo kKvqStages");
+  static_assert(!KVQ || S == kKvqStages, "an image for each stage of the step ring");
   uint8_t (*lds)[kImageBytes] = reinterpret_cast<uint8_t (*)[kImageBytes]>(smem);
 
   const int wave = threadIdx.x >> 6;
@@ -514,7 +515,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   const int q_sub = q_is_k ? q_half : lane / kUnits + 64 / kUnits * q_half;
   const int q_bytes = q_is_k ? kvq_k_tile<D>() : kvq_v_tile<D>();
   const uint32_t q_off = q_unit * (q_is_k ? D / 8 : 16) + q_sub * ND * 4;
-  const uint32_t q_scale_off = D * 8 + (q_is_k ? (lane & 15) * NO + q_half * ND : 2 * (lane & 15));
+  const uint32_t q_scale_off = D * 8 + (q_is_k ? (lane & 15) * NO + q_half * ND : 16 * ((q_unit >> 4) & 1));
   const uint8_t* q_base = static_cast<const uint8_t*>(q_is_k ? a.k_pool : a.v_pool) + (int64_t)it.kv_head * q_bytes;
   const int64_t q_stride = (int64_t)a.num_kv_heads * q_bytes;
   // where the first dword's 8 values go in an image (the others: K 1 KB on, V
@@ -536,13 +537,12 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     } else {
       r.w[0] = *reinterpret_cast<const uint32_t*>(base + q_off);
     }
-    // K: the ND scale bytes of this lane's dwords; V: the scale of slot lane % 16
     if (q_is_k) {
-      if constexpr (ND == 4) r.scale = *reinterpret_cast<const uint32_t*>(base + q_scale_off);
-      else if constexpr (ND == 2) r.scale = *reinterpret_cast<const uint16_t*>(base + q_scale_off);
-      else r.scale = base[q_scale_off];
+      if constexpr (ND == 4) r.scale[0] = *reinterpret_cast<const uint32_t*>(base + q_scale_off);
+      else if constexpr (ND == 2) r.scale[0] = *reinterpret_cast<const uint16_t*>(base + q_scale_off);
+      else r.scale[0] = base[q_scale_off];
     } else {
-      r.scale = *reinterpret_cast<const uint16_t*>(base + q_scale_off);
+      r.scale = *reinterpret_cast<const u32x4_t*>(base + q_scale_off);
     }
   };
   auto q_store = [&](const StepPos& p, const Regs& r, uint8_t* img) {
@@ -550,21 +550,36 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
       for (int k = 0; k < ND; ++k)
         *reinterpret_cast<bf16x8_t*>(img + q_to + k * 1024) =
-            kvq_decode_bf16(r.w[k], kvq_scale((r.scale >> (8 * k)) & 0xff));
+            kvq_decode_bf16(r.w[k], kvq_scale((r.scale[0] >> (8 * k)) & 0xff));
     } else {
+      float scale[8];
 #pragma unroll
-      for (int k = 0; k < ND; ++k) {
-        const int b = q_v_blk + k;
-        *reinterpret_cast<bf16x8_t*>(img + q_to + (b >> 1) * 1024 + (b & 1) * 256) = kvq_decode_bf16(r.w[k], 1.f);
+      for (int j = 0; j < 8; ++j)
+        scale[j] = __uint_as_float(j & 1 ? r.scale[j >> 1] & 0xffff0000u : r.scale[j >> 1] << 16);
+      if (!p.full) {
+        // slots 8 hh + j are keys 8 (j / 4) + 4 hh + j % 4 of the page
+        if (q_sub == 0 && (q_unit & ~16) == 0) {
+          const int hh = q_unit >> 4;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            reinterpret_cast<float*>(img + kStepBytes)[16 * (q_tile & 1) + 8 * (j >> 2) + 4 * hh + (j & 3)] = scale[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) scale[j] = 1.f;
       }
-      if (q_half == 0 && lane < 16) {
-        // slot order to token order; keys past the span may have any scale
-        const int key = 16 * (q_tile & 1) + ((lane & 3) | (lane & 4) << 1 | (lane & 8) >> 1);
-        reinterpret_cast<uint32_t*>(img + kStepBytes)[key] = p.t0 + key < p.key_end ? r.scale << 16 : 0u;
+#pragma unroll
+      for (int k = 0; k < ND; k += 2) {
+        F f[2];
+        kvq_decode_keys(r.w[k], k + 1 < ND ? r.w[k + 1 < ND ? k + 1 : k] : 0u, scale, f[0], f[1]);
+#pragma unroll
+        for (int i = 0; i < 2 && k + i < ND; ++i) {
+          const int b = q_v_blk + k + i;
+          *reinterpret_cast<F*>(img + q_to + (b >> 1) * 1024 + (b & 1) * 256) = f[i];
+        }
       }
     }
   };
-  // The V scales of this lane's 16 keys of a step.
+  // The V scales of this lane's 16 keys of a step that has masked ones.
   auto read_scales = [&](const uint8_t* img, float (&sc)[16]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -667,10 +682,9 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
     for (int i = 0; i < 16; i += 4) ps += (pr[i] + pr[i + 1]) + (pr[i + 2] + pr[i + 3]);
     lsum += ps;
-    if constexpr (KVQ) {
+    if (KVQ && !p.full) {
       float sc[16];
       read_scales(img, sc);
-      // (a hidden key of the chunk may have a NaN scale)
       const int lim = (p.causal ? min(p.key_end, row.qpos + 1) : p.key_end) - p.t0;
 #pragma unroll
       for (int i = 0; i < 16; ++i) pr[i] = skey(i) < lim ? pr[i] * sc[i] : 0.f;
@@ -706,8 +720,6 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
     for (int s = 0; s < NK; ++s) sn = mma32(kf[s], qf[s], sn);
     read_v(img_v, vf);
-    float sc[16];
-    if constexpr (KVQ) read_scales(img_v, sc);
     // softmax of step t (no masks: full step); the max as a tree of
     // three-input maxima (v_max3_f32, 8 instructions for 16 scores)
     auto max3 = [](float x, float y, float z) { return fmaxf(fmaxf(x, y), z); };
@@ -730,7 +742,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     for (int g = 0; g < 2; ++g) {
       float half[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) half[j] = KVQ ? pr[8 * g + j] * sc[8 * g + j] : pr[8 * g + j];
+      for (int j = 0; j < 8; ++j) half[j] = pr[8 * g + j];
       pf_cur[g] = to_frag(half, (F*)nullptr);
     }
     float ps = 0.f;
@@ -755,7 +767,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * NO + (KVQ ? 4 : 0), 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * NO, 0);
 #pragma unroll
     for (int k = 0; k < NK - 1; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -777,13 +789,13 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   StepPos ps[S];
   ps[0] = advance();
   if (ps[0].valid) {
-    Regs qr[KVQ ? kKvqStages : 1];
+    Regs qr;
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) {
       if (i > 0) ps[i] = advance();
       if constexpr (KVQ) {
-        q_fetch(pick(ps[i].valid, ps[i], ps[0]), qr[i % kKvqStages]);
-        if (i < 2) q_store(ps[i], qr[i], lds[i]);
+        q_fetch(pick(ps[i].valid, ps[i], ps[0]), qr);
+        if (i < 2) q_store(ps[i], qr, lds[i]);
       } else {
         issue(pick(ps[i].valid, ps[i], ps[0]), lds[i]);
       }
@@ -815,9 +827,8 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
         ps[pv_st] = advance();
         if constexpr (KVQ) {
           // step t+2 into the image of step t-1; step t+S-1 into its registers
-          constexpr int R = kKvqStages;
-          q_store(ps[(st + 2) % S], qr[(st + 2) % R], lds[(st + 2) % R]);
-          q_fetch(pick(ps[pv_st].valid, ps[pv_st], ps[st]), qr[(st + 2) % R]);
+          q_store(ps[(st + 2) % S], qr, lds[(st + 2) % S]);
+          q_fetch(pick(ps[pv_st].valid, ps[pv_st], ps[st]), qr);
         } else {
           issue(pick(ps[pv_st].valid, ps[pv_st], ps[st]), lds[pv_st]);
         }

@@ -320,7 +320,7 @@ __device__ __forceinline__ void narrow_block_kvq(const AttnArgs& a, int block) {
 }
 
 // Both roles in one launch, dealt as in attn_kernel.
-constexpr int kKvqStepStages = 2 * kKvqStages;
+constexpr int kKvqStepStages = kKvqStages;
 
 template <typename T, int D, typename TO, int RB>
 __global__ __launch_bounds__(64 * block_waves<T>())

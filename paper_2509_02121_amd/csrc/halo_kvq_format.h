@@ -39,6 +39,33 @@ __device__ __forceinline__ void kvq_decode_f32(uint32_t w, float scale, float (&
   v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
   v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
 }
+// 8 codes each of two dims of the same 8 keys, times the keys' scales: a byte of
+// two codes of one key is put together first, so that one conversion does both
+// dims with the key's scale.
+__device__ __forceinline__ void kvq_decode_keys(uint32_t w0, uint32_t w1, const float (&scale)[8], kvq_bf16x8_t& f0,
+                                                kvq_bf16x8_t& f1) {
+  constexpr uint32_t kLow = 0x0f0f0f0fu;
+  const uint32_t a = (w0 & kLow) | ((w1 << 4) & ~kLow);   // keys 0, 2, 4, 6
+  const uint32_t b = ((w0 >> 4) & kLow) | (w1 & ~kLow);   // keys 1, 3, 5, 7
+  const uint32_t c[8] = {
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale[0], 0)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, scale[1], 0)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale[2], 1)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, scale[3], 1)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale[4], 2)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, scale[5], 2)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, scale[6], 3)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(b, scale[7], 3))};
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 lo, hi;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lo[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100u);
+    hi[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302u);
+  }
+  f0 = __builtin_bit_cast(kvq_bf16x8_t, lo);
+  f1 = __builtin_bit_cast(kvq_bf16x8_t, hi);
+}
 // The nearest codes of 8 values over a power of two, ties to the even code,
 // magnitudes past 6 to 6.
 __device__ __forceinline__ uint32_t kvq_encode(const float (&v)[8], float scale) {
