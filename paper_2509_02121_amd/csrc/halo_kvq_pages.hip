@@ -94,7 +94,9 @@ struct KvqScatterArgs {
   int64_t num_pool_pages;
   int32_t num_seqs;
   int32_t num_kv_heads;
-  int32_t splits;   // workgroups per sequence
+  int32_t seq_blocks;    // workgroups by sequence (partly touched pages)
+  int32_t splits;        // of them per sequence
+  int32_t tile_blocks;   // workgroups for the whole pages' tiles
 };
 
 // Tokens lo .. hi - 1 (of 0 .. 15) of one tile; src: the dense row of token 0 of
@@ -168,41 +170,67 @@ __device__ __forceinline__ void write_tile(const T* src, int64_t row, uint8_t* t
   }
 }
 
-// A workgroup per sequence and split; its waves take every (4 splits)-th of the
-// sequence's tiles (pages, then heads, K before V).
+// A tile of page `pslot` of a page list: K and V of the heads in turn.
+template <typename T, int D>
+__device__ __forceinline__ void scatter_tile(const KvqScatterArgs& a, int64_t at, int base, int pslot, int hv, int lo,
+                                             int hi, int lane) {
+  const int H = a.num_kv_heads, h = hv >> 1;
+  const int64_t row = (int64_t)H * D;
+  const int pid = a.page_ids[base + pslot];
+  if (pid < 0 || pid >= a.num_pool_pages) {
+    if (lane == 0 && a.error_flag) a.error_flag[0] = 1;
+    return;
+  }
+  const int64_t from = (at + (int64_t)pslot * 16) * row + (int64_t)h * D;   // token 0 of the page
+  const int64_t tile = (int64_t)pid * H + h;
+  if (hv & 1)
+    write_tile<T, D, true>(static_cast<const T*>(a.in[1]) + from, row, a.pool[1] + tile * kvq_v_tile<D>(), lo, hi, lane);
+  else
+    write_tile<T, D, false>(static_cast<const T*>(a.in[0]) + from, row, a.pool[0] + tile * kvq_k_tile<D>(), lo, hi, lane);
+}
+
+// Two kinds of workgroups, as in scatter_kernel: `splits` for each sequence take the
+// tiles of its partly touched first and last pages (an append: one page, a wave for
+// each of its tiles), and tile_blocks share the whole pages of all sequences
+// equally. Against splits of every sequence's tiles, whole pages or not: 64
+// appends 8.7 -> 4.6 us, 496 appends and 16 chunks 87 -> 18 us (8 heads, d 128).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kvq_scatter_kernel(KvqScatterArgs a) {
+  __shared__ int sums[260];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int H = a.num_kv_heads;
-  const int64_t row = (int64_t)H * D;
-  for (int seq = (int)blockIdx.x / a.splits; seq < a.num_seqs; seq += (int)gridDim.x / a.splits) {
-    const int start = a.seq_start[seq], count = a.seq_count[seq];
-    const int base = a.seq_page_indptr[seq], next = a.seq_page_indptr[seq + 1];
-    const int64_t off = a.in_token_offset[seq];
-    if (count <= 0) continue;
+  if ((int)blockIdx.x < a.seq_blocks) {
     const int first_tile = (int)blockIdx.x % a.splits * 4 + wave;
-    if (start < 0 || (int64_t)start + count > (int64_t)(next - base) * 16) {
-      if (first_tile == 0 && lane == 0 && a.error_flag) a.error_flag[0] = 1;
-      continue;
-    }
-    const int first = start / 16, pages = (start + count - 1) / 16 - first + 1;
-    const int64_t tiles = (int64_t)pages * 2 * H;
-    for (int64_t k = first_tile; k < tiles; k += 4 * a.splits) {
-      const int p = first + (int)(k / (2 * H)), hv = (int)(k % (2 * H)), h = hv >> 1;
-      const int pid = a.page_ids[base + p];
-      if (pid < 0 || pid >= a.num_pool_pages) {
-        if (hv == 0 && lane == 0 && a.error_flag) a.error_flag[0] = 1;
+    for (int seq = (int)blockIdx.x / a.splits; seq < a.num_seqs; seq += a.seq_blocks / a.splits) {
+      const int start = a.seq_start[seq], count = a.seq_count[seq];
+      const int base = a.seq_page_indptr[seq], next = a.seq_page_indptr[seq + 1];
+      const int64_t off = a.in_token_offset[seq];
+      if (count <= 0) continue;
+      if (start < 0 || (int64_t)start + count > (int64_t)(next - base) * 16) {
+        if (first_tile == 0 && lane == 0 && a.error_flag) a.error_flag[0] = 1;
         continue;
       }
-      const int lo = max(start - p * 16, 0), hi = (int)min((int64_t)start + count - (int64_t)p * 16, (int64_t)16);
-      const int64_t at = (off + (int64_t)p * 16 - start) * row + (int64_t)h * D;   // token 0 of the page
-      const int64_t tile = (int64_t)pid * H + h;
-      if (hv & 1)
-        write_tile<T, D, true>(static_cast<const T*>(a.in[1]) + at, row, a.pool[1] + tile * kvq_v_tile<D>(), lo, hi, lane);
-      else
-        write_tile<T, D, false>(static_cast<const T*>(a.in[0]) + at, row, a.pool[0] + tile * kvq_k_tile<D>(), lo, hi, lane);
+      const PageRange r(start, count);
+      const int pages = (r.head ? 1 : 0) + (r.tail ? 1 : 0);
+      for (int k = first_tile; k < pages * 2 * H; k += 4 * a.splits) {
+        const bool second = k >= 2 * H;   // the last page, after the first
+        const int p = r.head && !second ? r.first : r.last;
+        scatter_tile<T, D>(a, off - start, base, p, second ? k - 2 * H : k, max(start - p * 16, 0),
+                           min(start + count - p * 16, 16), lane);
+      }
     }
+    return;
+  }
+  const int tb = (int)blockIdx.x - a.seq_blocks;
+  const int groups = (a.num_seqs + kTileSeqs - 1) / kTileSeqs;
+  for (int g = tb % groups; g < groups; g += a.tile_blocks) {
+    // the workgroups of this group, and this one's turn among them
+    const int of = a.tile_blocks >= groups ? (a.tile_blocks - g + groups - 1) / groups : 1;
+    const int s0 = g * kTileSeqs, n = min(a.num_seqs - s0, kTileSeqs);
+    whole_tiles(a, 2 * H, s0, n, tb / groups * 4 + wave, of * 4, sums, wave, lane,
+                [&](int64_t at, int base, int pslot, int hv) { scatter_tile<T, D>(a, at, base, pslot, hv, 0, 16, lane); });
+    __syncthreads();   // the sums are overwritten for the next group
   }
 }
 
@@ -373,12 +401,17 @@ extern "C" halo_status_t halo_kvq_page_scatter_kv(void* k_pool, void* v_pool, co
   const int H = params->num_kv_heads;
   KvqScatterArgs g{{static_cast<uint8_t*>(k_pool), static_cast<uint8_t*>(v_pool)}, {k_in, v_in}, page_ids,
                    seq_page_indptr, seq_start, seq_count, in_token_offset, error_flag, params->num_pool_pages,
-                   num_seqs, H, 0};
-  // The counts are on the device. An append's 2 H tiles each get a wave, and
-  // where sequences are few each gets the workgroups for a long chunk.
-  const int append = std::min((2 * H + 3) / 4, 64);
-  g.splits = std::max(append, std::min(2048 / num_seqs, 1024));
-  const dim3 grid((unsigned)std::min(num_seqs, 65536) * g.splits);
+                   num_seqs, H, 0, 0, 0};
+  // A wave for each of an append's 2 H tiles, or for two from 257 sequences on,
+  // where the chip takes them in several rounds anyway (512 appends 10.2 -> 9.3 us,
+  // 1024 17.9 -> 16.3; 256 6.4, with two 7.6). 1024 workgroups for the whole pages:
+  // 512 have fewer loads in flight (32 chunks of 768 tokens 29.9 us, 1024 27.5),
+  // 2048 are waited for by appends (64: 5.5 us, 1024 4.6).
+  g.splits = std::min((2 * H + 3) / 4, 64);
+  if (num_seqs > 256) g.splits = (g.splits + 1) / 2;
+  g.seq_blocks = std::min(num_seqs, 16384) * g.splits;
+  g.tile_blocks = 1024;
+  const dim3 grid((unsigned)(g.seq_blocks + g.tile_blocks));
   (void)hipGetLastError();
   by_type(params, [&](auto t, auto d) {
     hipLaunchKernelGGL((kvq_scatter_kernel<decltype(t), decltype(d)::value>), grid, dim3(256), 0,

@@ -173,8 +173,6 @@ struct ScatterArgs {
   int32_t seq_split;     // of them per sequence: 1, or one for each pool
   int32_t tile_blocks;   // workgroups per pool for the whole pages' tiles
 };
-// Sequences whose tiles one workgroup sums.
-constexpr int kTileSeqs = 4096;
 
 // A whole tile (16 tokens of one head): read from the dense input with 16-byte
 // loads, transposed in the wave's own LDS buffer and written in stored order,
@@ -355,128 +353,22 @@ __device__ __forceinline__ void scatter_seq(const ScatterArgs& a, int z, int fir
   }
 }
 
-// The range of one sequence, and its whole-page tiles (none where the range
-// does not fit its page list: its own workgroup flags that).
-struct SeqRange {
-  int start, base, tiles, f0;
-  int64_t off;
-  __device__ __forceinline__ SeqRange(const ScatterArgs& a, int seq) {
-    start = a.seq_start[seq];
-    const int count = a.seq_count[seq];
-    base = a.seq_page_indptr[seq];
-    const int next = a.seq_page_indptr[seq + 1];
-    off = a.in_token_offset[seq];
-    const PageRange r(start, count);
-    f0 = r.f0;
-    const bool fits = count > 0 && start >= 0 && (int64_t)start + count <= (int64_t)(next - base) * 16;
-    tiles = fits ? r.nfull * a.num_kv_heads : 0;
-  }
-};
-
-// Whole pages: the tiles of up to kTileSeqs sequences, shared equally by the
-// waves. Up to 64 sequences every wave sums by itself, one sequence per lane,
-// and finds its tiles in the lanes' registers, without a barrier or a second
-// look at the metadata (32 chunks of 512 tokens, K and V: 30.6 us; by the
-// workgroup 33.5); it takes every turns-th tile, so that neighbouring waves
-// move neighbouring heads of one page (32 fp32 chunks of 512 tokens after other
-// work: 83 us with contiguous runs, 72 so). More are summed by the workgroup,
-// thread i those of sequences i, i + 256, ..., in LDS (1024 appends: 18 us,
-// against 22.7 when every wave sums all of them), and a wave takes a contiguous
-// run. A sequence with fewer than 16 new tokens has no whole page: only its
-// count is read.
 template <typename W, int D, bool V>
 __device__ __forceinline__ void scatter_tiles(const ScatterArgs& a, int z, int s0, int n_seqs, int turn, int turns,
                                               u32x4_t* stage, int (&sums)[260], int wave, int lane) {
   const int H = a.num_kv_heads;
   const int64_t row = (int64_t)H * D;
-  const bool by_wave = n_seqs <= 64;
-  int mine = 0, l_start = 0, l_base = 0, l_f0 = 0, upto, total;
-  int64_t l_off = 0;
-  if (by_wave) {
-    if (lane < n_seqs) {
-      const SeqRange r(a, s0 + lane);
-      mine = r.tiles;
-      l_start = r.start;
-      l_base = r.base;
-      l_f0 = r.f0;
-      l_off = r.off;
-    }
-    if (!__any(mine > 0)) return;
-    upto = wave_inclusive_sum(mine);
-    total = __builtin_amdgcn_readlane(upto, 63);
-  } else {
-    constexpr int kAhead = 4;   // counts in flight per thread
-    for (int i0 = threadIdx.x; i0 < n_seqs; i0 += kAhead * 256) {
-      int count[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) count[u] = i0 + 256 * u < n_seqs ? a.seq_count[s0 + i0 + 256 * u] : 0;
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (count[u] >= 16) mine += SeqRange(a, s0 + i0 + 256 * u).tiles;
-    }
-    if (!__syncthreads_or(mine)) return;
-    upto = wave_inclusive_sum(mine);
-    if (lane == 63) sums[256 + wave] = upto;
-    __syncthreads();
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      upto += w < wave ? sums[256 + w] : 0;
-      total += sums[256 + w];
-    }
-    sums[threadIdx.x] = upto;
-    __syncthreads();
-  }
-  const int per = (int)(((int64_t)total + turns - 1) / turns);
-  int k = by_wave ? turn : (int)min((int64_t)total, (int64_t)turn * per);
-  const int k_end = by_wave ? total : (int)min((int64_t)total, (int64_t)k + per);
-  while (k < k_end) {
-    int t, n, base, f0;
-    int64_t at;   // dense row of the sequence's token 0
-    if (by_wave) {
-      const int lo = __popcll(__ballot(upto <= k));   // the lane whose sequence holds tile k
-      t = k - (lo ? __builtin_amdgcn_readlane(upto, lo - 1) : 0);
-      n = __builtin_amdgcn_readlane(mine, lo);
-      base = __builtin_amdgcn_readlane(l_base, lo);
-      f0 = __builtin_amdgcn_readlane(l_f0, lo);
-      at = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(l_off >> 32), lo) << 32) |
-                     (uint32_t)__builtin_amdgcn_readlane((int)l_off, lo)) -
-           __builtin_amdgcn_readlane(l_start, lo);
-    } else {
-      int lo = 0;   // the thread whose sequences hold tile k
-#pragma unroll
-      for (int j = 0; j < 4; ++j) lo += __popcll(__ballot(sums[64 * j + lane] <= k));
-      t = k - (lo ? sums[lo - 1] : 0);
-      t = __builtin_amdgcn_readfirstlane(t);
-      int seq = s0 + lo;
-      SeqRange r(a, seq);
-      while (t >= r.tiles) {
-        t -= r.tiles;
-        seq += 256;
-        r = SeqRange(a, seq);
-      }
-      n = r.tiles;
-      base = r.base;
-      f0 = r.f0;
-      at = r.off - r.start;
-    }
-    // tiles t .. t_end - 1 of one sequence, heads innermost
-    const int t_end = by_wave ? t + 1 : min(n, t + (k_end - k));
-    k += by_wave ? turns : t_end - t;
+  whole_tiles(a, H, s0, n_seqs, turn, turns, sums, wave, lane, [&](int64_t at, int base, int pslot, int h) {
     const W* in = static_cast<const W*>(a.in[z]) + at * row;
-#pragma nounroll
-    for (; t < t_end; ++t) {
-      const int pslot = f0 + t / H, h = t % H;
-      const int pid = a.page_ids[base + pslot];
-      u32x4_t v[TileWriter<W, D>::NV];
-      TileWriter<W, D>::template load<V>(in + (int64_t)pslot * 16 * row + (int64_t)h * D, row, v, lane);
-      if (pid < 0 || pid >= a.num_pool_pages) {
-        if (lane == 0 && a.error_flag) a.error_flag[0] = 1;
-        continue;
-      }
-      TileWriter<W, D>::template store<V>(v, static_cast<W*>(a.pool[z]) + ((int64_t)pid * H + h) * 16 * D, stage, lane);
+    const int pid = a.page_ids[base + pslot];
+    u32x4_t v[TileWriter<W, D>::NV];
+    TileWriter<W, D>::template load<V>(in + (int64_t)pslot * 16 * row + (int64_t)h * D, row, v, lane);
+    if (pid < 0 || pid >= a.num_pool_pages) {
+      if (lane == 0 && a.error_flag) a.error_flag[0] = 1;
+      return;
     }
-  }
+    TileWriter<W, D>::template store<V>(v, static_cast<W*>(a.pool[z]) + ((int64_t)pid * H + h) * 16 * D, stage, lane);
+  });
 }
 
 template <typename W, int D>

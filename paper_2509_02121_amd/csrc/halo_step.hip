@@ -224,7 +224,8 @@ __device__ __forceinline__ u32x4_t pack(const float (&v)[8]) {
 // as 64 bits after the point, so it is exact to 2^-33 of a turn at any
 // position, where a product in fp32 is off by whole radians at 10^6.
 // Products and sums in fp32, rounded once to the output's type. Bound by HBM:
-// q and k read and written once.
+// q and k read and written once (16384 tokens of 32 + 8 heads, d 128, bf16: 336 MB
+// in 67.7 us, 4.96 TB/s, where a device copy reaches 5.17).
 template <typename T, int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   constexpr int E = 16 / (int)sizeof(T);
@@ -395,12 +396,12 @@ extern "C" halo_status_t halo_rope_qk(const halo_rope_params_t* rope, float ampl
   g.heads = num_q_heads + num_kv_heads;
   g.rotary = rope->rotary_dim;
   // Of a workgroup's 256 threads `slots` share each unit of a token: one for
-  // every head while the chip is not full, fewer (so that angles are worked out
-  // less often) once there are several workgroups for each CU.
+  // every head, as far as they go. Fewer work out the angles less often, but have
+  // fewer loads in flight: 16384 tokens of 32 + 8 heads (d 128) take 67.7 us with
+  // 32, 70.9 with 8, 76.0 with 4; 64 tokens 3.7, 4.8 and 7.1.
   const int units = D * elt / 32, most = 256 / units;
   int slots = 1;
   while (slots < most && slots < g.heads) slots *= 2;
-  while (slots > 4 && (int64_t)num_tokens * slots / most > 8 * kNumCUs) slots /= 2;
   g.slots = slots;
   const int per_block = most / slots;
   const int64_t blocks = ((int64_t)num_tokens + per_block - 1) / per_block;
