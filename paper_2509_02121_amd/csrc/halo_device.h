@@ -83,6 +83,15 @@ __device__ __forceinline__ u32x4_t ld16(const void* p) {
   if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
   else return *reinterpret_cast<const u32x4_t*>(p);
 }
+// A load from an address told to be global. From an integer the compiler makes
+// flat loads, which count as LDS accesses too and which it can only wait for all
+// together.
+template <typename V, bool NT = false>
+__device__ __forceinline__ V load_global(int64_t at) {
+  typedef const V __attribute__((address_space(1))) * global_t;
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<global_t>(at));
+  else return *reinterpret_cast<global_t>(at);
+}
 // K fragment: dims d0..d0+7 of key t in a K tile stored as [D/E][16][E]
 // (E elements per 16-byte unit).
 template <bool NT>
@@ -385,9 +394,9 @@ template <int ND> struct KvqRegs {
   u32x4_t scale;
 };
 
-// A workgroup of W waves and an S-stage ring.
+// A workgroup of W waves and an S-stage ring, for the item's rows from row0 on.
 template <int D, typename TO, int W, int S, bool KVQ = false>
-__device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_t* smem) {
+__device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_t* smem, int row0 = 0) {
   using T = __bf16;
   using F = bf16x8_t;
   constexpr int NK = D / 16;                      // 16-dim slices of Q K^T
@@ -411,10 +420,10 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   const int h = lane >> 5;
   const Item it = a.wide_items[item_id];
   // waves without rows still load their share of every step image
-  const bool computes = wave * 32 < it.n_rows;
+  const bool computes = row0 + wave * 32 < it.n_rows;
 
   // This lane's row: row c of this wave's block.
-  const int r = wave * 32 + c;
+  const int r = row0 + wave * 32 + c;
   const Row row = r < it.n_rows ? a.rows[it.row_begin + r] : Row{-1, 0, -1, -1};
   F qf[NK];
   {
@@ -525,24 +534,24 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
                                : (NK + (q_tile & 1) * NO) * 1024 + ((q_unit >> 4) & 1) * 512 + (q_unit & 15) * 16;
   auto q_fetch = [&](const StepPos& p, Regs& r) {
     const int64_t page = uniform64((int64_t)(uint32_t)(q_tile & 1 ? p.pid1 : p.pid0) * q_stride);
-    const uint8_t* base = reinterpret_cast<const uint8_t*>(uniform64(reinterpret_cast<int64_t>(q_base) + page));
+    const int64_t base = uniform64(reinterpret_cast<int64_t>(q_base) + page);
     if constexpr (ND == 4) {
-      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(base + q_off);
+      const u32x4_t x = load_global<u32x4_t>(base + q_off);
 #pragma unroll
       for (int k = 0; k < ND; ++k) r.w[k] = x[k];
     } else if constexpr (ND == 2) {
-      const u32x2_t x = *reinterpret_cast<const u32x2_t*>(base + q_off);
+      const u32x2_t x = load_global<u32x2_t>(base + q_off);
 #pragma unroll
       for (int k = 0; k < ND; ++k) r.w[k] = x[k];
     } else {
-      r.w[0] = *reinterpret_cast<const uint32_t*>(base + q_off);
+      r.w[0] = load_global<uint32_t>(base + q_off);
     }
     if (q_is_k) {
-      if constexpr (ND == 4) r.scale[0] = *reinterpret_cast<const uint32_t*>(base + q_scale_off);
-      else if constexpr (ND == 2) r.scale[0] = *reinterpret_cast<const uint16_t*>(base + q_scale_off);
-      else r.scale[0] = base[q_scale_off];
+      if constexpr (ND == 4) r.scale[0] = load_global<uint32_t>(base + q_scale_off);
+      else if constexpr (ND == 2) r.scale[0] = load_global<uint16_t>(base + q_scale_off);
+      else r.scale[0] = load_global<uint8_t>(base + q_scale_off);
     } else {
-      r.scale = *reinterpret_cast<const u32x4_t*>(base + q_scale_off);
+      r.scale = load_global<u32x4_t>(base + q_scale_off);
     }
   };
   auto q_store = [&](const StepPos& p, const Regs& r, uint8_t* img) {

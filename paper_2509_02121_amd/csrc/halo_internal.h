@@ -210,6 +210,7 @@ struct halo_plan {
   int32_t n_wide = 0;
   int32_t wide_rb = 0;       // 1 when the plan has wide items (32 rows per wave), else 0
   int32_t wide_group = 1;    // wide items that share pages, kept on one XCD
+  int32_t max_wide_rows = 0; // most rows of a wide item
   bool small_wide = false;   // every item is wide and of at most kSmallWideRows rows
   int32_t n_narrow_blocks = 0;  // workgroups the narrow items are dealt to (a multiple of 8)
   int32_t narrow_slots = 0;     // item slots per narrow workgroup (slot k: wave k)

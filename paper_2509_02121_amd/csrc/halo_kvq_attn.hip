@@ -50,13 +50,6 @@ __device__ __forceinline__ void split(const float (&x)[8], bf16x8_t (&f)[N]) {
     }
 }
 
-// Loads marked non-temporal for keys that one item reads only (see ld16).
-template <bool NT, typename V>
-__device__ __forceinline__ V ld(const void* p) {
-  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
-  else return *reinterpret_cast<const V*>(p);
-}
-
 // One step's codes and scales of a lane: K dwords of 8 dims for the two 16-key
 // tiles, their scale bytes, V dwords of 8 keys, and those keys' scales in bf16.
 template <int D>
@@ -102,10 +95,6 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
     }
   }
 
-  const uint8_t* kbase = static_cast<const uint8_t*>(a.k_pool) + (int64_t)it.kv_head * kTile;
-  const uint8_t* vbase = static_cast<const uint8_t*>(a.v_pool) + (int64_t)it.kv_head * vTile;
-  const int64_t k_stride = (int64_t)a.num_kv_heads * kTile, v_stride = (int64_t)a.num_kv_heads * vTile;
-
   auto load_span = [&](int si) {
     SpanState st;
     st.valid = si < it.n_spans;
@@ -121,69 +110,44 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
     }
     return st;
   };
-  auto step_at = [&](const SpanState& st, int t0) {
-    StepPos p;
-    p.valid = st.valid;
-    p.t0 = t0;
-    p.key_end = st.ke;
-    p.causal = st.causal;
-    const int j = (t0 - st.kb) >> 4;
-    p.has1 = t0 + 16 < st.ke;
-    p.full = t0 + kKeysPerStep <= st.ke && !st.causal;
-    p.pid0 = __builtin_amdgcn_readlane(st.vpid, j);
-    p.pid1 = p.has1 ? __builtin_amdgcn_readlane(st.vpid, j + 1) : p.pid0;
-    return p;
-  };
-  // A step's addresses are, per lane, a scalar base chosen by page and an offset
-  // that never changes. A position past the item's end loads, in every lane, words
-  // at the start of the item table instead (all within its first 2 KB; a table has
-  // at least 8 workgroups of 4 items), so that the count of loads in flight stays
-  // fixed without reading pages again.
-  auto uniform64 = [](int64_t x) {   // on the scalar unit
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
-    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
-    return (int64_t)(((uint64_t)hi << 32) | lo);
-  };
-  const uint32_t k_lane = (grp * 16 + (col & 7)) * (D / 8);
-  const uint32_t ks_lane = D * 8 + (col & 7) * NS;
-  const uint32_t v_lane = ((grp & 1) * 16 + col) * 16;
-  const uint32_t vs_lane = D * 8 + (grp & 1) * 16;
+  // A lane's addresses of a step are page id * page bytes + an address that never
+  // changes, one instruction each for codes and scales of K and V. A position past
+  // the item's end loads from page 0 (of every wave the same few lines), so that
+  // the count of loads in flight stays fixed without reading pages again.
+  const uint32_t k_stride = a.num_kv_heads * kTile, v_stride = a.num_kv_heads * vTile;
+  const uint64_t k_at = reinterpret_cast<uint64_t>(a.k_pool) + (uint64_t)it.kv_head * kTile + (grp * 16 + (col & 7)) * (D / 8);
+  const uint64_t ks_at = reinterpret_cast<uint64_t>(a.k_pool) + (uint64_t)it.kv_head * kTile + D * 8 + (col & 7) * NS;
+  const uint64_t v_at = reinterpret_cast<uint64_t>(a.v_pool) + (uint64_t)it.kv_head * vTile + ((grp & 1) * 16 + col) * 16;
+  const uint64_t vs_at = reinterpret_cast<uint64_t>(a.v_pool) + (uint64_t)it.kv_head * vTile + D * 8 + (grp & 1) * 16;
   auto fetch = [&](const StepPos& p, Regs& r) {
-    const bool live = p.valid;
-    const int64_t idle = reinterpret_cast<int64_t>(a.items);
-    const int64_t k0 = uniform64(live ? reinterpret_cast<int64_t>(kbase) + (int64_t)(uint32_t)p.pid0 * k_stride : idle);
-    const int64_t k1 = uniform64(live ? reinterpret_cast<int64_t>(kbase) + (int64_t)(uint32_t)p.pid1 * k_stride : idle);
-    const int64_t v0 = uniform64(live ? reinterpret_cast<int64_t>(vbase) + (int64_t)(uint32_t)p.pid0 * v_stride : idle);
-    const int64_t v1 = uniform64(live ? reinterpret_cast<int64_t>(vbase) + (int64_t)(uint32_t)p.pid1 * v_stride : idle);
-    const uint8_t* kq = reinterpret_cast<const uint8_t*>((col < 8 ? k0 : k1) + (live ? k_lane : 0u));
-    const uint8_t* kz = reinterpret_cast<const uint8_t*>((col < 8 ? k0 : k1) + (live ? ks_lane : 0u));
-    const uint8_t* vq = reinterpret_cast<const uint8_t*>((grp < 2 ? v0 : v1) + (live ? v_lane : 0u));
-    const uint8_t* vz = reinterpret_cast<const uint8_t*>((grp < 2 ? v0 : v1) + (live ? vs_lane : 0u));
+    const uint32_t k_page = col < 8 ? p.pid0 : p.pid1, v_page = grp < 2 ? p.pid0 : p.pid1;
+    const int64_t kq = k_at + (uint64_t)k_page * k_stride, kz = ks_at + (uint64_t)k_page * k_stride;
+    const int64_t vq = v_at + (uint64_t)v_page * v_stride, vz = vs_at + (uint64_t)v_page * v_stride;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       if constexpr (D == 128) {
-        const u32x4_t w = ld<NT, u32x4_t>(kq + x * D);
+        const u32x4_t w = load_global<u32x4_t, NT>(kq + x * D);
 #pragma unroll
         for (int s = 0; s < NS; ++s) r.k[x][s] = w[s];
-        r.ks[x] = ld<NT, uint32_t>(kz + x * 8 * NS);
+        r.ks[x] = load_global<uint32_t, NT>(kz + x * 8 * NS);
       } else {
-        const u32x2_t w = ld<NT, u32x2_t>(kq + x * D);
+        const u32x2_t w = load_global<u32x2_t, NT>(kq + x * D);
 #pragma unroll
         for (int s = 0; s < NS; ++s) r.k[x][s] = w[s];
-        r.ks[x] = ld<NT, uint16_t>(kz + x * 8 * NS);
+        r.ks[x] = load_global<uint16_t, NT>(kz + x * 8 * NS);
       }
     }
 #pragma unroll
     for (int b = 0; b < NB; b += 4) {
-      const u32x4_t w = ld<NT, u32x4_t>(vq + b * 128);
+      const u32x4_t w = load_global<u32x4_t, NT>(vq + b * 128);
 #pragma unroll
       for (int i = 0; i < 4; ++i) r.v[b + i] = w[i];
     }
-    r.vs = ld<NT, u32x4_t>(vz);
+    r.vs = load_global<u32x4_t, NT>(vz);
   };
 
-  // The span cursor of run_item: a later span's page ids are loaded, and waited
-  // for, when the walk reaches it.
+  // The span cursor: a later span's page ids are loaded, and waited for, when the
+  // walk reaches it (see run_item).
   int si = 0;
   SpanState cur;
   cur.valid = it.n_spans > 0;
@@ -191,16 +155,24 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
   cur.ke = it.s0_key_end;
   cur.causal = it.s0_causal;
   cur.vpid = rl.page;
-  int gs = 0, sb = 0;
+  int t_next = cur.kb;
   auto advance = [&]() {
-    while (cur.valid && gs >= sb + ((cur.ke - cur.kb + kKeysPerStep - 1) >> 5)) {
-      sb += (cur.ke - cur.kb + kKeysPerStep - 1) >> 5;
-      ++si;
-      cur = load_span(si);
+    while (cur.valid && t_next >= cur.ke) {
+      cur = load_span(++si);
       wait_vmcnt<0>();
+      t_next = cur.kb;
     }
-    StepPos p = step_at(cur, cur.kb + (gs - sb) * kKeysPerStep);
-    ++gs;
+    StepPos p;
+    p.valid = cur.valid;
+    p.t0 = t_next;
+    p.key_end = cur.ke;
+    p.causal = cur.causal;
+    p.has1 = t_next + 16 < cur.ke;
+    p.full = t_next + kKeysPerStep <= cur.ke && !cur.causal;
+    const int j = (t_next - cur.kb) >> 4;
+    p.pid0 = cur.valid ? __builtin_amdgcn_readlane(cur.vpid, j) : 0;
+    p.pid1 = p.has1 ? __builtin_amdgcn_readlane(cur.vpid, j + 1) : p.pid0;
+    t_next += kKeysPerStep;
     return p;
   };
 
@@ -211,28 +183,27 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
   for (int b = 0; b < NB; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   auto compute = [&](const StepPos& p, Regs& r) {
-    f32x4_t sacc[2];
+    f32x4_t sacc[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      sacc[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const F kf = kvq_decode_bf16(r.k[x][s], kvq_scale((r.ks[x] >> (8 * s)) & 0xff));
+      for (int x = 0; x < 2; ++x) {
+        const F kf = kvq_decode_bf16(r.k[x][s], kvq_scale_byte(r.ks[x], s));
 #pragma unroll
         for (int n = NP - 1; n >= 0; --n) sacc[x] = mma(kf, qf[n][s], sacc[x]);
       }
-    }
-    // slot j = 4X + i holds key t0 + slot_key(grp, j)
-    const bool full = p.t0 + kKeysPerStep <= p.key_end && !p.causal;
+    // slot j = 4X + i holds key t0 + slot_key(grp, j); raw scores, the scale is
+    // applied with the maximum's subtraction (scale > 0)
     float sv[8], vs[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      sv[j] = sacc[j >> 2][j & 3] * a.scale_log2;
+      sv[j] = sacc[j >> 2][j & 3];
       vs[j] = __uint_as_float(j & 1 ? r.vs[j >> 1] & 0xffff0000u : r.vs[j >> 1] << 16);
     }
-    if (!full) {
+    if (!p.full) {
       // (a key that is not seen may have any scales: NaN scores, and a weight of
       // 0 times a NaN)
+      asm volatile("");   // (a branch, not selects in every step)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int key = p.t0 + slot_key(grp, j);
@@ -241,10 +212,8 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
         vs[j] = vis ? vs[j] : 0.f;
       }
     }
-    float mt = sv[0];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) mt = fmaxf(mt, sv[j]);
-    mt = rows_max(mt);
+    const float m4[2] = {fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7]))};
+    const float mt = rows_max(fmaxf(m4[0], m4[1])) * a.scale_log2;
     // the sums are rescaled only when some row's maximum moves
     if (__any(mt > m)) {
       const float m_new = fmaxf(m, mt);
@@ -256,13 +225,11 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
     }
     const float m_use = m == kNegInf ? 0.f : m;
     float pr[8];
-    float psum = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      pr[j] = __builtin_amdgcn_exp2f(sv[j] - m_use);
-      psum += pr[j];
-      pr[j] *= vs[j];
-    }
+    for (int j = 0; j < 8; ++j) pr[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[j], a.scale_log2, -m_use));
+    const float psum = ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) pr[j] *= vs[j];
     lsum += psum;
     F pf[NP];
     split(pr, pf);
@@ -306,11 +273,27 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
 
 constexpr int kKvqNarrowStages = 3;
 
+// Workgroups of four waves for either role, of which a CU holds two: narrow slots
+// are taken in runs of four (two for a plan's bf16 workgroup of eight), wide items
+// in runs of 128 rows. Next to each other on a CU, a wide workgroup's products and
+// a narrow one's loads and conversions overlap.
+constexpr int kKvqWaves = 4;
+constexpr int kKvqRows = kKvqWaves * 32;
+
 template <typename T, int D, typename TO>
 __device__ __forceinline__ void narrow_block_kvq(const AttnArgs& a, int block) {
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int lane = threadIdx.x & 63;
-  const int64_t item_id = (int64_t)block * block_waves<T>() + wave;
+  // A plan's workgroup stays on its XCD (its index modulo 8), and its runs come
+  // one dispatch cycle after the other, so that they go to the same shader engine:
+  // one workgroup after the other would leave the engines of the second ones idle
+  // where these are empty.
+  constexpr int kRuns = block_waves<T>() / kKvqWaves;
+  const int round = block >> 3, rounds = a.narrow_blocks / (8 * kRuns);
+  const int cycle = round / (kRuns * kSeCycle), width = min(kSeCycle, rounds - cycle * kSeCycle);
+  const int at = round - cycle * kRuns * kSeCycle;
+  const int of = (cycle * kSeCycle + at % width) * 8 + (block & 7);
+  const int64_t item_id = (int64_t)of * block_waves<T>() + at / width * kKvqWaves + wave;
   const Item it = a.items[item_id];
   const ItemRec* rec = a.item_recs + item_id;
   const int col = lane & 15;
@@ -319,14 +302,11 @@ __device__ __forceinline__ void narrow_block_kvq(const AttnArgs& a, int block) {
   else run_item_kvq<T, D, TO, false, kKvqNarrowStages>(a, it, rl, lane);
 }
 
-// Both roles in one launch, dealt as in attn_kernel.
-constexpr int kKvqStepStages = kKvqStages;
-
+// Both roles in one launch, dealt as in attn_kernel; wide unit u is run
+// u % runs of 128 rows of item u / runs.
 template <typename T, int D, typename TO, int RB>
-__global__ __launch_bounds__(64 * block_waves<T>())
-__attribute__((amdgpu_waves_per_eu(block_waves<T>() / 4)))
-void attn_kvq_kernel(AttnArgs a) {
-  static_assert(RB == 0 || block_waves<T>() == kWideWaves, "wide items need kWideWaves-wave blocks");
+__global__ __launch_bounds__(64 * kKvqWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void attn_kvq_kernel(AttnArgs a, int runs) {
   constexpr int kSmem = RB > 0 ? kKvqStages * kvq_image_bytes<D>() : 16;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kSmem];
   const int b = blockIdx.x;
@@ -338,8 +318,9 @@ void attn_kvq_kernel(AttnArgs a) {
     const int w_before = cyc < sp ? (int)((int64_t)cyc * ws / sp) : ws;
     const int w_upto = cyc < sp ? (int)((int64_t)(cyc + 1) * ws / sp) : ws;
     if (w_upto > w_before) {
-      const int item = xcd_remap((w_before * kSeCycle + q) * 8 + x, a.wide_group);
-      if (item < a.n_wide) wide_item<D, TO, kWideWaves, kKvqStepStages, true>(a, item, smem);
+      const int unit = xcd_remap((w_before * kSeCycle + q) * 8 + x, a.wide_group);
+      if (unit < a.n_wide)
+        wide_item<D, TO, kKvqWaves, kKvqStages, true>(a, unit / runs, smem, unit % runs * kKvqRows);
       return;
     }
     narrow_block_kvq<T, D, TO>(a, ((cyc - w_upto) * kSeCycle + q) * 8 + x);
@@ -349,34 +330,40 @@ void attn_kvq_kernel(AttnArgs a) {
   }
 }
 
-// Wide items of at most kSmallWideRows rows and nothing else (prefill).
+// Wide items and nothing else (prefill).
 template <int D, typename TO>
-__global__ __launch_bounds__(64 * kSmallWideWaves) __attribute__((amdgpu_waves_per_eu(2)))
-void wide_kvq_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * kKvqWaves) __attribute__((amdgpu_waves_per_eu(2)))
+void wide_kvq_kernel(AttnArgs a, int runs) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kKvqStages * kvq_image_bytes<D>()];
-  const int item = xcd_remap(blockIdx.x, a.wide_group);
-  if (item < a.n_wide) wide_item<D, TO, kSmallWideWaves, kKvqStepStages, true>(a, item, smem);
+  const int unit = xcd_remap(blockIdx.x, a.wide_group);
+  if (unit < a.n_wide)
+    wide_item<D, TO, kKvqWaves, kKvqStages, true>(a, unit / runs, smem, unit % runs * kKvqRows);
 }
 
 template <typename T, int D, typename TO>
 void launch_items(AttnArgs args, const halo_plan& plan, hipStream_t stream) {
-  const int rb = sizeof(T) == 2 ? plan.wide_rb : 0;
-  lay_out_rounds(args, rb > 0);
+  const bool wide = sizeof(T) == 2 && plan.wide_rb > 0;
+  const int runs = (plan.max_wide_rows + kKvqRows - 1) / kKvqRows;
+  if (wide) {
+    args.n_wide *= runs;
+    args.wide_group *= runs;
+  }
+  args.narrow_blocks *= block_waves<T>() / kKvqWaves;
+  lay_out_rounds(args, wide);
   const int grid = args.wide_blocks + args.narrow_blocks;
   if (grid == 0) return;
-  constexpr int W = block_waves<T>();
   if constexpr (sizeof(T) == 2) {
-    if (rb > 0 && plan.small_wide) {
+    if (wide && args.narrow_blocks == 0) {
       hipLaunchKernelGGL((wide_kvq_kernel<D, TO>), dim3(pad_to(args.n_wide, 8 * args.wide_group)),
-                         dim3(64 * kSmallWideWaves), 0, stream, args);
+                         dim3(64 * kKvqWaves), 0, stream, args, runs);
       return;
     }
-    if (rb > 0) {
-      hipLaunchKernelGGL((attn_kvq_kernel<T, D, TO, 1>), dim3(grid), dim3(64 * W), 0, stream, args);
+    if (wide) {
+      hipLaunchKernelGGL((attn_kvq_kernel<T, D, TO, 1>), dim3(grid), dim3(64 * kKvqWaves), 0, stream, args, runs);
       return;
     }
   }
-  hipLaunchKernelGGL((attn_kvq_kernel<T, D, TO, 0>), dim3(grid), dim3(64 * W), 0, stream, args);
+  hipLaunchKernelGGL((attn_kvq_kernel<T, D, TO, 0>), dim3(grid), dim3(64 * kKvqWaves), 0, stream, args, runs);
 }
 
 }  // namespace

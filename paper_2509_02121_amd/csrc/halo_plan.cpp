@@ -1181,6 +1181,8 @@ extern "C" halo_status_t halo_plan_create_with_options(const halo_attn_params_t*
   plan->n_items = (int32_t)n_real_items;
   plan->n_wide = (int32_t)witems.size();
   if (plan->n_wide == 0) plan->wide_rb = 0;
+  for (const Item& it : witems) plan->max_wide_rows = std::max(plan->max_wide_rows, it.n_rows);
+  for (const Item& it : whole_witems) plan->max_wide_rows = std::max(plan->max_wide_rows, it.n_rows);
   plan->n_spans = (int32_t)spans.size();
   plan->n_rows = (int32_t)rows.size();
   plan->n_merge_parts = (int32_t)merge_parts.size();
