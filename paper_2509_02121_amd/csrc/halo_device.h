@@ -374,24 +374,27 @@ constexpr float kRescaleLog2 = 8.f;
 // of 1 KB.
 template <int D, int S> constexpr int wide_ring_bytes() { return S * (D / 16 + 2 * (D / 32)) * 1024; }
 
-// 4-bit pools (KVQ). The loads go to registers instead: a wave has one of the
-// step's four tiles (K and V of two pages; with 8 waves, half of one), two
-// instructions of it. An iteration later it converts them to bf16, scales
-// included, and writes them into the step image in the form above, which from
-// there on is read as any other; every value is converted once for the
-// workgroup's rows. K is one conversion per two values. V scales run along the
-// keys of a dim: see kvq_decode_keys. (On the softmax's weights instead, 16 products
-// and 4 LDS reads a step for every wave, they took registers that had to be
-// spilled: chunked prefill 1765 us.) Only in a step with masked keys, whose scales
-// may be NaN, are they put on the weights, with the masked ones at 0.
+// 4-bit pools (KVQ, workgroups of four waves). The loads go to registers instead: a
+// wave has half of one page's K tile and half of its V tile. An iteration later it
+// converts them to bf16, scales included, and writes them into the step image in
+// the form above, which from there on is read as any other; every value is
+// converted once for the workgroup's rows. K is one conversion per two values. V
+// scales run along the keys of a dim: see kvq_decode_keys. (On the softmax's weights
+// instead, 16 products and 4 LDS reads a step for every wave, they took registers
+// that had to be spilled: chunked prefill 1765 us, at the conversion 1290.) Only in a
+// step with masked keys, whose scales may be NaN, are they put on the weights, with
+// the masked ones at 0. The conversion has no branch and runs between the MFMAs of
+// the step before: with a K or a V tile to a wave, ahead of them, it cost 280 of
+// 1219 us.
 constexpr int kKvqStages = 4;
 template <int D> constexpr int kvq_image_bytes() { return (D / 16 + 2 * (D / 32)) * 1024 + 128; }
 
-// What a lane holds of a step: ND dwords of codes; of K their scale bytes, of V
-// the scales of the 8 keys in bf16.
+// What a lane holds of a step: ND dwords of K codes and their scale bytes, ND of V
+// codes and the scales of their 8 keys in bf16.
 template <int ND> struct KvqRegs {
-  uint32_t w[ND];
-  u32x4_t scale;
+  uint32_t k[ND], v[ND];
+  uint32_t k_scale;
+  u32x4_t v_scale;
 };
 
 // A workgroup of W waves and an S-stage ring, for the item's rows from row0 on.
@@ -511,81 +514,67 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
           img + (uwave + W * k) * 1024, 16, 0, 0);
     }
   };
-  // ---- 4-bit loads: tile `tile` of the step (K of pages 0 and 1, then V), of
-  // which this wave has part `half`
-  constexpr int ND = KVQ ? NO / (W / 4) : 1;   // dwords of codes per lane
+  // ---- 4-bit loads: half q_half of page q_page's tiles
+  static_assert(!KVQ || W == 4, "a wave for each half of a page's tiles");
+  constexpr int ND = NO / 2;   // dwords of codes per lane, of K and of V
   using Regs = KvqRegs<ND>;
-  const int q_tile = uwave / (W / 4), q_half = uwave % (W / 4);
-  const bool q_is_k = q_tile < 2;
+  const int q_page = uwave & 1, q_half = uwave >> 1;
   // K: dwords ND half .. of unit (g, token) = lane. V: unit (bq, h, c) = lane
   // modulo their number, dwords ND sub .. of its four
   constexpr int kUnits = D / 2;
-  const int q_unit = q_is_k ? lane : lane % kUnits;
-  const int q_sub = q_is_k ? q_half : lane / kUnits + 64 / kUnits * q_half;
-  const int q_bytes = q_is_k ? kvq_k_tile<D>() : kvq_v_tile<D>();
-  const uint32_t q_off = q_unit * (q_is_k ? D / 8 : 16) + q_sub * ND * 4;
-  const uint32_t q_scale_off = D * 8 + (q_is_k ? (lane & 15) * NO + q_half * ND : 16 * ((q_unit >> 4) & 1));
-  const uint8_t* q_base = static_cast<const uint8_t*>(q_is_k ? a.k_pool : a.v_pool) + (int64_t)it.kv_head * q_bytes;
-  const int64_t q_stride = (int64_t)a.num_kv_heads * q_bytes;
-  // where the first dword's 8 values go in an image (the others: K 1 KB on, V
-  // by the dim blocks below)
-  const int q_v_blk = 4 * (q_unit / 32) + q_sub * ND;   // 16-dim block of the first dword
-  const uint32_t q_to = q_is_k ? (q_tile & 1) * (NK / 2) * 1024 + (4 * q_sub * ND + (lane >> 4)) * 256 + (lane & 15) * 16
-                               : (NK + (q_tile & 1) * NO) * 1024 + ((q_unit >> 4) & 1) * 512 + (q_unit & 15) * 16;
+  const int q_unit = lane % kUnits, q_sub = lane / kUnits + 64 / kUnits * q_half;
+  const uint32_t q_k_off = lane * (D / 8) + q_half * ND * 4, q_ks_off = D * 8 + (lane & 15) * NO + q_half * ND;
+  const uint32_t q_v_off = q_unit * 16 + q_sub * ND * 4, q_vs_off = D * 8 + 16 * ((q_unit >> 4) & 1);
+  const int64_t q_k_base = reinterpret_cast<int64_t>(a.k_pool) + (int64_t)it.kv_head * kvq_k_tile<D>();
+  const int64_t q_v_base = reinterpret_cast<int64_t>(a.v_pool) + (int64_t)it.kv_head * kvq_v_tile<D>();
+  // where the first dword's 8 values go in an image
+  const int q_v_blk = 4 * (q_unit / 32) + q_sub * ND;   // its 16-dim block
+  const uint32_t q_k_to = (q_page * (NK / 2) + q_half * ND) * 1024 + lane * 16;
+  const uint32_t q_v_to = (NK + q_page * NO + (q_v_blk >> 1)) * 1024 + ((q_unit >> 4) & 1) * 512 + (q_v_blk & 1) * 256 +
+                          (q_unit & 15) * 16;
   auto q_fetch = [&](const StepPos& p, Regs& r) {
-    const int64_t page = uniform64((int64_t)(uint32_t)(q_tile & 1 ? p.pid1 : p.pid0) * q_stride);
-    const int64_t base = uniform64(reinterpret_cast<int64_t>(q_base) + page);
-    if constexpr (ND == 4) {
-      const u32x4_t x = load_global<u32x4_t>(base + q_off);
-#pragma unroll
-      for (int k = 0; k < ND; ++k) r.w[k] = x[k];
-    } else if constexpr (ND == 2) {
-      const u32x2_t x = load_global<u32x2_t>(base + q_off);
-#pragma unroll
-      for (int k = 0; k < ND; ++k) r.w[k] = x[k];
+    const int64_t page = (int64_t)(uint32_t)(q_page ? p.pid1 : p.pid0) * a.num_kv_heads;
+    const int64_t kb = uniform64(q_k_base + page * kvq_k_tile<D>()), vb = uniform64(q_v_base + page * kvq_v_tile<D>());
+    if constexpr (ND == 2) {
+      const u32x2_t x = load_global<u32x2_t>(kb + q_k_off), y = load_global<u32x2_t>(vb + q_v_off);
+      r.k[0] = x[0];
+      r.k[1] = x[1];
+      r.v[0] = y[0];
+      r.v[1] = y[1];
+      r.k_scale = load_global<uint16_t>(kb + q_ks_off);
     } else {
-      r.w[0] = load_global<uint32_t>(base + q_off);
+      r.k[0] = load_global<uint32_t>(kb + q_k_off);
+      r.v[0] = load_global<uint32_t>(vb + q_v_off);
+      r.k_scale = load_global<uint8_t>(kb + q_ks_off);
     }
-    if (q_is_k) {
-      if constexpr (ND == 4) r.scale[0] = load_global<uint32_t>(base + q_scale_off);
-      else if constexpr (ND == 2) r.scale[0] = load_global<uint16_t>(base + q_scale_off);
-      else r.scale[0] = load_global<uint8_t>(base + q_scale_off);
-    } else {
-      r.scale = load_global<u32x4_t>(base + q_scale_off);
-    }
+    r.v_scale = load_global<u32x4_t>(vb + q_vs_off);
   };
-  auto q_store = [&](const StepPos& p, const Regs& r, uint8_t* img) {
-    if (q_is_k) {
+  // (full: of the step the registers hold)
+  auto q_convert = [&](bool full, const Regs& r, uint8_t* img) {
 #pragma unroll
-      for (int k = 0; k < ND; ++k)
-        *reinterpret_cast<bf16x8_t*>(img + q_to + k * 1024) =
-            kvq_decode_bf16(r.w[k], kvq_scale((r.scale[0] >> (8 * k)) & 0xff));
-    } else {
-      float scale[8];
+    for (int k = 0; k < ND; ++k)
+      *reinterpret_cast<bf16x8_t*>(img + q_k_to + k * 1024) = kvq_decode_bf16(r.k[k], kvq_scale_byte(r.k_scale, k));
+    float scale[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = full ? r.v_scale[i] : 0x3f803f80u;
+      scale[2 * i] = __uint_as_float(x << 16);
+      scale[2 * i + 1] = __uint_as_float(x & 0xffff0000u);
+    }
+    F f[2];
+    kvq_decode_keys(r.v[0], ND == 2 ? r.v[ND - 1] : 0u, scale, f[0], f[1]);
+    *reinterpret_cast<F*>(img + q_v_to) = f[0];
+    if constexpr (ND == 2) *reinterpret_cast<F*>(img + q_v_to + 256) = f[1];
+  };
+  // The V scales of a step with masked keys, in token order.
+  auto q_scales = [&](const Regs& r, uint8_t* img) {
+    if (q_sub == 0 && (q_unit & ~16) == 0) {
+      // slots 8 hh + j are keys 8 (j / 4) + 4 hh + j % 4 of the page
+      const int hh = q_unit >> 4;
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        scale[j] = __uint_as_float(j & 1 ? r.scale[j >> 1] & 0xffff0000u : r.scale[j >> 1] << 16);
-      if (!p.full) {
-        // slots 8 hh + j are keys 8 (j / 4) + 4 hh + j % 4 of the page
-        if (q_sub == 0 && (q_unit & ~16) == 0) {
-          const int hh = q_unit >> 4;
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            reinterpret_cast<float*>(img + kStepBytes)[16 * (q_tile & 1) + 8 * (j >> 2) + 4 * hh + (j & 3)] = scale[j];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) scale[j] = 1.f;
-      }
-#pragma unroll
-      for (int k = 0; k < ND; k += 2) {
-        F f[2];
-        kvq_decode_keys(r.w[k], k + 1 < ND ? r.w[k + 1 < ND ? k + 1 : k] : 0u, scale, f[0], f[1]);
-#pragma unroll
-        for (int i = 0; i < 2 && k + i < ND; ++i) {
-          const int b = q_v_blk + k + i;
-          *reinterpret_cast<F*>(img + q_to + (b >> 1) * 1024 + (b & 1) * 256) = f[i];
-        }
-      }
+        reinterpret_cast<uint32_t*>(img + kStepBytes)[16 * q_page + 8 * (j >> 2) + 4 * hh + (j & 3)] =
+            j & 1 ? r.v_scale[j >> 1] & 0xffff0000u : r.v_scale[j >> 1] << 16;
     }
   };
   // The V scales of this lane's 16 keys of a step that has masked ones.
@@ -716,8 +705,9 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   // for the next iteration, go out behind the Q K^T products. The
   // accumulator rescale, which must wait for the P V products, is returned
   // (alpha) and applied afterwards.
+  // KVQ: `convert` turns the registers' step into its image.
   auto fast_iter = [&](F (&vf)[2][NO], const uint8_t* img_qk, const uint8_t* img_v, const F (&pf_prev)[2],
-                       const f32x16_t& sacc_cur, f32x16_t& sacc_nxt, F (&pf_cur)[2], float& alpha) {
+                       const f32x16_t& sacc_cur, f32x16_t& sacc_nxt, F (&pf_cur)[2], float& alpha, auto convert) {
     F kf[NK];
 #pragma unroll
     for (int s = 0; s < NK; ++s) kf[s] = __builtin_bit_cast(F, *reinterpret_cast<const u32x4_t*>(k_at(img_qk, s)));
@@ -759,6 +749,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     for (int i = 0; i < 16; i += 4) ps += (pr[i] + pr[i + 1]) + (pr[i + 2] + pr[i + 3]);
     lsum = __builtin_fmaf(lsum, alpha, ps);
     sacc_nxt = sn;
+    convert();
     // keep the softmax results in this block (they are consumed only after
     // the next barrier, and would otherwise sink below the rescale branch)
 #pragma unroll
@@ -770,17 +761,21 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     // schedule: the K reads, the P V MFMAs, then the Q K^T MFMAs with the V
     // reads of step t after the first of them; each MFMA followed by VALU
     // work
-    __builtin_amdgcn_sched_group_barrier(0x100, NK, 0);
+    // (KVQ: half of the K reads after three of the P V products, which leaves
+    // registers for the conversion)
+    constexpr int kBetween = KVQ ? 4 : 5, kAhead = KVQ ? NK / 2 : NK;
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
     for (int k = 0; k < 2 * NO + 1; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, kBetween, 0);
+      if (KVQ && k >= 3 && k - 3 < (NK - kAhead) / 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x100, 2 * NO, 0);
 #pragma unroll
     for (int k = 0; k < NK - 1; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, kBetween, 0);
     }
   };
 
@@ -804,7 +799,10 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
       if (i > 0) ps[i] = advance();
       if constexpr (KVQ) {
         q_fetch(pick(ps[i].valid, ps[i], ps[0]), qr);
-        if (i < 2) q_store(ps[i], qr, lds[i]);
+        if (i < 2) {
+          q_convert(ps[i].full, qr, lds[i]);
+          if (!ps[i].full) q_scales(qr, lds[i]);
+        }
       } else {
         issue(pick(ps[i].valid, ps[i], ps[0]), lds[i]);
       }
@@ -834,34 +832,42 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
         asm volatile("" ::: "memory");
         const StepPos prev = ps[pv_st];   // step t-1, whose V is in vf
         ps[pv_st] = advance();
-        if constexpr (KVQ) {
-          // step t+2 into the image of step t-1; step t+S-1 into its registers
-          q_store(ps[(st + 2) % S], qr, lds[(st + 2) % S]);
-          q_fetch(pick(ps[pv_st].valid, ps[pv_st], ps[st]), qr);
-        } else {
-          issue(pick(ps[pv_st].valid, ps[pv_st], ps[st]), lds[pv_st]);
-        }
+        if constexpr (!KVQ) issue(pick(ps[pv_st].valid, ps[pv_st], ps[st]), lds[pv_st]);
         const bool more = ps[nx].valid;
         const bool fast = !first && more && ps[st].full && prev.full;
+        // KVQ: step t+2 into its image (that of step t-2), then step t+S-1 into
+        // the registers
+        const bool full2 = ps[(st + 2) % S].full;
+        auto convert = [&]() {
+          if constexpr (KVQ) q_convert(full2, qr, lds[(st + 2) % kImages]);
+        };
         if (computes && fast) {
           float alpha;
-          fast_iter(vf, lds[nx % kImages], lds[st % kImages], pf[nxt_p], sacc[cur_p], sacc[nxt_p], pf[cur_p], alpha);
+          fast_iter(vf, lds[nx % kImages], lds[st % kImages], pf[nxt_p], sacc[cur_p], sacc[nxt_p], pf[cur_p], alpha,
+                    convert);
           if (__any(alpha != 1.f)) {
 #pragma unroll
             for (int b = 0; b < NO; ++b) acc[b] *= alpha;
           }
-        } else if (computes) {
-          if (!first) {
-            if constexpr (!KVQ) mask_v(prev, vf);   // (4-bit codes are finite, and the weights 0)
-            pv(vf, pf[nxt_p]);
+        } else {
+          convert();
+          if (computes) {
+            if (!first) {
+              if constexpr (!KVQ) mask_v(prev, vf);   // (4-bit codes are finite, and the weights 0)
+              pv(vf, pf[nxt_p]);
+            }
+            if (more) qk(lds[nx % kImages], sacc[nxt_p]);
+            softmax(ps[st], sacc[cur_p], lds[st % kImages], pf[cur_p]);
+            read_v(lds[st % kImages], vf);
+            if (!more) {
+              if constexpr (!KVQ) mask_v(ps[st], vf);
+              pv(vf, pf[cur_p]);
+            }
           }
-          if (more) qk(lds[nx % kImages], sacc[nxt_p]);
-          softmax(ps[st], sacc[cur_p], lds[st % kImages], pf[cur_p]);
-          read_v(lds[st % kImages], vf);
-          if (!more) {
-            if constexpr (!KVQ) mask_v(ps[st], vf);
-            pv(vf, pf[cur_p]);
-          }
+        }
+        if constexpr (KVQ) {
+          if (!full2) q_scales(qr, lds[(st + 2) % kImages]);
+          q_fetch(pick(ps[pv_st].valid, ps[pv_st], ps[st]), qr);
         }
         first = false;
         if (!more) {
@@ -929,12 +935,12 @@ int lcm_int(int a, int b) {
 
 // The wide role's blocks: whole dispatch cycles of wide rounds, each a multiple
 // of wide_group rounds.
-void lay_out_rounds(AttnArgs& args, bool wide) {
+void lay_out_rounds(AttnArgs& args, bool wide, int narrow_pct = kWideSpanNarrowPct) {
   args.wide_blocks =
       (wide && args.n_wide > 0) ? pad_to(args.n_wide, 8 * lcm_int(args.wide_group, kSeCycle)) : 0;
   {
     const int ws = args.wide_blocks / (8 * kSeCycle), ns = args.narrow_blocks / (8 * kSeCycle);
-    args.wide_span = ws + (int)((int64_t)ns * kWideSpanNarrowPct / 100);
+    args.wide_span = ws + (int)((int64_t)ns * narrow_pct / 100);
   }
 }
 

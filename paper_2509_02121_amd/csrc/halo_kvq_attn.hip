@@ -271,29 +271,42 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
   finish_item<T, D, TO>(a, it, row, col, grp, acc, m, lsum);
 }
 
-constexpr int kKvqNarrowStages = 3;
+// (3 and 4 stages: 64 requests on 2048 keys 16.4 and 16.6 us, 2: 16.1; loads are
+// not what a step waits for)
+constexpr int kKvqNarrowStages = 2;
 
-// Workgroups of four waves for either role, of which a CU holds two: narrow slots
-// are taken in runs of four (two for a plan's bf16 workgroup of eight), wide items
-// in runs of 128 rows. Next to each other on a CU, a wide workgroup's products and
-// a narrow one's loads and conversions overlap.
+// Launches with wide items have workgroups of four waves for either role, of which
+// a CU holds two: narrow slots are taken in runs of four (two for a plan's bf16
+// workgroup of eight), wide items in runs of 128 rows. Next to each other on a CU, a
+// wide workgroup's products and a narrow one's loads and conversions overlap
+// (70B-shaped decode: 526 us, with workgroups of eight 545). Launches of narrow items
+// alone keep the plan's workgroups, one to a CU: with two half as large the
+// dispatcher fills some CUs twice and leaves others empty (64 requests on 2048
+// shared keys 16.4 us, with eight 12.8).
 constexpr int kKvqWaves = 4;
 constexpr int kKvqRows = kKvqWaves * 32;
 
-template <typename T, int D, typename TO>
+// Share (percent) of the narrow rounds dealt among the wide ones (see
+// kWideSpanNarrowPct): narrow items are a third as long as over bf16 pages, so the
+// wide ones, of which an unpaired rest would end the launch, start earlier. 70B-shaped
+// decode 526 us with 80, 495 with 40, 512 with 20; two-level tree (d 64) 60, 49, 49;
+// 500 requests of 32 query heads 199 with 40, 181 with 20.
+constexpr int kKvqNarrowPct = 40;
+
+template <typename T, int RB> constexpr int kvq_waves() { return RB > 0 ? kKvqWaves : block_waves<T>(); }
+
+template <typename T, int D, typename TO, int W>
 __device__ __forceinline__ void narrow_block_kvq(const AttnArgs& a, int block) {
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int lane = threadIdx.x & 63;
   // A plan's workgroup stays on its XCD (its index modulo 8), and its runs come
-  // one dispatch cycle after the other, so that they go to the same shader engine:
-  // one workgroup after the other would leave the engines of the second ones idle
-  // where these are empty.
-  constexpr int kRuns = block_waves<T>() / kKvqWaves;
+  // one dispatch cycle after the other.
+  constexpr int kRuns = block_waves<T>() / W;
   const int round = block >> 3, rounds = a.narrow_blocks / (8 * kRuns);
   const int cycle = round / (kRuns * kSeCycle), width = min(kSeCycle, rounds - cycle * kSeCycle);
   const int at = round - cycle * kRuns * kSeCycle;
-  const int of = (cycle * kSeCycle + at % width) * 8 + (block & 7);
-  const int64_t item_id = (int64_t)of * block_waves<T>() + at / width * kKvqWaves + wave;
+  const int of = kRuns == 1 ? block : (cycle * kSeCycle + at % width) * 8 + (block & 7);
+  const int64_t item_id = (int64_t)of * block_waves<T>() + (kRuns == 1 ? 0 : at / width * W) + wave;
   const Item it = a.items[item_id];
   const ItemRec* rec = a.item_recs + item_id;
   const int col = lane & 15;
@@ -305,8 +318,9 @@ __device__ __forceinline__ void narrow_block_kvq(const AttnArgs& a, int block) {
 // Both roles in one launch, dealt as in attn_kernel; wide unit u is run
 // u % runs of 128 rows of item u / runs.
 template <typename T, int D, typename TO, int RB>
-__global__ __launch_bounds__(64 * kKvqWaves) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__((64 * kvq_waves<T, RB>())) __attribute__((amdgpu_waves_per_eu(2)))
 void attn_kvq_kernel(AttnArgs a, int runs) {
+  constexpr int W = kvq_waves<T, RB>();
   constexpr int kSmem = RB > 0 ? kKvqStages * kvq_image_bytes<D>() : 16;
   __shared__ __attribute__((aligned(1024))) uint8_t smem[kSmem];
   const int b = blockIdx.x;
@@ -319,14 +333,13 @@ void attn_kvq_kernel(AttnArgs a, int runs) {
     const int w_upto = cyc < sp ? (int)((int64_t)(cyc + 1) * ws / sp) : ws;
     if (w_upto > w_before) {
       const int unit = xcd_remap((w_before * kSeCycle + q) * 8 + x, a.wide_group);
-      if (unit < a.n_wide)
-        wide_item<D, TO, kKvqWaves, kKvqStages, true>(a, unit / runs, smem, unit % runs * kKvqRows);
+      if (unit < a.n_wide) wide_item<D, TO, W, kKvqStages, true>(a, unit / runs, smem, unit % runs * kKvqRows);
       return;
     }
-    narrow_block_kvq<T, D, TO>(a, ((cyc - w_upto) * kSeCycle + q) * 8 + x);
+    narrow_block_kvq<T, D, TO, W>(a, ((cyc - w_upto) * kSeCycle + q) * 8 + x);
   } else {
     (void)smem;
-    narrow_block_kvq<T, D, TO>(a, b);
+    narrow_block_kvq<T, D, TO, W>(a, b);
   }
 }
 
@@ -348,8 +361,8 @@ void launch_items(AttnArgs args, const halo_plan& plan, hipStream_t stream) {
     args.n_wide *= runs;
     args.wide_group *= runs;
   }
-  args.narrow_blocks *= block_waves<T>() / kKvqWaves;
-  lay_out_rounds(args, wide);
+  args.narrow_blocks *= block_waves<T>() / (wide ? kKvqWaves : block_waves<T>());
+  lay_out_rounds(args, wide, kKvqNarrowPct);
   const int grid = args.wide_blocks + args.narrow_blocks;
   if (grid == 0) return;
   if constexpr (sizeof(T) == 2) {
@@ -363,7 +376,7 @@ void launch_items(AttnArgs args, const halo_plan& plan, hipStream_t stream) {
       return;
     }
   }
-  hipLaunchKernelGGL((attn_kvq_kernel<T, D, TO, 0>), dim3(grid), dim3(64 * kKvqWaves), 0, stream, args, runs);
+  hipLaunchKernelGGL((attn_kvq_kernel<T, D, TO, 0>), dim3(grid), dim3(64 * block_waves<T>()), 0, stream, args, runs);
 }
 
 }  // namespace
