@@ -395,13 +395,19 @@ halo_status_t halo_kvq_page_copy(void* pool, const halo_attn_params_t* params, h
                                  const int32_t* src_pages, const int32_t* dst_pages, int32_t num_pages,
                                  int32_t* error_flag, void* stream);
 
+/* The workspace (bytes) that a plan's calls over 4-bit pools need: the plan's
+ * workspace_bytes and, of a decode plan with a bf16 output, a scale for each partial
+ * row. 0 for NULL. */
+size_t halo_plan_kvq_workspace_bytes(const halo_plan_t* plan);
+
 /* halo_prefix_attn_decode and halo_prefix_attn_prefill over 4-bit pools, with the
- * same plans, metadata, workspaces and errors: k_pool and v_pool hold
+ * same plans, metadata and errors, and a workspace of halo_plan_kvq_workspace_bytes
+ * (prefill: as there, none runs the items uncut): k_pool and v_pool hold
  * halo_kvq_pool_bytes each, kv_dtype is the type of q. The result is that of
- * attention over the values the pools stand for: for bf16 queries as exact as
- * over bf16 pools, for fp32 queries as over fp32 pools (4-bit values are exact in
- * bf16, so fp32 queries and softmax weights are multiplied in three bf16 parts).
- * Slots past a segment's length may hold any bytes. */
+ * attention over the values the pools stand for, in fp32 for an fp32 output (4-bit
+ * values are exact in bf16, so fp32 queries, and softmax weights for an fp32
+ * output, are multiplied in three bf16 parts); for a bf16 output the weights are
+ * rounded to bf16. Slots past a segment's length may hold any bytes. */
 halo_status_t halo_prefix_attn_decode_kvq(const halo_plan_t* plan, const void* device_meta,
                                           const void* q, const void* k_pool, const void* v_pool,
                                           void* o, float* lse,

@@ -38,6 +38,7 @@ struct AttnArgs {
   int32_t wide_span;       // launch rounds (of 8 blocks) the wide rounds are spread over
   int32_t num_kv_heads;
   float scale_log2;   // sm_scale * log2(e)
+  float* part_scale;  // 4-bit pools, bf16 output: of each partial row (see store_half)
 };
 
 // The items of a plan over 4-bit pools (halo_kvq_attn.hip).
@@ -152,6 +153,21 @@ __device__ __forceinline__ f32x8_t to_frag(const float (&p)[8], f32x8_t*) {
   return r;
 }
 
+// x as a sum of N bf16 fragments, the largest first.
+template <int N>
+__device__ __forceinline__ void split(const float (&x)[8], bf16x8_t (&f)[N]) {
+  float r[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = x[j];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      f[n][j] = (__bf16)r[j];
+      if (n + 1 < N) r[j] -= (float)f[n][j];
+    }
+}
+
 __device__ __forceinline__ void store4(float* dst, f32x4_t v) {
   *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
 }
@@ -175,6 +191,27 @@ __device__ __forceinline__ void store4(__bf16* dst, f32x4_t v) {
   *reinterpret_cast<uint2*>(dst) = __builtin_bit_cast(uint2, r);
 }
 __device__ __forceinline__ void store4_part(__bf16* dst, f32x4_t v) { store4(dst, v); }
+
+// Partial results over 4-bit pools with a bf16 output: as long as bf16 ones, but in
+// fp16 with a power of two for each row, the largest element's, so that each is off
+// by at most 2^-11 of itself (or 2^-25 of the row's largest) where bf16 is by 2^-8:
+// rows of three or more partials were otherwise further off than the output's
+// rounding (70B-shaped decode: 0.0027 of the row, 0.0022 so; 64 requests on 2048 keys
+// 0.0024 and 0.0018).
+__device__ __forceinline__ float row_scale(float top) {
+  const uint32_t e = min(__float_as_uint(top) & 0x7f800000u, 0x7e800000u);
+  return __uint_as_float(e ? e : 0x3f800000u);
+}
+__device__ __forceinline__ float reciprocal_of_scale(float scale) {   // of a power of two in [2^-126, 2^126]
+  return __uint_as_float(0x7f000000u - __float_as_uint(scale));
+}
+__device__ __forceinline__ void store_half(void* dst, f32x4_t v) {
+  typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+  f16x4_t r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = (_Float16)v[j];
+  *reinterpret_cast<uint2*>(dst) = __builtin_bit_cast(uint2, r);
+}
 
 // Reductions over the four 16-lane rows of a wave (lanes l, l^16, l^32,
 // l^48) with the gfx950 row-swap instructions, which stay on the VALU
@@ -298,7 +335,8 @@ struct RecLane {
 
 // The end of a narrow item: lane (col, grp) holds dims 16b + 4grp .. + 3 of row
 // col in acc[b], and its share of the row's sum.
-template <typename T, int D, typename TO>
+// HALF: partial results by store_half.
+template <typename T, int D, typename TO, bool HALF = false>
 __device__ __forceinline__ void finish_item(const AttnArgs& a, const Item& it, const Row& row, int col, int grp,
                                             f32x4_t (&acc)[D / 16], float m, float lsum) {
   constexpr int NB = D / 16;
@@ -313,6 +351,23 @@ __device__ __forceinline__ void finish_item(const AttnArgs& a, const Item& it, c
 #pragma unroll
       for (int b = 0; b < NB; ++b) store4(dst + 16 * b, acc[b] * inv);
       if (grp == 0) reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
+    } else if constexpr (HALF) {
+      float top = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(acc[b][j]));
+      const float scale = row_scale(rows_max(top) * inv), x = inv * reciprocal_of_scale(scale);
+      if (has_row) {
+        const int64_t prow = row.slot;
+        uint16_t* dst = static_cast<uint16_t*>(a.part_o) + prow * D + 4 * grp;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) store_half(dst + 16 * b, acc[b] * x);
+        if (grp == 0) {
+          reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
+          a.part_scale[prow] = scale;
+        }
+      }
     } else if (has_row) {
       const int64_t prow = row.slot;
       TO* dst = static_cast<TO*>(a.part_o) + prow * D + 4 * grp;
@@ -395,6 +450,18 @@ template <int ND> struct KvqRegs {
   uint32_t k[ND], v[ND];
   uint32_t k_scale;
   u32x4_t v_scale;
+};
+
+// A step's softmax weights between their softmax and their product with V: the
+// bf16 operands, one per page. Or, where the output is fp32 and every other
+// operand of P V exact in bf16 (4-bit V), the weights in fp32, which are split into
+// three bf16 parts at the product: the output then has fp32's accuracy, not that of
+// bf16 weights (2^-9 each).
+template <bool EXACT> struct Weights {
+  bf16x8_t f[2];
+};
+template <> struct Weights<true> {
+  float p[16];
 };
 
 // A workgroup of W waves and an S-stage ring, for the item's rows from row0 on.
@@ -639,16 +706,45 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
         }
     }
   };
-  auto pv = [&](const F (&vf)[2][NO], const F (&pf)[2]) {
+  constexpr bool kExact = KVQ && sizeof(TO) == 4;
+  using P = Weights<kExact>;
+  auto pv = [&](const F (&vf)[2][NO], const P& w) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < 2; ++g) {
+      if constexpr (kExact) {
+        float half[8];
+        F part[3];
 #pragma unroll
-      for (int b = 0; b < NO; ++b) acc[b] = mma32(vf[g][b], pf[g], acc[b]);
+        for (int j = 0; j < 8; ++j) half[j] = w.p[8 * g + j];
+        split(half, part);
+#pragma unroll
+        for (int n = 2; n >= 0; --n)
+#pragma unroll
+          for (int b = 0; b < NO; ++b) acc[b] = mma32(vf[g][b], part[n], acc[b]);
+      } else {
+#pragma unroll
+        for (int b = 0; b < NO; ++b) acc[b] = mma32(vf[g][b], w.f[g], acc[b]);
+      }
+    }
+  };
+  auto put_weights = [&](const float (&pr)[16], P& w) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      if constexpr (kExact) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w.p[8 * g + j] = pr[8 * g + j];
+      } else {
+        float half[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) half[j] = pr[8 * g + j];
+        w.f[g] = to_frag(half, (F*)nullptr);
+      }
+    }
   };
 
   // Online softmax of one step's scores into P (bf16, RNE), one operand per
   // page of the step (registers 0-7: page 0, 8-15: page 1).
-  auto softmax = [&](const StepPos& p, const f32x16_t& sacc, const uint8_t* img, F (&pf)[2]) {
+  auto softmax = [&](const StepPos& p, const f32x16_t& sacc, const uint8_t* img, P& pf) {
     // raw scores (masked ones -inf); the scale is applied inside the exponent
     // with one FMA (scale > 0, so it commutes with the max)
     float sv[16];
@@ -687,13 +783,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
       for (int i = 0; i < 16; ++i) pr[i] = skey(i) < lim ? pr[i] * sc[i] : 0.f;
     }
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      float half[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) half[j] = pr[8 * g + j];
-      pf[g] = to_frag(half, (F*)nullptr);
-    }
+    put_weights(pr, pf);
   };
 
   // One iteration on full, unmasked steps as a single basic block: the 16
@@ -706,15 +796,12 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   // accumulator rescale, which must wait for the P V products, is returned
   // (alpha) and applied afterwards.
   // KVQ: `convert` turns the registers' step into its image.
-  auto fast_iter = [&](F (&vf)[2][NO], const uint8_t* img_qk, const uint8_t* img_v, const F (&pf_prev)[2],
-                       const f32x16_t& sacc_cur, f32x16_t& sacc_nxt, F (&pf_cur)[2], float& alpha, auto convert) {
+  auto fast_iter = [&](F (&vf)[2][NO], const uint8_t* img_qk, const uint8_t* img_v, const P& pf_prev,
+                       const f32x16_t& sacc_cur, f32x16_t& sacc_nxt, P& pf_cur, float& alpha, auto convert) {
     F kf[NK];
 #pragma unroll
     for (int s = 0; s < NK; ++s) kf[s] = __builtin_bit_cast(F, *reinterpret_cast<const u32x4_t*>(k_at(img_qk, s)));
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int b = 0; b < NO; ++b) acc[b] = mma32(vf[g][b], pf_prev[g], acc[b]);
+    pv(vf, pf_prev);
     f32x16_t sn = f32x16_t{};
 #pragma unroll
     for (int s = 0; s < NK; ++s) sn = mma32(kf[s], qf[s], sn);
@@ -737,13 +824,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     float pr[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) pr[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc_cur[i], a.scale_log2, -m_use));
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      float half[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) half[j] = pr[8 * g + j];
-      pf_cur[g] = to_frag(half, (F*)nullptr);
-    }
+    put_weights(pr, pf_cur);
     float ps = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; i += 4) ps += (pr[i] + pr[i + 1]) + (pr[i + 2] + pr[i + 3]);
@@ -752,10 +833,15 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     convert();
     // keep the softmax results in this block (they are consumed only after
     // the next barrier, and would otherwise sink below the rescale branch)
+    if constexpr (kExact) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const u32x4_t w = __builtin_bit_cast(u32x4_t, pf_cur[g]);
-      asm volatile("" ::"v"(w[0]), "v"(w[1]), "v"(w[2]), "v"(w[3]));
+      for (int i = 0; i < 16; ++i) asm volatile("" ::"v"(pf_cur.p[i]));
+    } else {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const u32x4_t w = __builtin_bit_cast(u32x4_t, pf_cur.f[g]);
+        asm volatile("" ::"v"(w[0]), "v"(w[1]), "v"(w[2]), "v"(w[3]));
+      }
     }
     asm volatile("" ::"v"(lsum));
     // schedule: the K reads, the P V MFMAs, then the Q K^T MFMAs with the V
@@ -808,7 +894,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
       }
     }
     f32x16_t sacc[2];
-    F pf[2][2];
+    P pf[2];
     F vf[2][NO];
     if constexpr (KVQ) {
       asm volatile("" ::: "memory");
@@ -882,6 +968,15 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 
   // ---- epilogue: lane (c, h) holds dims 32b + 8(i/4) + 4h + i%4 of row c
   const float l = halves_sum(lsum);
+  constexpr bool kHalf = KVQ && sizeof(TO) == 2;   // partial results by store_half
+  float top = 0.f;
+  if constexpr (kHalf) {
+#pragma unroll
+    for (int b = 0; b < NO; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(acc[b][i]));
+    top = halves_max(top);
+  }
   if (computes && r < it.n_rows) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const float lse2 = l > 0.f ? m + __log2f(l) : kNegInf;
@@ -894,6 +989,19 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
         for (int q = 0; q < 4; ++q)
           store4(dst + 32 * b + 8 * q, f32x4_t{acc[b][4 * q], acc[b][4 * q + 1], acc[b][4 * q + 2], acc[b][4 * q + 3]} * inv);
       if (h == 0) reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, l);
+    } else if (kHalf && it.part_base >= 0) {
+      const int64_t prow = row.slot;
+      const float scale = row_scale(top * inv), x = inv * reciprocal_of_scale(scale);
+      uint16_t* dst = static_cast<uint16_t*>(a.part_o) + prow * D + 4 * h;
+#pragma unroll
+      for (int b = 0; b < NO; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          store_half(dst + 32 * b + 8 * q, f32x4_t{acc[b][4 * q], acc[b][4 * q + 1], acc[b][4 * q + 2], acc[b][4 * q + 3]} * x);
+      if (h == 0) {
+        reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, l);
+        a.part_scale[prow] = scale;
+      }
     } else if (it.part_base >= 0) {
       const int64_t prow = row.slot;
       TO* dst = static_cast<TO*>(a.part_o) + prow * D + 4 * h;

@@ -32,6 +32,7 @@
 #include <cstring>
 #include <mutex>
 #include <string>
+#include <type_traits>
 #include <vector>
 
 #include "halo_device.h"
@@ -388,7 +389,12 @@ void wide_kernel(AttnArgs a) {
 // element 0 whatever the index.
 template <typename TO, int E>
 __device__ __forceinline__ void unpack16(u32x4_t x, float (&v)[E]) {
-  if constexpr (sizeof(TO) == 4) {
+  if constexpr (std::is_same<TO, _Float16>::value) {
+    typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+    const f16x8_t h = __builtin_bit_cast(f16x8_t, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)h[j];
+  } else if constexpr (sizeof(TO) == 4) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(x[j]);
   } else {
@@ -413,7 +419,7 @@ __device__ __forceinline__ void store16(TO* dst, const float (&v)[E]) {
 }
 
 struct MergeArgs {
-  const void* part_o;     // in the output element type
+  const void* part_o;     // in the output element type, or in fp16 with a scale per row
   const float* part_lse;
   const int32_t* merge_rows;
   const int32_t* merge_indptr;
@@ -423,6 +429,7 @@ struct MergeArgs {
   int32_t n_merge;
   int32_t k0;   // partials of entry r at slots k * n_merge + r for k < k0
   int32_t n_parts;
+  const float* part_scale;   // of partials in fp16 (see store_half)
 };
 
 // Rows per merge workgroup (256 threads, 16 bytes of a row per thread).
@@ -440,9 +447,11 @@ template <int D, typename TO> constexpr int merge_rows_per_block() { return 256 
 // by integer selects, which fast math cannot fold away whatever bits they
 // hold. Further partials (entries with more than k0) come from the slot
 // list merge_parts. One group of threads per row, 16 bytes of each partial
-// (8 bf16 or 4 fp32 dims) per thread.
-template <int D, typename TO>
+// (8 bf16 or 4 fp32 dims) per thread. TP: the partials' element type; a partial in
+// fp16 has a scale, which goes into its weight.
+template <int D, typename TO, typename TP = TO>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void merge_kernel(MergeArgs a) {
+  constexpr bool kScaled = std::is_same<TP, _Float16>::value;
   constexpr int E = 16 / (int)sizeof(TO);
   constexpr int TPR = D / E;
   constexpr int RPB = 256 / TPR;
@@ -451,19 +460,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
   const int r = blockIdx.x * RPB + threadIdx.x / TPR;
   const int t = threadIdx.x % TPR;
   if (r >= a.n_merge) return;
-  const TO* part_o = static_cast<const TO*>(a.part_o);
+  const TP* part_o = static_cast<const TP*>(a.part_o);
   const int q_row = a.merge_rows[r];
   const int p0 = a.merge_indptr[r], p1 = a.merge_indptr[r + 1];
-  uint32_t lb[kBatch];
+  uint32_t lb[kBatch], sb[kBatch];
   u32x4_t vb[kBatch];
 #pragma unroll
   for (int k = 0; k < kBatch; ++k) {
     if (k < a.k0) {
       const int64_t slot = (int64_t)k * a.n_merge + r;
       lb[k] = __builtin_bit_cast(uint32_t, a.part_lse[slot]);
+      sb[k] = kScaled ? __builtin_bit_cast(uint32_t, a.part_scale[slot]) : 0;
       vb[k] = *reinterpret_cast<const u32x4_t*>(part_o + slot * D + E * t);
     } else {
-      lb[k] = 0;
+      lb[k] = sb[k] = 0;
       vb[k] = u32x4_t{0u, 0u, 0u, 0u};
     }
   }
@@ -473,7 +483,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   float wsum = 0.f;
   // online over batches of parts: rescale when the running max moves
-  auto fold = [&](const float (&l)[kBatch], const u32x4_t (&raw)[kBatch]) {
+  auto fold = [&](const float (&l)[kBatch], const float (&sc)[kBatch], const u32x4_t (&raw)[kBatch]) {
     float bm = kNegInf;
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) bm = fmaxf(bm, l[k]);
@@ -487,17 +497,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
     for (int k = 0; k < kBatch; ++k) {
       const float w = __builtin_amdgcn_exp2f(l[k] - m_new);   // 0 for absent parts
       float v[E];
-      unpack16<TO, E>(raw[k], v);
+      unpack16<TP, E>(raw[k], v);
       wsum += w;
+      const float x = kScaled ? w * sc[k] : w;
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(w, v[e], acc[e]);
+      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(x, v[e], acc[e]);
     }
     mx = m_new;
   };
   {
     const int n = p1 - p0;
     const uint32_t neg_inf_bits = 0xff800000u;
-    float l[kBatch];
+    float l[kBatch], sc[kBatch];
     u32x4_t raw[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
@@ -505,22 +516,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
       l[k] = __builtin_bit_cast(float, keep ? lb[k] : neg_inf_bits);
       const uint32_t m = keep ? 0xffffffffu : 0u;
       raw[k] = vb[k] & u32x4_t{m, m, m, m};
+      sc[k] = __builtin_bit_cast(float, sb[k] & m);
     }
-    fold(l, raw);
+    fold(l, sc, raw);
   }
   for (int pb = p0 + a.k0; pb < p1; pb += kBatch) {
     int pid[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) pid[k] = pb + k < p1 ? a.merge_parts[pb + k] : -1;
-    float l[kBatch];
+    float l[kBatch], sc[kBatch];
     u32x4_t raw[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) l[k] = pid[k] >= 0 ? a.part_lse[pid[k]] : kNegInf;
+    for (int k = 0; k < kBatch; ++k) {
+      l[k] = pid[k] >= 0 ? a.part_lse[pid[k]] : kNegInf;
+      sc[k] = kScaled && pid[k] >= 0 ? a.part_scale[pid[k]] : 0.f;
+    }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k)
       raw[k] = pid[k] >= 0 ? *reinterpret_cast<const u32x4_t*>(part_o + (int64_t)pid[k] * D + E * t)
                            : u32x4_t{0u, 0u, 0u, 0u};
-    fold(l, raw);
+    fold(l, sc, raw);
   }
   const float inv = wsum > 0.f ? 1.f / wsum : 0.f;
 #pragma unroll
@@ -535,10 +550,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
 // merge kernels walk a row's partials in rounds of 8 of two dependent loads
 // each: 4 requests of 12000-24000 private keys (128 rows of 24-47 partials)
 // 58.3 -> 53.3 us, one of 24000 33 -> 20 us (whole calls, 32/8 heads, d 128).
-// TP: the partials' element type; slot_of(k): the slot of partial k < n.
+// TP: the partials' element type (fp16: with the scales part_scale); slot_of(k): the
+// slot of partial k < n.
 template <int D, typename TP, typename TO, typename SlotOf>
-__device__ __forceinline__ void merge_row(const void* part_o, const float* part_lse, int n, SlotOf slot_of, TO* o,
-                                          float* lse, int64_t q_row) {
+__device__ __forceinline__ void merge_row(const void* part_o, const float* part_lse, const float* part_scale, int n,
+                                          SlotOf slot_of, TO* o, float* lse, int64_t q_row) {
+  constexpr bool kScaled = std::is_same<TP, _Float16>::value;
   constexpr int E = 16 / (int)sizeof(TP);
   constexpr int TPR = D / E;
   constexpr int kGroups = 256 / TPR;
@@ -560,16 +577,18 @@ __device__ __forceinline__ void merge_row(const void* part_o, const float* part_
     m = m_new;
   };
   for (int k0 = g; k0 < n; k0 += kBatch * kGroups) {
-    float l[kBatch];
+    float l[kBatch], sc[kBatch];
     u32x4_t raw[kBatch];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
       const int k = k0 + j * kGroups;
       l[j] = kNegInf;
+      sc[j] = 0.f;
       raw[j] = u32x4_t{0u, 0u, 0u, 0u};
       if (k < n) {
         const int64_t slot = slot_of(k);
         l[j] = part_lse[slot];
+        if constexpr (kScaled) sc[j] = part_scale[slot];
         raw[j] = *reinterpret_cast<const u32x4_t*>(static_cast<const TP*>(part_o) + slot * D + E * t);
       }
     }
@@ -584,8 +603,9 @@ __device__ __forceinline__ void merge_row(const void* part_o, const float* part_
       float v[E];
       unpack16<TP, E>(raw[j], v);
       wsum += w;
+      const float x = kScaled ? w * sc[j] : w;
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(w, v[e], acc[e]);
+      for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(x, v[e], acc[e]);
     }
   }
   // over the groups of the wave
@@ -628,12 +648,12 @@ __device__ __forceinline__ void merge_row(const void* part_o, const float* part_
 }
 
 // Merge entry blockIdx.x (see merge_kernel for the slots).
-template <int D, typename TO>
+template <int D, typename TO, typename TP = TO>
 __global__ __launch_bounds__(256) void merge_row_kernel(MergeArgs a) {
   const int r = blockIdx.x;
   const int p0 = a.merge_indptr[r], n = a.merge_indptr[r + 1] - p0;
-  merge_row<D, TO, TO>(
-      a.part_o, a.part_lse, n,
+  merge_row<D, TP, TO>(
+      a.part_o, a.part_lse, a.part_scale, n,
       [&](int k) { return k < a.k0 ? (int64_t)k * a.n_merge + r : (int64_t)a.merge_parts[p0 + k]; },
       static_cast<TO*>(a.o), a.lse, a.merge_rows[r]);
 }
@@ -707,7 +727,7 @@ __global__ __launch_bounds__(256) void merge_item_row_kernel(MergeItemArgs a) {
   const int r = blockIdx.x % a.blocks_per_item;
   if (r >= mi.n_rows) return;
   merge_row<D, float, TO>(
-      a.part_o, a.part_lse, mi.n_parts, [&](int k) { return (int64_t)a.bases[mi.part_begin + k] + r; },
+      a.part_o, a.part_lse, nullptr, mi.n_parts, [&](int k) { return (int64_t)a.bases[mi.part_begin + k] + r; },
       static_cast<TO*>(a.o), a.lse, a.rows[mi.row_begin + r].q_row);
 }
 
@@ -750,14 +770,14 @@ void launch_attention(AttnArgs args, int wide_rb, bool small_wide, hipStream_t s
   }
 }
 
-template <int D, typename TO>
+template <int D, typename TO, typename TP = TO>
 void launch_merge(const MergeArgs& margs, hipStream_t stream) {
   if (margs.n_merge > 0 && margs.n_merge <= kMergeRowMax && margs.n_parts > kMergeK0 * (int64_t)margs.n_merge) {
-    hipLaunchKernelGGL((merge_row_kernel<D, TO>), dim3(margs.n_merge), dim3(256), 0, stream, margs);
+    hipLaunchKernelGGL((merge_row_kernel<D, TO, TP>), dim3(margs.n_merge), dim3(256), 0, stream, margs);
   } else if (margs.n_merge > 0) {
     constexpr int rpb = merge_rows_per_block<D, TO>();
     const int blocks = (margs.n_merge + rpb - 1) / rpb;
-    hipLaunchKernelGGL((merge_kernel<D, TO>), dim3(blocks), dim3(256), 0, stream, margs);
+    hipLaunchKernelGGL((merge_kernel<D, TO, TP>), dim3(blocks), dim3(256), 0, stream, margs);
   }
 }
 
@@ -772,6 +792,13 @@ void launch_merge_items(MergeItemArgs args, int n_items, int most_rows, int64_t 
   constexpr int rpb = 256 / (D / 4);
   args.blocks_per_item = (most_rows + rpb - 1) / rpb;
   hipLaunchKernelGGL((merge_items_kernel<D, TO>), dim3(n_items * args.blocks_per_item), dim3(256), 0, stream, args);
+}
+
+// The workspace of a plan's calls over 4-bit pools: partials in fp16 have a scale
+// each.
+size_t kvq_workspace_bytes(const halo_plan_t& plan) {
+  const bool half = !plan.prefill && plan.params.out_dtype == HALO_BF16 && plan.n_part_slots > 0;
+  return plan.workspace_bytes + (half ? align256((size_t)plan.n_part_slots * sizeof(float)) : 0);
 }
 
 // kvq: k_pool and v_pool are 4-bit ones.
@@ -792,9 +819,10 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq
   const bool whole = plan->prefill && plan->n_merge_items > 0 &&
                      (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 ||
                       workspace_bytes < plan->workspace_bytes);
-  if (!plan->prefill && workspace_bytes < plan->workspace_bytes)
-    return fail(HALO_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(plan->workspace_bytes) +
-                                                  " bytes, got " + std::to_string(workspace_bytes));
+  const size_t needs = kvq ? kvq_workspace_bytes(*plan) : plan->workspace_bytes;
+  if (!plan->prefill && workspace_bytes < needs)
+    return fail(HALO_ERR_WORKSPACE_TOO_SMALL, "workspace needs " + std::to_string(needs) + " bytes, got " +
+                                                  std::to_string(workspace_bytes));
   if (!plan->prefill && plan->workspace_bytes > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0))
     return fail(HALO_ERR_INVALID_ARGUMENT, "workspace must be a 256-byte aligned device pointer");
 
@@ -809,6 +837,10 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq
                         ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
                                                    align256((size_t)plan->n_part_slots * D * part_elem))
                         : nullptr;
+  // (4-bit pools, decode with a bf16 output: the partials' scales last)
+  float* part_scale = kvq && needs > plan->workspace_bytes
+                          ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan->workspace_bytes)
+                          : nullptr;
   AttnArgs args{q, k_pool, v_pool, o, lse, part_o, part_lse,
                 reinterpret_cast<const int32_t*>(m + L.seg_page_off),
                 reinterpret_cast<const int32_t*>(m + L.seg_len),
@@ -821,12 +853,12 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq
                 plan->n_items, whole ? plan->n_whole_wide : plan->n_wide, 0,
                 whole ? plan->n_whole_blocks : plan->n_narrow_blocks, plan->narrow_slots,
                 plan->wide_group, 0,
-                p.num_kv_heads, p.sm_scale * kLog2e};
+                p.num_kv_heads, p.sm_scale * kLog2e, part_scale};
   MergeArgs margs{part_o, part_lse,
                   reinterpret_cast<const int32_t*>(m + L.merge_rows),
                   reinterpret_cast<const int32_t*>(m + L.merge_indptr),
                   reinterpret_cast<const int32_t*>(m + L.merge_parts),
-                  o, lse, plan->n_merge, plan->merge_k0, plan->n_merge_parts};
+                  o, lse, plan->n_merge, plan->merge_k0, plan->n_merge_parts, part_scale};
   if (plan->n_narrow_blocks > 0 &&
       plan->narrow_slots != (p.kv_dtype == HALO_BF16 ? block_waves<__bf16>() : block_waves<float>()))
     return fail(HALO_ERR_INVALID_ARGUMENT, "internal: narrow slots per workgroup differ from its waves");
@@ -849,9 +881,11 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq
   }
   if (D == 128) {
     if (out_f32) launch_merge<128, float>(margs, st);
+    else if (kvq) launch_merge<128, __bf16, _Float16>(margs, st);
     else launch_merge<128, __bf16>(margs, st);
   } else {
     if (out_f32) launch_merge<64, float>(margs, st);
+    else if (kvq) launch_merge<64, __bf16, _Float16>(margs, st);
     else launch_merge<64, __bf16>(margs, st);
   }
   if (plan->n_merge_items > 0 && !whole) {
@@ -1008,6 +1042,10 @@ extern "C" halo_status_t halo_prefix_attn_prefill(const halo_plan_t* plan, const
                                                   size_t workspace_bytes, void* stream) {
   return run_attention(plan, true, false, device_meta, q, k_pool, v_pool, o, lse, workspace, workspace_bytes,
                        stream);
+}
+
+extern "C" size_t halo_plan_kvq_workspace_bytes(const halo_plan_t* plan) {
+  return plan ? kvq_workspace_bytes(*plan) : 0;
 }
 
 extern "C" halo_status_t halo_prefix_attn_decode_kvq(const halo_plan_t* plan, const void* device_meta,

@@ -16,9 +16,10 @@
 // 64 conversions (about 5 cycles each, measured) and 40 instructions for the scales
 // to the softmax and the 16 MFMAs.
 //
-// fp32 queries: K and V are exact in bf16, so a product with fp32 accuracy needs
-// only q and P split into three bf16 parts each (8 + 8 + 8 bits): three MFMAs of
-// 16x16x32 in place of eight 16x16x4 fp32 ones.
+// fp32 queries and outputs: K and V are exact in bf16, so products with fp32
+// accuracy need only q (fp32 queries) and P (fp32 outputs) split into three bf16
+// parts each (8 + 8 + 8 bits): three MFMAs of 16x16x32 in place of eight 16x16x4
+// fp32 ones.
 
 #include <hip/hip_runtime.h>
 
@@ -32,23 +33,9 @@ using namespace halo;
 
 namespace {
 
-// bf16 parts of an operand: 1 for bf16 (rounded, as over bf16 pools), 3 for fp32.
+// bf16 parts of an operand whose products go to type T: 1 for bf16 (rounded, as
+// over bf16 pools), 3 for fp32.
 template <typename T> constexpr int parts() { return sizeof(T) == 2 ? 1 : 3; }
-
-// x as a sum of N bf16 fragments, the largest first.
-template <int N>
-__device__ __forceinline__ void split(const float (&x)[8], bf16x8_t (&f)[N]) {
-  float r[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) r[j] = x[j];
-#pragma unroll
-  for (int n = 0; n < N; ++n)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      f[n][j] = (__bf16)r[j];
-      if (n + 1 < N) r[j] -= (float)f[n][j];
-    }
-}
 
 // One step's codes and scales of a lane: K dwords of 8 dims for the two 16-key
 // tiles, their scale bytes, V dwords of 8 keys, and those keys' scales in bf16.
@@ -69,6 +56,7 @@ template <typename T, int D, typename TO, bool NT, int P>
 __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, const RecLane& rl, int lane) {
   using F = bf16x8_t;
   constexpr int NS = D / 32, NB = D / 16, NP = parts<T>();
+  constexpr int NW = parts<TO>();   // of the softmax's weights
   constexpr int kTile = kvq_k_tile<D>(), vTile = kvq_v_tile<D>();
   using Regs = KvqStep<D>;
   const int col = lane & 15;
@@ -231,13 +219,13 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
 #pragma unroll
     for (int j = 0; j < 8; ++j) pr[j] *= vs[j];
     lsum += psum;
-    F pf[NP];
+    F pf[NW];
     split(pr, pf);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const F vf = kvq_decode_bf16(r.v[b], 1.f);
 #pragma unroll
-      for (int n = NP - 1; n >= 0; --n) acc[b] = mma(vf, pf[n], acc[b]);
+      for (int n = NW - 1; n >= 0; --n) acc[b] = mma(vf, pf[n], acc[b]);
     }
   };
 
@@ -268,7 +256,7 @@ __device__ __forceinline__ void run_item_kvq(const AttnArgs& a, const Item& it, 
       }
     }
   }
-  finish_item<T, D, TO>(a, it, row, col, grp, acc, m, lsum);
+  finish_item<T, D, TO, sizeof(TO) == 2>(a, it, row, col, grp, acc, m, lsum);
 }
 
 // (3 and 4 stages: 64 requests on 2048 keys 16.4 and 16.6 us, 2: 16.1; loads are

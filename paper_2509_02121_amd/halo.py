@@ -87,7 +87,7 @@ EXPORTED_SYMBOLS = (
     "halo_prefix_attn_decode", "halo_prefix_attn_prefill", "halo_prefix_attn_decode_noalloc",
     "halo_kv_page_gather",
     "halo_kv_page_scatter", "halo_kv_page_scatter_kv", "halo_kv_page_copy",
-    "halo_prefix_attn_decode_kvq", "halo_prefix_attn_prefill_kvq",
+    "halo_plan_kvq_workspace_bytes", "halo_prefix_attn_decode_kvq", "halo_prefix_attn_prefill_kvq",
     "halo_kvq_pool_bytes", "halo_kvq_page_scatter_kv", "halo_kvq_page_gather_kv", "halo_kvq_page_copy",
     "halo_kv_step_tables", "halo_rope_params_default", "halo_rope_turns", "halo_rope_qk",
     "halo_prefix_tree_build", "halo_prefix_tree_get", "halo_prefix_tree_destroy",
@@ -197,6 +197,8 @@ def load_library(require_gpu=False):
     lib.halo_kv_page_scatter_kv.restype = ctypes.c_int
     lib.halo_kv_page_copy.argtypes = [vp, ctypes.POINTER(AttnParams), vp, vp, ctypes.c_int32, vp, vp]
     lib.halo_kv_page_copy.restype = ctypes.c_int
+    lib.halo_plan_kvq_workspace_bytes.argtypes = [vp]
+    lib.halo_plan_kvq_workspace_bytes.restype = sz
     lib.halo_kvq_pool_bytes.argtypes = [ctypes.POINTER(AttnParams), ctypes.c_int]
     lib.halo_kvq_pool_bytes.restype = ctypes.c_int64
     lib.halo_kvq_page_scatter_kv.argtypes = [vp, vp, ctypes.POINTER(AttnParams), vp, vp, vp, vp, vp, ctypes.c_int32,
@@ -330,6 +332,7 @@ class Plan:
         self._keep = keep
         self.device_meta_bytes = meta.value
         self.workspace_bytes = ws.value
+        self.kvq_workspace_bytes = lib.halo_plan_kvq_workspace_bytes(handle)   # of calls over 4-bit pools
         self.is_prefill = q_len is not None
         st = self.stats()
         self.num_query_rows = int(st["num_query_rows"])
@@ -516,8 +519,9 @@ def _check_run(plan, device_meta, q, k_pool, v_pool, o, lse, workspace, library_
         if have < n:
             raise ValueError(f"{name} has {have} {unit}, the plan needs at least {n}")
     ws = _nbytes(workspace) if workspace is not None else 0
-    if not library_workspace and not plan.is_prefill and ws < plan.workspace_bytes:
-        raise ValueError(f"workspace has {ws} bytes, the plan needs {plan.workspace_bytes}")
+    ws_needs = plan.kvq_workspace_bytes if kvq else plan.workspace_bytes
+    if not library_workspace and not plan.is_prefill and ws < ws_needs:
+        raise ValueError(f"workspace has {ws} bytes, the plan needs {ws_needs}")
     _gpu(device_meta, "device_meta")
     _gpu(q, "q", kv)
     _gpu(k_pool, "k_pool", torch.uint8 if kvq else kv)
@@ -1197,22 +1201,22 @@ class PrefixAttention:
         the plan needs none)."""
         return self._workspace_on(None)
 
-    def _workspace_on(self, stream):
+    def _workspace_on(self, stream, kvq=False):
         """The workspace of a call on `stream` (None: the current stream): the
         stream's own, or, while it is being captured, a new one from the
-        graph's pool."""
+        graph's pool. kvq: of a call over 4-bit pools."""
         import torch
         if not self.plan.workspace_bytes:
             return None
         if stream is None:
-            return self._current_workspace(torch.cuda.current_stream(self.device))
+            return self._current_workspace(torch.cuda.current_stream(self.device), kvq)
         with torch.cuda.stream(stream):
-            return self._current_workspace(stream)
+            return self._current_workspace(stream, kvq)
 
-    def _current_workspace(self, s):
+    def _current_workspace(self, s, kvq=False):
         """_workspace_on(s) for the current stream s."""
         import torch
-        n = self.plan.workspace_bytes
+        n = self.plan.kvq_workspace_bytes if kvq else self.plan.workspace_bytes
         if not n:
             return None
         if torch.cuda.is_current_stream_capturing():
@@ -1247,9 +1251,9 @@ class PrefixAttention:
         fn = getattr(_LIB, ("halo_prefix_attn_prefill" if self.plan.is_prefill else "halo_prefix_attn_decode") +
                      ("_kvq" if kvq else ""))
         capturing = torch.cuda.is_current_stream_capturing
-        n = self.plan.workspace_bytes
+        n = self.plan.kvq_workspace_bytes if kvq else self.plan.workspace_bytes
         # (bound during a capture: the graph's memory is not for eager calls)
-        ws = None if capturing() else self._workspace_on(stream)
+        ws = None if capturing() else self._workspace_on(stream, kvq)
         _check_run(self.plan, self.meta, q, k_pool, v_pool, o, lse, ws, library_workspace=ws is None, kvq=kvq)
         s = self._before_run(stream)
         self._bound[self._cur].add(s)
@@ -1293,12 +1297,13 @@ class PrefixAttention:
         if o is None:
             o, lse_new = self.alloc_outputs(q)
             lse = lse if lse is not None else lse_new
-        if _kvq_pair(k_pool, v_pool):
+        kvq = _kvq_pair(k_pool, v_pool)
+        if kvq:
             fn = prefix_attn_prefill_kvq if self.plan.is_prefill else prefix_attn_decode_kvq
         else:
             fn = prefix_attn_prefill if self.plan.is_prefill else prefix_attn_decode
         s = self._before_run(stream)
-        ws = self._current_workspace(s) if stream is None else self._workspace_on(s)
+        ws = self._current_workspace(s, kvq) if stream is None else self._workspace_on(s, kvq)
         with self._enqueue:
             fn(self.plan, self.meta, q, k_pool, v_pool, o, lse, ws, s)
         self._after_run(s)

@@ -110,20 +110,19 @@ def assert_close(w, out_dtype, o, lse, want, split, label=""):
     error, which is at most (D + 16) roundings of sums bounded by B (products,
     three parts for fp32, the scale, the maximum); exp2 and its argument 4 more;
     n roundings in a sum of n keys, in the numerator and in the denominator, 16
-    for rescaling and merging. bf16 queries: a weight is rounded to bf16 for P V
-    (half a step, 2^-8), a partial result to the output's type, and the output
-    itself."""
+    for rescaling and merging. bf16 outputs: a weight is rounded to bf16 for P V
+    (half a step, 2^-8), a partial result to fp16 (2^-11, or 2^-25 of the row's
+    largest element, which is at most the largest A), and the output itself."""
     ro, rl, A, B, keys = want
     D = w.head_dim
     sums = U32 * ((D + 16) * B + 4 * (1 + B) + keys[:, None] + 16)
-    coarse = 0.0
-    if w.dtype == torch.bfloat16:
-        coarse += 2.0 ** -8
-        if out_dtype == torch.bfloat16:
-            coarse += 2.0 ** -8 + (2.0 ** -8 if split else 0.0)
+    coarse, floor = 0.0, 1e-30
+    if out_dtype == torch.bfloat16:
+        coarse = 2 * 2.0 ** -8 + (2.0 ** -11 if split else 0.0)
+        floor += 2.0 ** -25 * A.max(-1, keepdims=True) if split else 0.0
     seen = np.isfinite(rl)
     assert np.isneginf(lse[~seen]).all() and (o[~seen] == 0).all(), f"{label}: rows without keys"
-    tol = A * (coarse + 2 * 2 * sums[..., None]) + 1e-30
+    tol = A * (coarse + 2 * 2 * sums[..., None]) + floor
     err = np.abs(o - ro)
     assert (err[seen] <= tol[seen]).all(), f"{label}: {np.nanmax(err[seen] / tol[seen]):.3f} of the bound, " \
                                            f"finite {np.isfinite(o).all()}"

@@ -201,5 +201,19 @@ def test_attention_refusals(lib, name, prefill):
         args = list(good)
         args[i] = bad
         assert fn(*args) == halo.HALO_ERR_INVALID_ARGUMENT, i
-    if not prefill and plan.workspace_bytes:
-        assert fn(*good[:8], 0, None) == halo.HALO_ERR_WORKSPACE_TOO_SMALL
+    if not prefill:
+        assert plan.kvq_workspace_bytes > plan.workspace_bytes > 0   # (bf16 output: a scale for each partial)
+        for n in (0, plan.workspace_bytes, plan.kvq_workspace_bytes - 1):
+            assert fn(*good[:8], n, None) == halo.HALO_ERR_WORKSPACE_TOO_SMALL
+
+
+def test_workspace_bytes(lib):
+    from workloads import build_workload
+    w = build_workload("ws", 1, 4, 2, 64, torch.bfloat16, [300, 5, 7], [[0, 1], [0, 2]])
+    for out, scales in ((torch.bfloat16, True), (torch.float32, False)):
+        plan = halo.Plan.from_csr(halo.make_params(4, 2, 64, torch.bfloat16, w.num_pool_pages, w.scale, out), w.forest_csr())
+        slots = len(plan.inspect()["merge_parts"])
+        assert plan.stats()["num_merge_rows"] > 0
+        more = plan.kvq_workspace_bytes - plan.workspace_bytes
+        assert more >= 4 * slots and more % 256 == 0 if scales else more == 0
+    assert lib.halo_plan_kvq_workspace_bytes(None) == 0
