@@ -194,8 +194,10 @@ __device__ __forceinline__ void scatter_tile(const KvqScatterArgs& a, int64_t at
 // each of its tiles), and tile_blocks share the whole pages of all sequences
 // equally. Against splits of every sequence's tiles, whole pages or not: 64
 // appends 8.7 -> 4.6 us, 496 appends and 16 chunks 87 -> 18 us (8 heads, d 128).
+// Six waves per SIMD, of the four that its registers would ask for: 32 chunks of 768
+// tokens after other work 37.2 -> 32.7 us (3.9 TB/s), 1024 appends 20.6 -> 17.8.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void kvq_scatter_kernel(KvqScatterArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void kvq_scatter_kernel(KvqScatterArgs a) {
   __shared__ int sums[260];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -291,7 +293,9 @@ __device__ __forceinline__ void read_tile(const uint8_t* tile, T* dst, int64_t r
 
 // The tiles of all sequences (pages, then heads, K before V) are cut into equal
 // contiguous runs, one per wave, so that a few long sequences among many short
-// ones spread over the chip.
+// ones spread over the chip. 8192 workgroups: 256 sequences of 100-500 tokens after
+// other work (400 MB) 115 us, with 2048 127; 25000 tokens 39 and 43; 16384 cost
+// small calls more than they bring large ones.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void kvq_gather_kernel(KvqGatherArgs a) {
   const int lane = threadIdx.x & 63;
@@ -441,7 +445,7 @@ extern "C" halo_status_t halo_kvq_page_gather_kv(const void* k_pool, const void*
                   params->num_kv_heads};
   (void)hipGetLastError();
   by_type(params, [&](auto t, auto d) {
-    hipLaunchKernelGGL((kvq_gather_kernel<decltype(t), decltype(d)::value>), dim3(2048), dim3(256), 0,
+    hipLaunchKernelGGL((kvq_gather_kernel<decltype(t), decltype(d)::value>), dim3(8192), dim3(256), 0,
                        static_cast<hipStream_t>(stream), g);
   });
   return hip_check("4-bit gather launch");
