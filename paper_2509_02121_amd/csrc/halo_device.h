@@ -20,7 +20,7 @@ struct AttnArgs {
   void* o;
   float* lse;
   void* part_o;      // partial O rows, in the output element type
-  float* part_lse;
+  float* part_lse;   // (4-bit pools, bf16 output: pairs with a scale, see store_half)
   const int32_t* seg_page_off;
   const int32_t* seg_len;
   const int32_t* page_ids;
@@ -38,7 +38,6 @@ struct AttnArgs {
   int32_t wide_span;       // launch rounds (of 8 blocks) the wide rounds are spread over
   int32_t num_kv_heads;
   float scale_log2;   // sm_scale * log2(e)
-  float* part_scale;  // 4-bit pools, bf16 output: of each partial row (see store_half)
 };
 
 // The items of a plan over 4-bit pools (halo_kvq_attn.hip).
@@ -197,7 +196,7 @@ __device__ __forceinline__ void store4_part(__bf16* dst, f32x4_t v) { store4(dst
 // by at most 2^-11 of itself (or 2^-25 of the row's largest) where bf16 is by 2^-8:
 // rows of three or more partials were otherwise further off than the output's
 // rounding (70B-shaped decode: 0.0027 of the row, 0.0022 so; 64 requests on 2048 keys
-// 0.0024 and 0.0018).
+// 0.0024 and 0.0018). The scale stands beside the row's LSE, one load for both.
 __device__ __forceinline__ float row_scale(float top) {
   const uint32_t e = min(__float_as_uint(top) & 0x7f800000u, 0x7e800000u);
   return __uint_as_float(e ? e : 0x3f800000u);
@@ -363,10 +362,8 @@ __device__ __forceinline__ void finish_item(const AttnArgs& a, const Item& it, c
         uint16_t* dst = static_cast<uint16_t*>(a.part_o) + prow * D + 4 * grp;
 #pragma unroll
         for (int b = 0; b < NB; ++b) store_half(dst + 16 * b, acc[b] * x);
-        if (grp == 0) {
-          reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
-          a.part_scale[prow] = scale;
-        }
+        if (grp == 0)
+          reinterpret_cast<int2*>(a.part_lse)[prow] = make_int2(part_lse_bits(lse2, lsum), __float_as_int(scale));
       }
     } else if (has_row) {
       const int64_t prow = row.slot;
@@ -998,10 +995,8 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
         for (int q = 0; q < 4; ++q)
           store_half(dst + 32 * b + 8 * q, f32x4_t{acc[b][4 * q], acc[b][4 * q + 1], acc[b][4 * q + 2], acc[b][4 * q + 3]} * x);
-      if (h == 0) {
-        reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, l);
-        a.part_scale[prow] = scale;
-      }
+      if (h == 0)
+        reinterpret_cast<int2*>(a.part_lse)[prow] = make_int2(part_lse_bits(lse2, l), __float_as_int(scale));
     } else if (it.part_base >= 0) {
       const int64_t prow = row.slot;
       TO* dst = static_cast<TO*>(a.part_o) + prow * D + 4 * h;

@@ -420,7 +420,7 @@ __device__ __forceinline__ void store16(TO* dst, const float (&v)[E]) {
 
 struct MergeArgs {
   const void* part_o;     // in the output element type, or in fp16 with a scale per row
-  const float* part_lse;
+  const float* part_lse;  // (pairs with that scale)
   const int32_t* merge_rows;
   const int32_t* merge_indptr;
   const int32_t* merge_parts;
@@ -429,7 +429,6 @@ struct MergeArgs {
   int32_t n_merge;
   int32_t k0;   // partials of entry r at slots k * n_merge + r for k < k0
   int32_t n_parts;
-  const float* part_scale;   // of partials in fp16 (see store_half)
 };
 
 // Rows per merge workgroup (256 threads, 16 bytes of a row per thread).
@@ -469,11 +468,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
   for (int k = 0; k < kBatch; ++k) {
     if (k < a.k0) {
       const int64_t slot = (int64_t)k * a.n_merge + r;
-      lb[k] = __builtin_bit_cast(uint32_t, a.part_lse[slot]);
-      sb[k] = kScaled ? __builtin_bit_cast(uint32_t, a.part_scale[slot]) : 0;
+      if constexpr (kScaled) {
+        const uint2 x = reinterpret_cast<const uint2*>(a.part_lse)[slot];
+        lb[k] = x.x;
+        sb[k] = x.y;
+      } else {
+        lb[k] = __builtin_bit_cast(uint32_t, a.part_lse[slot]);
+      }
       vb[k] = *reinterpret_cast<const u32x4_t*>(part_o + slot * D + E * t);
     } else {
-      lb[k] = sb[k] = 0;
+      lb[k] = 0;
+      if constexpr (kScaled) sb[k] = 0;
       vb[k] = u32x4_t{0u, 0u, 0u, 0u};
     }
   }
@@ -516,7 +521,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
       l[k] = __builtin_bit_cast(float, keep ? lb[k] : neg_inf_bits);
       const uint32_t m = keep ? 0xffffffffu : 0u;
       raw[k] = vb[k] & u32x4_t{m, m, m, m};
-      sc[k] = __builtin_bit_cast(float, sb[k] & m);
+      if constexpr (kScaled) sc[k] = __builtin_bit_cast(float, sb[k] & m);
     }
     fold(l, sc, raw);
   }
@@ -528,8 +533,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
     u32x4_t raw[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      l[k] = pid[k] >= 0 ? a.part_lse[pid[k]] : kNegInf;
-      sc[k] = kScaled && pid[k] >= 0 ? a.part_scale[pid[k]] : 0.f;
+      if constexpr (kScaled) {
+        const float2 x = pid[k] >= 0 ? reinterpret_cast<const float2*>(a.part_lse)[pid[k]] : make_float2(kNegInf, 0.f);
+        l[k] = x.x;
+        sc[k] = x.y;
+      } else {
+        l[k] = pid[k] >= 0 ? a.part_lse[pid[k]] : kNegInf;
+      }
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k)
@@ -550,11 +560,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void m
 // merge kernels walk a row's partials in rounds of 8 of two dependent loads
 // each: 4 requests of 12000-24000 private keys (128 rows of 24-47 partials)
 // 58.3 -> 53.3 us, one of 24000 33 -> 20 us (whole calls, 32/8 heads, d 128).
-// TP: the partials' element type (fp16: with the scales part_scale); slot_of(k): the
-// slot of partial k < n.
+// TP: the partials' element type (fp16: with scales); slot_of(k): the slot of partial
+// k < n.
 template <int D, typename TP, typename TO, typename SlotOf>
-__device__ __forceinline__ void merge_row(const void* part_o, const float* part_lse, const float* part_scale, int n,
-                                          SlotOf slot_of, TO* o, float* lse, int64_t q_row) {
+__device__ __forceinline__ void merge_row(const void* part_o, const float* part_lse, int n, SlotOf slot_of, TO* o,
+                                          float* lse, int64_t q_row) {
   constexpr bool kScaled = std::is_same<TP, _Float16>::value;
   constexpr int E = 16 / (int)sizeof(TP);
   constexpr int TPR = D / E;
@@ -587,8 +597,13 @@ __device__ __forceinline__ void merge_row(const void* part_o, const float* part_
       raw[j] = u32x4_t{0u, 0u, 0u, 0u};
       if (k < n) {
         const int64_t slot = slot_of(k);
-        l[j] = part_lse[slot];
-        if constexpr (kScaled) sc[j] = part_scale[slot];
+        if constexpr (kScaled) {
+          const float2 x = reinterpret_cast<const float2*>(part_lse)[slot];
+          l[j] = x.x;
+          sc[j] = x.y;
+        } else {
+          l[j] = part_lse[slot];
+        }
         raw[j] = *reinterpret_cast<const u32x4_t*>(static_cast<const TP*>(part_o) + slot * D + E * t);
       }
     }
@@ -653,7 +668,7 @@ __global__ __launch_bounds__(256) void merge_row_kernel(MergeArgs a) {
   const int r = blockIdx.x;
   const int p0 = a.merge_indptr[r], n = a.merge_indptr[r + 1] - p0;
   merge_row<D, TP, TO>(
-      a.part_o, a.part_lse, a.part_scale, n,
+      a.part_o, a.part_lse, n,
       [&](int k) { return k < a.k0 ? (int64_t)k * a.n_merge + r : (int64_t)a.merge_parts[p0 + k]; },
       static_cast<TO*>(a.o), a.lse, a.merge_rows[r]);
 }
@@ -727,7 +742,7 @@ __global__ __launch_bounds__(256) void merge_item_row_kernel(MergeItemArgs a) {
   const int r = blockIdx.x % a.blocks_per_item;
   if (r >= mi.n_rows) return;
   merge_row<D, float, TO>(
-      a.part_o, a.part_lse, nullptr, mi.n_parts, [&](int k) { return (int64_t)a.bases[mi.part_begin + k] + r; },
+      a.part_o, a.part_lse, mi.n_parts, [&](int k) { return (int64_t)a.bases[mi.part_begin + k] + r; },
       static_cast<TO*>(a.o), a.lse, a.rows[mi.row_begin + r].q_row);
 }
 
@@ -795,7 +810,7 @@ void launch_merge_items(MergeItemArgs args, int n_items, int most_rows, int64_t 
 }
 
 // The workspace of a plan's calls over 4-bit pools: partials in fp16 have a scale
-// each.
+// each, in pairs with the LSEs that end the plan's.
 size_t kvq_workspace_bytes(const halo_plan_t& plan) {
   const bool half = !plan.prefill && plan.params.out_dtype == HALO_BF16 && plan.n_part_slots > 0;
   return plan.workspace_bytes + (half ? align256((size_t)plan.n_part_slots * sizeof(float)) : 0);
@@ -837,10 +852,6 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq
                         ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
                                                    align256((size_t)plan->n_part_slots * D * part_elem))
                         : nullptr;
-  // (4-bit pools, decode with a bf16 output: the partials' scales last)
-  float* part_scale = kvq && needs > plan->workspace_bytes
-                          ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan->workspace_bytes)
-                          : nullptr;
   AttnArgs args{q, k_pool, v_pool, o, lse, part_o, part_lse,
                 reinterpret_cast<const int32_t*>(m + L.seg_page_off),
                 reinterpret_cast<const int32_t*>(m + L.seg_len),
@@ -853,12 +864,12 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq
                 plan->n_items, whole ? plan->n_whole_wide : plan->n_wide, 0,
                 whole ? plan->n_whole_blocks : plan->n_narrow_blocks, plan->narrow_slots,
                 plan->wide_group, 0,
-                p.num_kv_heads, p.sm_scale * kLog2e, part_scale};
+                p.num_kv_heads, p.sm_scale * kLog2e};
   MergeArgs margs{part_o, part_lse,
                   reinterpret_cast<const int32_t*>(m + L.merge_rows),
                   reinterpret_cast<const int32_t*>(m + L.merge_indptr),
                   reinterpret_cast<const int32_t*>(m + L.merge_parts),
-                  o, lse, plan->n_merge, plan->merge_k0, plan->n_merge_parts, part_scale};
+                  o, lse, plan->n_merge, plan->merge_k0, plan->n_merge_parts};
   if (plan->n_narrow_blocks > 0 &&
       plan->narrow_slots != (p.kv_dtype == HALO_BF16 ? block_waves<__bf16>() : block_waves<float>()))
     return fail(HALO_ERR_INVALID_ARGUMENT, "internal: narrow slots per workgroup differ from its waves");
