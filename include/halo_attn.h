@@ -443,8 +443,8 @@ halo_status_t halo_prefix_attn_prefill_kvq(const halo_plan_t* plan, const void* 
  * outside [0, num_free], more than max_pages pages or max_tokens tokens) is
  * refused whole: every sequence takes part like that and no page is taken.
  * Either way 1 is written to error_flag (may be NULL; 0 never is). The call can
- * be repeated: the same inputs give the same outputs. seq_len, seq_new and
- * free_next must not overlap the outputs. */
+ * be repeated: the same inputs give the same outputs. No array that is written
+ * (block_table and the outputs) may overlap another one. */
 typedef struct {
   int32_t num_seqs;
   int32_t page_size;     /* 16 */

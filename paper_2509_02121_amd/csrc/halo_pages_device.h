@@ -1,5 +1,5 @@
 // Device code that the page kernels over bf16 / fp32 pools (halo_pages.hip) and
-// over 4-bit ones (halo_kv4_pages.hip) share.
+// over 4-bit ones (halo_kvq_pages.hip) share.
 #pragma once
 
 #include <hip/hip_runtime.h>

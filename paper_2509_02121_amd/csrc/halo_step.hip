@@ -292,6 +292,32 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 
 // ---------------------------------------------------------------- host side
 
+// Memory that a call reads or writes.
+struct Range {
+  const char* name;
+  const void* p;
+  int64_t bytes;
+};
+bool overlap(const Range& a, const Range& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
+}
+
+// Whether two operands of `tokens` rows share memory. Rows the same stride apart may
+// lie between each other (q and k in the rows of one projection).
+struct Rows {
+  const void* p;
+  int64_t stride, width;   // bytes
+};
+bool rows_overlap(const Rows& a, const Rows& b, int64_t tokens) {
+  const Range x{"", a.p, (tokens - 1) * a.stride + a.width}, y{"", b.p, (tokens - 1) * b.stride + b.width};
+  if (!overlap(x, y)) return false;
+  if (a.stride != b.stride) return true;
+  const int64_t s = a.stride, d = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+  const int64_t ahead = ((d % s) + s) % s;   // from a row of a to the next one of b
+  return ahead < a.width || s - ahead < b.width;
+}
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 halo_status_t hip_check(const char* what) {
@@ -319,16 +345,28 @@ extern "C" halo_status_t halo_kv_step_tables(const halo_step_sizes_t* sizes, con
       (seqs && sizes->table_width > 0 && !block_table) || (sizes->num_free > 0 && !free_pages) ||
       (sizes->max_pages > 0 && !tables->page_ids))
     return fail(HALO_ERR_INVALID_ARGUMENT, "only positions, slots and error_flag (and arrays of no elements) may be NULL");
-  // every workgroup reads the lengths and the free list's start while others
-  // write their outputs
-  if (seqs) {
-    const void* ins[2] = {seq_len, seq_new};
-    const void* outs[3] = {tables->seq_start, tables->seq_count, tables->seq_end};
-    for (const void* i : ins)
-      for (const void* o : outs)
-        if (i == o) return fail(HALO_ERR_INVALID_ARGUMENT, "seq_len and seq_new must not be outputs too");
+  // every workgroup reads the lengths and the free list while others write their
+  // outputs
+  const int64_t n = sizes->num_seqs;
+  const Range reads[] = {{"seq_len", seq_len, 4 * n}, {"seq_new", seq_new, 4 * n},
+                         {"free_pages", free_pages, 4 * (int64_t)sizes->num_free}, {"free_next", free_next, 4}};
+  const Range writes[] = {{"block_table", block_table, 4 * n * sizes->table_width},
+                          {"tables' seq_page_indptr", tables->seq_page_indptr, 4 * (n + 1)},
+                          {"tables' page_ids", tables->page_ids, 4 * (int64_t)sizes->max_pages},
+                          {"tables' seq_start", tables->seq_start, 4 * n},
+                          {"tables' seq_count", tables->seq_count, 4 * n},
+                          {"tables' seq_end", tables->seq_end, 4 * n},
+                          {"tables' in_token_offset", tables->in_token_offset, 8 * n},
+                          {"tables' positions", tables->positions, 4 * (int64_t)sizes->max_tokens},
+                          {"tables' slots", tables->slots, 8 * (int64_t)sizes->max_tokens},
+                          {"tables' free_next", tables->free_next, 4},
+                          {"error_flag", error_flag, 4}};
+  for (const Range& w : writes) {
+    for (const Range& r : reads)
+      if (overlap(w, r)) return fail(HALO_ERR_INVALID_ARGUMENT, std::string(r.name) + " must not overlap " + w.name);
+    for (const Range* v = writes; v != &w; ++v)
+      if (overlap(w, *v)) return fail(HALO_ERR_INVALID_ARGUMENT, std::string(v->name) + " must not overlap " + w.name);
   }
-  if (free_next == tables->free_next) return fail(HALO_ERR_INVALID_ARGUMENT, "free_next must not be the output too");
   StepArgs g{*tables, seq_len, seq_new, block_table, free_pages, free_next, error_flag,
              sizes->num_seqs, sizes->table_width, sizes->num_free, sizes->max_tokens, sizes->max_pages, 0, 0, 0};
   // A group of sequences for each of up to 512 workgroups (2000 sequences 6.6 us,
@@ -388,6 +426,19 @@ extern "C" halo_status_t halo_rope_qk(const halo_rope_params_t* rope, float ampl
     g.in_stride[z] = in_stride[z];
     g.out_stride[z] = out_stride[z];
   }
+  for (int z = 0; z < 2; ++z) {
+    if (heads[z] == 0) continue;
+    const int64_t width = (int64_t)heads[z] * D * elt;
+    const Rows to{out[z], out_stride[z] * elt, width};
+    for (int y = 0; y < 2; ++y) {
+      if (heads[y] == 0) continue;
+      const int64_t w = (int64_t)heads[y] * D * elt;
+      if ((y != z || in[y] != out[z]) && rows_overlap(to, Rows{in[y], in_stride[y] * elt, w}, num_tokens))
+        return fail(HALO_ERR_INVALID_ARGUMENT, "an output must be its operand, or overlap none");
+      if (y < z && rows_overlap(to, Rows{out[y], out_stride[y] * elt, w}, num_tokens))
+        return fail(HALO_ERR_INVALID_ARGUMENT, "q_out and k_out must not overlap");
+    }
+  }
   g.positions = positions;
   g.turns = turns;
   g.amplitude = amplitude;
@@ -405,6 +456,7 @@ extern "C" halo_status_t halo_rope_qk(const halo_rope_params_t* rope, float ampl
   g.slots = slots;
   const int per_block = most / slots;
   const int64_t blocks = ((int64_t)num_tokens + per_block - 1) / per_block;
+  if (blocks >= 1 << 24) return fail(HALO_ERR_UNSUPPORTED, "too many tokens for one call (2^32 threads)");
   const dim3 grid((unsigned)blocks);
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();

@@ -845,17 +845,28 @@ def bind_kvq_page_gather_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, s
                                    k_out, v_out, error_flag, stream))
 
 
-def kvq_page_copy(pool, params, pool_kind, src_pages, dst_pages, error_flag=None, stream=None):
-    """halo_kvq_page_copy on torch tensors (int arrays on the GPU)."""
+def _kvq_copy_args(pool, params, pool_kind, src_pages, dst_pages, error_flag, stream):
     import torch
-    load_library()
     _gpu(pool, "pool", torch.uint8, kvq_pool_bytes(params, pool_kind))
     _gpu(src_pages, "src_pages", torch.int32)
     _gpu(dst_pages, "dst_pages", torch.int32, src_pages.numel())
     _one_gpu([pool, src_pages, dst_pages] + _flag(error_flag), stream)
-    _check(_LIB.halo_kvq_page_copy(pool.data_ptr(), ctypes.byref(params), int(pool_kind), src_pages.data_ptr(),
-                                   dst_pages.data_ptr(), int(src_pages.numel()),
-                                   error_flag.data_ptr() if error_flag is not None else None, _stream_handle(stream)))
+    return (pool.data_ptr(), ctypes.byref(params), int(pool_kind), src_pages.data_ptr(), dst_pages.data_ptr(),
+            int(src_pages.numel()), error_flag.data_ptr() if error_flag is not None else None, _stream_handle(stream))
+
+
+def kvq_page_copy(pool, params, pool_kind, src_pages, dst_pages, error_flag=None, stream=None):
+    """halo_kvq_page_copy on torch tensors (int arrays on the GPU)."""
+    load_library()
+    _check(_LIB.halo_kvq_page_copy(*_kvq_copy_args(pool, params, pool_kind, src_pages, dst_pages, error_flag,
+                                                   stream)))
+
+
+def bind_kvq_page_copy(pool, params, pool_kind, src_pages, dst_pages, error_flag=None, stream=None):
+    """kvq_page_copy as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kvq_page_copy, _kvq_copy_args(pool, params, pool_kind, src_pages, dst_pages, error_flag,
+                                                          stream))
 
 
 class StepTables:
@@ -902,7 +913,8 @@ def _step_args(tables, seq_len, seq_new, block_table, free_pages, free_next, err
         _gpu(t, name, dtype, numel)
         ptrs[name] = t.data_ptr()
         used.append(t)
-        for other, what in ((seq_len, "seq_len"), (seq_new, "seq_new"), (free_next, "free_next")):
+        for other, what in ((seq_len, "seq_len"), (seq_new, "seq_new"), (block_table, "block_table"),
+                            (free_pages, "free_pages"), (free_next, "free_next")):
             if _overlap(t, other):
                 raise ValueError(f"{what} must not overlap the output {name}")
     _one_gpu(used + _flag(error_flag), stream)

@@ -226,6 +226,10 @@ def test_page_copy(gpu_lib):
             halo.kvq_page_copy(dev, p, z, _cuda(src), _cuda(dst), err)
             want, flagged = paged_kv.page_copy(pools[z].reshape(-1), 3 * pools[z].shape[2], 12, src, dst)
             assert np.array_equal(dev.cpu().numpy().reshape(-1), want) and flagged and err.item() == 1
+            again, lists = torch.from_numpy(pools[z]).cuda(), (_cuda(src), _cuda(dst))
+            call = halo.bind_kvq_page_copy(again, p, z, *lists)
+            call()
+            assert torch.equal(again, dev)
 
 
 def test_long_offsets(gpu_lib):

@@ -107,6 +107,30 @@ def test_rope_qk_unaligned(lib):
     assert _rope_call(lib, turns=at + 4) == halo.HALO_ERR_INVALID_ARGUMENT
 
 
+def test_rope_qk_overlaps(lib):
+    """Two tokens of two query heads (256 elements) and one key head (128), rows of
+    384 elements at byte 0 of the buffer, or of 256 and 128."""
+    buf = np.zeros(4096, np.float32)
+    at = (buf.ctypes.data + 15) // 16 * 16
+    far = {"q": at, "k": at + 4 * 1024, "qo": at + 4 * 2048, "ko": at + 4 * 3000}
+    bad = [{"qo": at + 16}, {"qo": at + 4 * 512 - 16}, {"qo": far["k"]}, {"ko": at}, {"ko": at + 4 * 255 + 4},
+           {"ko": far["k"] + 32}, {"ko": far["qo"] + 4 * 256}, {"qo": far["k"] - 4 * 256},
+           {"qs": 384, "qos": 384, "qo": at + 4 * 128},   # a row apart by less than its width
+           {"qs": 384, "qo": at, "ks": 384, "kos": 384, "qos": 384, "ko": at + 4 * 240},
+           {"qs": 384, "kos": 512, "ko": at + 4 * 256}]   # strides that differ
+    for given in bad:
+        assert _rope_call(lib, **{**far, **given}) == halo.HALO_ERR_INVALID_ARGUMENT, given
+        assert b"overlap" in lib.halo_last_error_message(), given
+
+
+def test_rope_qk_too_many_tokens(lib):
+    """A workgroup takes the 40 heads of one token: 2^24 of them are 2^32 threads."""
+    a = 1 << 20   # (addresses far enough apart, read by nobody)
+    far = {"q": a, "k": a + (1 << 50), "qo": a, "ko": a + (1 << 51)}
+    assert _rope_call(lib, **far, tokens=1 << 24, hq=32, hk=8, qs=4096, qos=4096, ks=1024,
+                      kos=1024) == halo.HALO_ERR_UNSUPPORTED
+
+
 def test_rope_qk_nothing_to_do(lib):
     assert _rope_call(lib, tokens=0) == halo.HALO_OK
     assert _rope_call(lib, hq=0, hk=0) == halo.HALO_OK
@@ -137,6 +161,10 @@ def test_step_tables_refusals(lib):
     assert _tables_call(lib, seq_end="seq_len") == halo.HALO_ERR_INVALID_ARGUMENT
     assert _tables_call(lib, seq_count="seq_new") == halo.HALO_ERR_INVALID_ARGUMENT
     assert _tables_call(lib, free_next="in_next") == halo.HALO_ERR_INVALID_ARGUMENT
+    for written, other in (("page_ids", "free_pages"), ("slots", "block_table"), ("error", "free_next"),
+                           ("positions", "slots"), ("seq_start", "seq_new"), ("block_table", "free_pages")):
+        assert _tables_call(lib, **{written: other}) == halo.HALO_ERR_INVALID_ARGUMENT
+        assert b"overlap" in lib.halo_last_error_message()
     assert lib.halo_kv_step_tables(None, *[None] * 8) == halo.HALO_ERR_INVALID_ARGUMENT
 
 
