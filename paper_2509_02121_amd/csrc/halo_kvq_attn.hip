@@ -275,11 +275,15 @@ constexpr int kKvqWaves = 4;
 constexpr int kKvqRows = kKvqWaves * 32;
 
 // Share (percent) of the narrow rounds dealt among the wide ones (see
-// kWideSpanNarrowPct): narrow items are a third as long as over bf16 pages, so the
-// wide ones, of which an unpaired rest would end the launch, start earlier. 70B-shaped
-// decode 526 us with 80, 495 with 40, 512 with 20; two-level tree (d 64) 60, 49, 49;
-// 500 requests of 32 query heads 199 with 40, 181 with 20.
-constexpr int kKvqNarrowPct = 40;
+// kWideSpanNarrowPct), by the number of wide workgroups. Up to one for each CU start
+// first, all at once, and the narrow ones run beside and behind them: those that start
+// later would end the launch. More are spread out, so that the two kinds share CUs.
+// (us, with 0, 20 and 40) 256 workgroups: 128 requests of 64 query heads in 4 groups
+// of 8192 shared and 128-512 own keys 71, 82, 83; 600 of 32 in 8 of 4096 151, 153,
+// 177; 384: 300 of 64 in 6 of 4096 99, 98, 113, 700 in 8 of 2048 with up to 2048 own
+// 255, 253, 246; 512: 512 in 4 of 8192 with up to 4096 own 442, 408, 394; 1024: the
+// 70B-shaped decode 554, 521, 508 (with 60 517).
+int kvq_narrow_pct(int wide_units) { return wide_units <= kNumCUs ? 0 : wide_units < 2 * kNumCUs ? 20 : 40; }
 
 template <typename T, int RB> constexpr int kvq_waves() { return RB > 0 ? kKvqWaves : block_waves<T>(); }
 
@@ -350,7 +354,7 @@ void launch_items(AttnArgs args, const halo_plan& plan, hipStream_t stream) {
     args.wide_group *= runs;
   }
   args.narrow_blocks *= block_waves<T>() / (wide ? kKvqWaves : block_waves<T>());
-  lay_out_rounds(args, wide, kKvqNarrowPct);
+  lay_out_rounds(args, wide, kvq_narrow_pct(args.n_wide));
   const int grid = args.wide_blocks + args.narrow_blocks;
   if (grid == 0) return;
   if constexpr (sizeof(T) == 2) {
