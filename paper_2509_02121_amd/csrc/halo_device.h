@@ -486,6 +486,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   const int c = lane & 31;
   const int h = lane >> 5;
   const Item it = a.wide_items[item_id];
+  if (KVQ && row0 >= it.n_rows) return;   // (a run past the rows of a shorter item)
   // waves without rows still load their share of every step image
   const bool computes = row0 + wave * 32 < it.n_rows;
 
