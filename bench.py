@@ -36,7 +36,7 @@ def source_sha256():
     traffic stays valid only for the code it was measured on."""
     import hashlib
     h = hashlib.sha256()
-    for name in ("halo_kernels.hip", "halo_plan.cpp", "halo_internal.h"):
+    for name in ("halo_kernels.hip", "halo_device.h", "halo_plan.cpp", "halo_internal.h"):
         with open(os.path.join(ROOT, "paper_2509_02121_amd", "csrc", name), "rb") as f:
             h.update(f.read())
     return h.hexdigest()
