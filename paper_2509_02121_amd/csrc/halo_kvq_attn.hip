@@ -16,10 +16,20 @@
 // 64 conversions (about 5 cycles each, measured) and 40 instructions for the scales
 // to the softmax and the 16 MFMAs.
 //
+// What bounds them (d 128, bf16): narrow items over private keys read at the rate of
+// the memory (1024 requests of 256-2048 keys, 1.24 GB: 252 us, 4.9 TB/s), those over
+// shared keys wait for their instructions (VALU 926 cycles a step and SIMD); wide
+// items for products and VALU instructions together, which take 95% of the cycles
+// (32 chunks of 512 tokens on 4096 keys 1225 us, 0.95 PFLOP/s, 8 prefixes of 8192
+// under 1024 requests 303 us). A launch of both kinds takes nearly the sum of the two
+// (70B-shaped decode 508 us); small calls are chains of dependent loads in two
+// launches (8 requests of 300 keys 6.8 us).
+//
 // fp32 queries and outputs: K and V are exact in bf16, so products with fp32
 // accuracy need only q (fp32 queries) and P (fp32 outputs) split into three bf16
 // parts each (8 + 8 + 8 bits): three MFMAs of 16x16x32 in place of eight 16x16x4
-// fp32 ones.
+// fp32 ones (4 requests of 12000-24000 keys 32 us: 16 steps in a chain, of 0.9 us
+// alone on a SIMD and 1.4 where two share it).
 
 #include <hip/hip_runtime.h>
 
@@ -267,10 +277,10 @@ constexpr int kKvqNarrowStages = 2;
 // a CU holds two: narrow slots are taken in runs of four (two for a plan's bf16
 // workgroup of eight), wide items in runs of 128 rows. Next to each other on a CU, a
 // wide workgroup's products and a narrow one's loads and conversions overlap
-// (70B-shaped decode: 526 us, with workgroups of eight 545). Launches of narrow items
-// alone keep the plan's workgroups, one to a CU: with two half as large the
-// dispatcher fills some CUs twice and leaves others empty (64 requests on 2048
-// shared keys 16.4 us, with eight 12.8).
+// (70B-shaped decode 508 us; when it took 526, workgroups of eight took 545).
+// Launches of narrow items alone keep the plan's workgroups, one to a CU: with two
+// half as large the dispatcher fills some CUs twice and leaves others empty (64
+// requests on 2048 shared keys 16.4 us, with eight 12.8).
 constexpr int kKvqWaves = 4;
 constexpr int kKvqRows = kKvqWaves * 32;
 
