@@ -9,7 +9,7 @@
 // their D / 32 vectors. 8 dims are one dword of K codes as they are; V codes have
 // the 8 tokens of a half (slots 8 h .. + 7) of one dim in a dword, which is a
 // transposition of 8 x 8 codes between the 8 lanes of a half and the 8 codes of a
-// lane: three rounds of lane exchanges, no LDS.
+// lane: three rounds of lane exchanges, no LDS (CodeTransposer).
 
 #include <hip/hip_runtime.h>
 
@@ -57,16 +57,29 @@ __device__ __forceinline__ void store_decoded(float* p, uint32_t w, float scale)
 
 // Codes i of the lanes 4 (8 h + j) + g become codes j of the lanes
 // 4 (8 h + i) + g (its own inverse): bit b of i and of j are swapped by an
-// exchange with the lane 4 << b away.
-__device__ __forceinline__ uint32_t transpose_codes(uint32_t x, int lane) {
-  constexpr uint32_t kLow[3] = {0x0f0f0f0fu, 0x00ff00ffu, 0x0000ffffu};
-#pragma unroll
-  for (int b = 0; b < 3; ++b) {
-    const uint32_t y = __shfl_xor(x, 4 << b);
-    x = lane & (4 << b) ? (x & ~kLow[b]) | ((y >> (4 << b)) & kLow[b]) : (x & kLow[b]) | ((y & kLow[b]) << (4 << b));
+// exchange with the lane 4 << b away, on the VALU and without branches (with
+// __shfl_xor and a choice between two results, 12 branches and LDS waits a tile: 64
+// appends 4.65 -> 4.36 us, 60 with 4 chunks 7.2 -> 6.8).
+struct CodeTransposer {
+  uint32_t rot, keep, bytes, halves;
+  __device__ __forceinline__ explicit CodeTransposer(int lane) {
+    rot = lane & 4 ? 4 : 28;
+    keep = lane & 4 ? 0xf0f0f0f0u : 0x0f0f0f0fu;
+    bytes = lane & 8 ? 0x03070105u : 0x06020400u;
+    halves = lane & 16 ? 0x07060302u : 0x05040100u;
   }
-  return x;
-}
+  __device__ __forceinline__ uint32_t operator()(uint32_t x) const {
+    // 4 lanes away: reversed in 8 lanes, then in 4
+    const int half = __builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, true);        // row_half_mirror
+    uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, half, 0x1B, 0xf, 0xf, true);   // quad_perm 3,2,1,0
+    x = (x & keep) | (__builtin_amdgcn_alignbit(y, y, rot) & ~keep);
+    y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true);           // row_ror:8
+    x = __builtin_amdgcn_perm(y, x, bytes);
+    // the even and the odd row's
+    const auto rows = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return __builtin_amdgcn_perm(rows[1], rows[0], halves);
+  }
+};
 
 // The dword of a V tile that holds dim 32 s + 8 g + i for half h.
 __device__ __forceinline__ int v_dword(int s, int g, int i, int h) {
@@ -129,7 +142,7 @@ __device__ __forceinline__ void write_tile(const T* src, int64_t row, uint8_t* t
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int e = kvq_exponent(slot_max(top[s]));
-      w[s] = e == 255 ? 0 : kvq_encode(v[s], kvq_scale(e));
+      w[s] = kvq_encode(v[s], kvq_scale(e)) & (e == 255 ? 0u : 0xffffffffu);
       scales |= (uint32_t)e << (8 * s);
     }
     if (!live) return;
@@ -154,9 +167,11 @@ __device__ __forceinline__ void write_tile(const T* src, int64_t row, uint8_t* t
       mask |= tok >= lo && tok < hi ? 0xfu << (4 * j) : 0u;
     }
     uint32_t* codes = reinterpret_cast<uint32_t*>(tile);
+    const CodeTransposer transpose(lane);
+    const uint32_t real = e == 255 ? 0u : 0xffffffffu;
     uint32_t w[S];
 #pragma unroll
-    for (int s = 0; s < S; ++s) w[s] = transpose_codes(e == 255 ? 0 : kvq_encode(v[s], kvq_scale(e)), lane);
+    for (int s = 0; s < S; ++s) w[s] = transpose(kvq_encode(v[s], kvq_scale(e)) & real);
     if (lo != 0 || hi != 16) {
 #pragma unroll
       for (int s = 0; s < S; ++s) w[s] = (w[s] & mask) | (mask != 0xffffffffu ? codes[v_dword(s, g, i, h)] & ~mask : 0u);
@@ -195,10 +210,11 @@ __device__ __forceinline__ void scatter_tile(const KvqScatterArgs& a, int64_t at
 // equally. Against splits of every sequence's tiles, whole pages or not: 64
 // appends 8.7 -> 4.6 us, 496 appends and 16 chunks 87 -> 18 us (8 heads, d 128).
 // 32 chunks of 512-1024 tokens (137 MB) 24.7 us, 5.5 TB/s out of the caches.
-// Six waves per SIMD, of the four that its registers would ask for: 32 chunks of 768
-// tokens after other work 37.2 -> 32.7 us (3.9 TB/s), 1024 appends 20.6 -> 17.8.
+// Five waves per SIMD: with the four that its registers would ask for 32 chunks of
+// 512-1024 tokens (after other work) take 36.2 us, so 30.7, 1024 appends 19.0 and 17.8;
+// six spill (64 appends 4.34 us, so 4.10).
 template <typename T, int D>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(6))) void kvq_scatter_kernel(KvqScatterArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(5))) void kvq_scatter_kernel(KvqScatterArgs a) {
   __shared__ int sums[260];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -278,12 +294,13 @@ __device__ __forceinline__ void read_tile(const uint8_t* tile, T* dst, int64_t r
 #pragma unroll
     for (int s = 0; s < S; ++s) scale[s] = kvq_scale((scales >> (8 * s)) & 0xff);
   } else {
+    const CodeTransposer transpose(lane);
     const uint32_t e = *reinterpret_cast<const uint16_t*>(tile + D * 8 + 2 * sl);
 #pragma unroll
     for (int s = 0; s < S; ++s) w[s] = codes[v_dword(s, g, sl & 7, sl >> 3)];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      w[s] = transpose_codes(w[s], lane);
+      w[s] = transpose(w[s]);
       scale[s] = __uint_as_float(e << 16);
     }
   }
