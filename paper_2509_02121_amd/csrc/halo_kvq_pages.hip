@@ -209,7 +209,7 @@ __device__ __forceinline__ void scatter_tile(const KvqScatterArgs& a, int64_t at
 // each of its tiles), and tile_blocks share the whole pages of all sequences
 // equally. Against splits of every sequence's tiles, whole pages or not: 64
 // appends 8.7 -> 4.6 us, 496 appends and 16 chunks 87 -> 18 us (8 heads, d 128).
-// 32 chunks of 512-1024 tokens (137 MB) 24.7 us, 5.5 TB/s out of the caches.
+// 32 chunks of 512-1024 tokens (137 MB) 23.4 us, 5.9 TB/s out of the caches.
 // Five waves per SIMD: with the four that its registers would ask for 32 chunks of
 // 512-1024 tokens (after other work) take 36.2 us, so 30.7, 1024 appends 19.0 and 17.8;
 // six spill (64 appends 4.34 us, so 4.10).
