@@ -851,8 +851,10 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
     // reads of step t after the first of them; each MFMA followed by VALU
     // work
     // (KVQ: half of the K reads after three of the P V products, which leaves
-    // registers for the conversion)
-    constexpr int kBetween = KVQ ? 4 : 5, kAhead = KVQ ? NK / 2 : NK;
+    // registers for the conversion, and more VALU work to the Q K^T products: 4 and 6
+    // instructions, chunked prefill 1184 us, 4 and 4 1191, 5 and 6 1191, 6 and 6 1228;
+    // d 64: 3 and 6 843, 4 and 4 850)
+    constexpr int kBetween = KVQ ? (D == 128 ? 4 : 3) : 5, kBehind = KVQ ? 6 : 5, kAhead = KVQ ? NK / 2 : NK;
     __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
 #pragma unroll
     for (int k = 0; k < 2 * NO + 1; ++k) {
@@ -864,7 +866,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
 #pragma unroll
     for (int k = 0; k < NK - 1; ++k) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, kBetween, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, kBehind, 0);
     }
   };
 
@@ -931,13 +933,26 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
         const bool fast = !first && more && ps[st].full && prev.full && (!KVQ || full2);
         auto fetch = [&]() { q_fetch(pick(ps[pv_st].valid, ps[pv_st], ps[st]), qr); };
         auto convert = [&]() {
-          if constexpr (KVQ) q_convert(fast || full2, qr, lds[(st + 2) % kImages]);
-          if (kFetchEarly && fast) fetch();
+          if constexpr (KVQ) q_convert(full2, qr, lds[(st + 2) % kImages]);
+        };
+        auto convert_fast = [&]() {
+          if constexpr (KVQ) {
+            if constexpr (!kFetchEarly) {
+              // (of its own: what it shares with the one below would be computed
+              // before the branch, and the loads waited for there; 70B-shaped decode
+              // 501 -> 494 us)
+#pragma unroll
+              for (int k = 0; k < ND; ++k) asm volatile("" : "+v"(qr.k[k]), "+v"(qr.v[k]));
+              asm volatile("" : "+v"(qr.k_scale), "+v"(qr.v_scale));
+            }
+            q_convert(true, qr, lds[(st + 2) % kImages]);
+          }
+          if constexpr (kFetchEarly) fetch();
         };
         if (computes && fast) {
           float alpha;
           fast_iter(vf, lds[nx % kImages], lds[st % kImages], pf[nxt_p], sacc[cur_p], sacc[nxt_p], pf[cur_p], alpha,
-                    convert);
+                    convert_fast);
           if (__any(alpha != 1.f)) {
 #pragma unroll
             for (int b = 0; b < NO; ++b) acc[b] *= alpha;
@@ -960,7 +975,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
         }
         if constexpr (KVQ) {
           if (!full2) q_scales(qr, lds[(st + 2) % kImages]);
-          if (!(kFetchEarly && fast)) fetch();
+          if (!(kFetchEarly && computes && fast)) fetch();
         }
         first = false;
         if (!more) {
