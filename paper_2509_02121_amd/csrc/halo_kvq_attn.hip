@@ -20,9 +20,9 @@
 // the memory (1024 requests of 256-2048 keys, 1.24 GB: 252 us, 4.9 TB/s), those over
 // shared keys wait for their instructions (VALU 926 cycles a step and SIMD); wide
 // items for products and VALU instructions together, which take 95% of the cycles
-// (32 chunks of 512 tokens on 4096 keys 1225 us, 0.95 PFLOP/s, 8 prefixes of 8192
-// under 1024 requests 303 us). A launch of both kinds takes nearly the sum of the two
-// (70B-shaped decode 508 us); small calls are chains of dependent loads in two
+// (32 chunks of 512 tokens on 4096 keys 1190 us, 0.98 PFLOP/s, 8 prefixes of 8192
+// under 1024 requests 300 us). A launch of both kinds takes nearly the sum of the two
+// (70B-shaped decode 492 us); small calls are chains of dependent loads in two
 // launches (8 requests of 300 keys 6.8 us).
 //
 // fp32 queries and outputs: K and V are exact in bf16, so products with fp32
@@ -277,7 +277,7 @@ constexpr int kKvqNarrowStages = 2;
 // a CU holds two: narrow slots are taken in runs of four (two for a plan's bf16
 // workgroup of eight), wide items in runs of 128 rows. Next to each other on a CU, a
 // wide workgroup's products and a narrow one's loads and conversions overlap
-// (70B-shaped decode 508 us; when it took 526, workgroups of eight took 545).
+// (70B-shaped decode 492 us; when it took 526, workgroups of eight took 545).
 // Launches of narrow items alone keep the plan's workgroups, one to a CU: with two
 // half as large the dispatcher fills some CUs twice and leaves others empty (64
 // requests on 2048 shared keys 16.4 us, with eight 12.8).
@@ -292,7 +292,7 @@ constexpr int kKvqRows = kKvqWaves * 32;
 // of 8192 shared and 128-512 own keys 71, 82, 83; 600 of 32 in 8 of 4096 151, 153,
 // 177; 384: 300 of 64 in 6 of 4096 99, 98, 113, 700 in 8 of 2048 with up to 2048 own
 // 255, 253, 246; 512: 512 in 4 of 8192 with up to 4096 own 442, 408, 394; 1024: the
-// 70B-shaped decode 554, 521, 508 (with 60 517).
+// 70B-shaped decode 554, 521, 508 (with 60 517; 492 since).
 int kvq_narrow_pct(int wide_units) { return wide_units <= kNumCUs ? 0 : wide_units < 2 * kNumCUs ? 20 : 40; }
 
 template <typename T, int RB> constexpr int kvq_waves() { return RB > 0 ? kKvqWaves : block_waves<T>(); }
