@@ -355,7 +355,8 @@ halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t* params,
  * its largest magnitude rounded to two significant bits, less two (at least
  * 2^-126); its codes are the nearest ones, ties to the even code, magnitudes past
  * 6 to 6. A block with an infinity or a NaN becomes NaN (scale byte 255, or bf16
- * NaN). Every value that a code stands for is exact in bf16.
+ * NaN). Every value that a code stands for is exact in bf16; a magnitude of 3.5 *
+ * 2^126 (2.98e38) or more is stored as 2^128, which reads as an infinity.
  * Pools are bytes, [num_pool_pages][num_kv_heads][tile], and a tile (D = head_dim)
  *   K: codes  [g: 4][token: 16][s: D/32][i: 8], dim 32 s + 8 g + i   (D * 8 bytes)
  *      scales [token: 16][s: D/32]                                    (D / 2 bytes)
@@ -366,7 +367,8 @@ halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t* params,
  * v_pool. */
 
 /* Bytes of a 4-bit pool (-1 and an error message for unsupported params). Of
- * params num_kv_heads, head_dim, page_size and num_pool_pages are used. */
+ * params num_kv_heads (up to 65536), head_dim, page_size, num_pool_pages (up to
+ * 2^31 - 1) and kv_dtype are looked at. */
 int64_t halo_kvq_pool_bytes(const halo_attn_params_t* params, halo_pool_kind_t pool_kind);
 
 /* halo_kv_page_scatter_kv into 4-bit pools: the tokens (of kv_dtype) are

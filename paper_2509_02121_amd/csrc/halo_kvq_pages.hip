@@ -368,6 +368,8 @@ halo_status_t check_pool_params(const halo_attn_params_t* p) {
   if (p->page_size != 16) return fail(HALO_ERR_UNSUPPORTED, "page_size must be 16");
   if (p->num_kv_heads < 1) return fail(HALO_ERR_INVALID_ARGUMENT, "num_kv_heads must be >= 1");
   if (p->num_pool_pages < 0) return fail(HALO_ERR_INVALID_ARGUMENT, "num_pool_pages must be >= 0");
+  if (p->num_kv_heads > 65536 || p->num_pool_pages > INT32_MAX)   // (products of these stay in their types)
+    return fail(HALO_ERR_UNSUPPORTED, "at most 65536 heads and 2^31 - 1 pages");
   if (p->kv_dtype != HALO_BF16 && p->kv_dtype != HALO_F32)
     return fail(HALO_ERR_UNSUPPORTED, "kv_dtype must be HALO_F32 or HALO_BF16");
   return HALO_OK;

@@ -2,6 +2,8 @@
 quantised into pages (appends, chunks, ragged ones), read back, and pages
 copied."""
 
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -285,3 +287,21 @@ def test_in_a_graph_and_on_a_stream(gpu_lib):
     halo.kvq_page_gather_kv(*ref, p, ids, indptr, total, out_off, *out, stream=side)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_largest_magnitudes(gpu_lib, dtype):
+    """From 3.5 * 2^126 on a value is stored as 2^128: an infinity, where one below
+    it is finite, and so are its neighbours."""
+    p = _params(64, 1, 2, dtype)
+    k, v = halo.alloc_kvq_pools(p)
+    x = torch.zeros(2, 1, 64, dtype=dtype, device="cuda")
+    x[0, 0, 5], x[0, 0, 6] = 2.0 ** 126 * 3.5, -2.0 ** 126
+    x[1, 0, 5], x[1, 0, 6] = 2.0 ** 126 * 3.375, -2.0 ** 126
+    lists = (_cuda([0]), _cuda([0, 1]))
+    halo.kvq_page_scatter_kv(k, v, p, *lists, _cuda([0]), _cuda([2]), _cuda([0], torch.int64), x, x)
+    out = [torch.empty_like(x) for _ in range(2)]
+    halo.kvq_page_gather_kv(k, v, p, *lists, _cuda([2]), _cuda([0], torch.int64), *out)
+    for o in out:
+        assert o[0, 0, 5] == math.inf and o[1, 0, 5] == 2.0 ** 126 * 3 and (o[:, 0, 6] == -2.0 ** 126).all()
+        assert (o[:, 0, 7:] == 0).all()

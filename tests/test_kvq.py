@@ -82,7 +82,8 @@ def test_pool_bytes(lib):
     assert halo.kvq_pool_bytes(_params(head_dim=128), halo.HALO_POOL_V) == 10 * 2 * 1056
     k, v = halo.alloc_kvq_pools(_params(head_dim=128), "cpu")
     assert k.shape == (10, 2, 1088) and v.shape == (10, 2, 1056)
-    for bad in ({"head_dim": 96}, {"page_size": 32}, {"num_kv_heads": 0}, {"kv_dtype": 7}, {"num_pool_pages": -1}):
+    for bad in ({"head_dim": 96}, {"page_size": 32}, {"num_kv_heads": 0}, {"kv_dtype": 7}, {"num_pool_pages": -1},
+                {"num_kv_heads": 1 << 30}, {"num_pool_pages": 1 << 60}):
         with pytest.raises(halo.HaloError):
             halo.kvq_pool_bytes(_params(**bad), halo.HALO_POOL_K)
     with pytest.raises(halo.HaloError):
@@ -126,6 +127,8 @@ def test_refusals(lib, call):
     assert run(params=_params(kv_dtype=3)) == halo.HALO_ERR_UNSUPPORTED
     assert run(params=_params(num_kv_heads=0)) == halo.HALO_ERR_INVALID_ARGUMENT
     assert run(params=_params(num_pool_pages=-1)) == halo.HALO_ERR_INVALID_ARGUMENT
+    assert run(params=_params(num_kv_heads=1 << 30)) == halo.HALO_ERR_UNSUPPORTED
+    assert run(params=_params(num_pool_pages=1 << 40)) == halo.HALO_ERR_UNSUPPORTED
     if call == "copy":
         assert run(kind=2) == halo.HALO_ERR_INVALID_ARGUMENT
 
