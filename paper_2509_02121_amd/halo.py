@@ -1052,12 +1052,6 @@ def bind_rope_qk(q, k, positions, rope, q_out=None, k_out=None, stream=None):
     return _bound(_LIB.halo_rope_qk, _rope_args(q, k, positions, rope, q_out, k_out, stream))
 
 
-def _kvq_pair(k_pool, v_pool):
-    """Whether the pools are 4-bit ones (both or neither)."""
-    import torch
-    return k_pool.dtype == torch.uint8 and v_pool.dtype == torch.uint8
-
-
 class PrefixAttention:
     """Plan + uploaded metadata + workspace for one forest on one GPU.
 
@@ -1094,6 +1088,7 @@ class PrefixAttention:
         self.plan = Plan.from_csr(params, csr, options)
         self.options = options
         self.device = torch.device(device)
+        self._uint8 = torch.uint8
         self._metas = [self._meta_buffer(self.plan.device_meta_bytes), None]
         self._cur = 0
         # one workspace per stream (the MAX_WORKSPACES latest), so that calls
@@ -1265,7 +1260,7 @@ class PrefixAttention:
         is being captured, one from the graph's own pool: the graph may then
         replay on any stream, beside any other call of this object."""
         import torch
-        kvq = _kvq_pair(k_pool, v_pool)
+        kvq = k_pool.dtype is self._uint8 and v_pool.dtype is self._uint8   # 4-bit pools
         fn = getattr(_LIB, ("halo_prefix_attn_prefill" if self.plan.is_prefill else "halo_prefix_attn_decode") +
                      ("_kvq" if kvq else ""))
         capturing = torch.cuda.is_current_stream_capturing
@@ -1315,7 +1310,7 @@ class PrefixAttention:
         if o is None:
             o, lse_new = self.alloc_outputs(q)
             lse = lse if lse is not None else lse_new
-        kvq = _kvq_pair(k_pool, v_pool)
+        kvq = k_pool.dtype is self._uint8 and v_pool.dtype is self._uint8   # 4-bit pools
         if kvq:
             fn = prefix_attn_prefill_kvq if self.plan.is_prefill else prefix_attn_decode_kvq
         else:
