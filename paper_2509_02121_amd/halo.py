@@ -869,6 +869,13 @@ def bind_kvq_page_copy(pool, params, pool_kind, src_pages, dst_pages, error_flag
                                                           stream))
 
 
+# The same calls by the width of the codes, the names they were first given;
+# programs written for those (perf/operators.py) keep working.
+kv4_page_scatter_kv, bind_kv4_page_scatter_kv = kvq_page_scatter_kv, bind_kvq_page_scatter_kv
+kv4_page_gather_kv, bind_kv4_page_gather_kv = kvq_page_gather_kv, bind_kvq_page_gather_kv
+kv4_page_copy, bind_kv4_page_copy = kvq_page_copy, bind_kvq_page_copy
+
+
 class StepTables:
     """The outputs of kv_step_tables (torch tensors on one GPU): the page
     lists, ranges and offsets that kv_page_scatter_kv and kv_page_gather take,
