@@ -94,9 +94,9 @@ def listed():
         _rope("rope_prompt", tokens=16384, rotary=64, interleaved=True, scaling="yarn", factor=4.0, span=16384),
         # A mixed step's cache writes into 4 bits, read back by a consumer of
         # dense tokens (ragged, small).
-        _write("kvq_write_mixed", sequences=64, length=(16, 256), chunks=4, chunk=(64, 512)),
+        _write("kv4_write_mixed", sequences=64, length=(16, 256), chunks=4, chunk=(64, 512)),
         # 32 prompt chunks written and read back: the copy-bound end.
-        _write("kvq_write_prompt", sequences=32, length=(1, 100), chunks=32, chunk=(512, 1024)),
+        _write("kv4_write_prompt", sequences=32, length=(1, 100), chunks=32, chunk=(512, 1024)),
         # A handful of agents on a short prompt: launches and latency.
         _attention("decode", "decode_tiny", requests=8, prefix=256, private=(16, 64), heads=(4, 4), dim=64, out="fp32"),
         # One layer of an 8B-shaped model: 64 workflows on a 2048-token prompt.
@@ -164,7 +164,7 @@ def draw(rng):
             if w["bytes"] <= top["decode_70b"]["bytes"] and w["flops"] * share <= top["prefill_chunked"]["flops"]:
                 return case
         else:
-            largest = {"tables": "tables_mixed", "rope": "rope_prompt", "write": "kvq_write_prompt"}[case["kind"]]
+            largest = {"tables": "tables_mixed", "rope": "rope_prompt", "write": "kv4_write_prompt"}[case["kind"]]
             if w["bytes"] <= top[largest]["bytes"]:
                 return case
 
@@ -445,9 +445,9 @@ def _prepare_own(case, x):
         p = state["params"] = _params(case, x["size"])
         shape = (sum(x["length"]) + sum(x["new"]), case["kv_heads"], case["head_dim"])
         state["out"] = [torch.empty(shape, dtype=DTYPES[case["dtype"]], device="cuda") for _ in range(2)]
-        state["calls"] = [halo.bind_kvq_page_scatter_kv(x["k"], x["v"], p, x["ids"], x["indptr"], x["start"],
+        state["calls"] = [halo.bind_kv4_page_scatter_kv(x["k"], x["v"], p, x["ids"], x["indptr"], x["start"],
                                                         x["count"], x["in_offset"], x["k_new"], x["v_new"]),
-                          halo.bind_kvq_page_gather_kv(x["k"], x["v"], p, x["ids"], x["indptr"], x["total"],
+                          halo.bind_kv4_page_gather_kv(x["k"], x["v"], p, x["ids"], x["indptr"], x["total"],
                                                        x["out_offset"], *state["out"])]
     else:
         page_indptr, page_ids = _csr(x["pages"])
