@@ -967,7 +967,8 @@ def bind_kv_step_tables(tables, seq_len, seq_new, block_table, free_pages, free_
                                                        error_flag, stream))
 
 
-def _bound(fn, args):
+def _bound(fn, args, keep=None):
+    # (keep: what lives as long as the callable)
     # the arguments in C form, for a function that converts none (a call of
     # halo_rope_qk 1.5 -> 0.8 us on the host)
     args = tuple(t(v) if v is None or isinstance(v, (int, float)) else v for t, v in zip(fn.argtypes, args))
@@ -978,6 +979,7 @@ def _bound(fn, args):
         st = fn(*args)
         if st != HALO_OK:
             _check(st)
+    call.keep = keep
     return call
 
 
@@ -1054,9 +1056,10 @@ def rope_qk(q, k, positions, rope, q_out=None, k_out=None, stream=None):
 
 
 def bind_rope_qk(q, k, positions, rope, q_out=None, k_out=None, stream=None):
-    """rope_qk as a zero-argument callable (see bind_kv_page_scatter)."""
+    """rope_qk as a zero-argument callable (see bind_kv_page_scatter), which
+    holds rope's angles."""
     load_library()
-    return _bound(_LIB.halo_rope_qk, _rope_args(q, k, positions, rope, q_out, k_out, stream))
+    return _bound(_LIB.halo_rope_qk, _rope_args(q, k, positions, rope, q_out, k_out, stream), rope.turns)
 
 
 class PrefixAttention:

@@ -2,9 +2,12 @@
 names that programs use, the status of a refusal."""
 
 import ast
+import gc
 import os
+import weakref
 
 import pytest
+import torch
 
 from paper_2509_02121_amd import halo
 
@@ -25,3 +28,27 @@ def test_operator_cases_call_what_there_is():
              if isinstance(n, ast.Attribute) and isinstance(n.value, ast.Name) and n.value.id == "halo"}
     assert len(names) > 5
     assert sorted(n for n in names if not hasattr(halo, n)) == []
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """The bound calls' arguments are taken from host tensors (nothing is
+    called)."""
+    halo.load_library()
+    monkeypatch.setattr(halo, "_gpu", lambda t, *a: t)
+    monkeypatch.setattr(halo, "_one_gpu", lambda *a: None)
+    monkeypatch.setattr(halo, "_rope_operand", lambda t, *a: (t.shape[1], t.stride(0)))
+    monkeypatch.setattr(halo, "_stream_handle", lambda s: None)
+
+
+def test_bound_rope_holds_its_angles(on_host):
+    """A Rope made in the call's expression lives as long as the callable."""
+    q, k, pos = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32)
+    ropes = [halo.Rope(64, device="cpu")]
+    turns = weakref.ref(ropes[0].turns)
+    call = halo.bind_rope_qk(q, k, pos, ropes.pop())
+    gc.collect()
+    assert turns() is not None
+    del call
+    gc.collect()
+    assert turns() is None
