@@ -961,10 +961,11 @@ def kv_step_tables(tables, seq_len, seq_new, block_table, free_pages, free_next,
 
 
 def bind_kv_step_tables(tables, seq_len, seq_new, block_table, free_pages, free_next, error_flag=None, stream=None):
-    """kv_step_tables as a zero-argument callable (see bind_kv_page_scatter)."""
+    """kv_step_tables as a zero-argument callable (see bind_kv_page_scatter),
+    which holds the arrays of `tables`."""
     load_library()
     return _bound(_LIB.halo_kv_step_tables, _step_args(tables, seq_len, seq_new, block_table, free_pages, free_next,
-                                                       error_flag, stream))
+                                                       error_flag, stream), list(vars(tables).values()))
 
 
 def _bound(fn, args, keep=None):

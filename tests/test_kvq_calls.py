@@ -52,3 +52,20 @@ def test_bound_rope_holds_its_angles(on_host):
     del call
     gc.collect()
     assert turns() is None
+
+
+def test_bound_step_tables_hold_their_arrays(on_host):
+    """So do the arrays of a StepTables of which the caller keeps only some:
+    the calls write all of them."""
+    def ints(*shape):
+        return torch.zeros(shape, dtype=torch.int32)
+    tabs = halo.StepTables(2, 4, 8, device="cpu")
+    arrays = [weakref.ref(t) for t in vars(tabs).values() if isinstance(t, torch.Tensor)]
+    assert len(arrays) == 9
+    call = halo.bind_kv_step_tables(tabs, ints(2), ints(2), ints(2, 4), ints(8), ints(1))
+    del tabs
+    gc.collect()
+    assert all(t() is not None for t in arrays)
+    del call
+    gc.collect()
+    assert all(t() is None for t in arrays)
