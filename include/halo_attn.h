@@ -366,7 +366,8 @@ halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t* params,
  * with two codes to a byte, the first one low, and the slots of a V tile as in a
  * v_pool. */
 
-/* Bytes of a 4-bit pool (-1 and an error message for unsupported params). Of
+/* Bytes of a 4-bit pool (-1, an error message and halo_last_error_status for
+ * params that are refused). Of
  * params num_kv_heads (up to 65536), head_dim, page_size, num_pool_pages (up to
  * 2^31 - 1) and kv_dtype are looked at. */
 int64_t halo_kvq_pool_bytes(const halo_attn_params_t* params, halo_pool_kind_t pool_kind);
@@ -636,6 +637,9 @@ halo_status_t halo_plan_inspect(const halo_plan_t* plan, const void** image,
 
 const char* halo_status_string(halo_status_t status);
 const char* halo_last_error_message(void);
+/* The status of the failure that the message describes (HALO_OK after a call
+ * that did not fail): for calls that return a size, thread-local like it. */
+halo_status_t halo_last_error_status(void);
 
 #ifdef __cplusplus
 }

@@ -241,6 +241,7 @@ namespace halo {
 halo_status_t fail(halo_status_t st, const std::string& msg);
 void clear_error();
 const char* last_error();
+halo_status_t last_status();
 // Whole-page copies inside a pool of pages of page_bytes (a multiple of 16).
 halo_status_t launch_page_copy(void* pool, const int32_t* src_pages, const int32_t* dst_pages, int32_t num_pages,
                                int64_t num_pool_pages, int64_t page_bytes, int32_t* error_flag, void* stream);

@@ -39,6 +39,7 @@ namespace halo {
 
 namespace {
 thread_local std::string g_last_error;
+thread_local halo_status_t g_last_status = HALO_OK;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -47,12 +48,17 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 halo_status_t fail(halo_status_t st, const std::string& msg) {
   g_last_error = msg;
+  g_last_status = st;
   return st;
 }
 
-void clear_error() { g_last_error.clear(); }
+void clear_error() {
+  g_last_error.clear();
+  g_last_status = HALO_OK;
+}
 
 const char* last_error() { return g_last_error.c_str(); }
+halo_status_t last_status() { return g_last_status; }
 
 }  // namespace halo
 
@@ -1429,6 +1435,7 @@ extern "C" const char* halo_status_string(halo_status_t s) {
 }
 
 extern "C" const char* halo_last_error_message(void) { return halo::last_error(); }
+extern "C" halo_status_t halo_last_error_status(void) { return halo::last_status(); }
 
 extern "C" halo_status_t halo_plan_update_lengths(halo_plan_t* plan, const halo_forest_t* forest) {
   clear_error();

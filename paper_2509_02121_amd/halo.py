@@ -91,7 +91,7 @@ EXPORTED_SYMBOLS = (
     "halo_kvq_pool_bytes", "halo_kvq_page_scatter_kv", "halo_kvq_page_gather_kv", "halo_kvq_page_copy",
     "halo_kv_step_tables", "halo_rope_params_default", "halo_rope_turns", "halo_rope_qk",
     "halo_prefix_tree_build", "halo_prefix_tree_get", "halo_prefix_tree_destroy",
-    "halo_status_string", "halo_last_error_message",
+    "halo_status_string", "halo_last_error_message", "halo_last_error_status",
 )
 
 
@@ -231,6 +231,8 @@ def load_library(require_gpu=False):
     lib.halo_status_string.restype = ctypes.c_char_p
     lib.halo_last_error_message.argtypes = []
     lib.halo_last_error_message.restype = ctypes.c_char_p
+    lib.halo_last_error_status.argtypes = []
+    lib.halo_last_error_status.restype = ctypes.c_int
     if require_gpu:
         runtimes = _hip_runtimes_mapped()
         if len(runtimes) > 1:
@@ -749,7 +751,7 @@ def kvq_pool_bytes(params, pool_kind):
     """Bytes of a 4-bit pool of params' pages (halo_kvq_pool_bytes)."""
     n = load_library().halo_kvq_pool_bytes(ctypes.byref(params), int(pool_kind))
     if n < 0:
-        raise HaloError(HALO_ERR_INVALID_ARGUMENT, _LIB.halo_last_error_message().decode())
+        _check(_LIB.halo_last_error_status())
     return n
 
 

@@ -69,3 +69,24 @@ def test_bound_step_tables_hold_their_arrays(on_host):
     del call
     gc.collect()
     assert all(t() is None for t in arrays)
+
+
+@pytest.mark.parametrize("bad,status", [({"head_dim": 96}, halo.HALO_ERR_UNSUPPORTED), ({"page_size": 32}, halo.HALO_ERR_UNSUPPORTED),
+                                        ({"kv_dtype": 7}, halo.HALO_ERR_UNSUPPORTED),
+                                        ({"num_kv_heads": 1 << 30}, halo.HALO_ERR_UNSUPPORTED),
+                                        ({"num_pool_pages": 1 << 60}, halo.HALO_ERR_UNSUPPORTED),
+                                        ({"num_kv_heads": 0}, halo.HALO_ERR_INVALID_ARGUMENT),
+                                        ({"num_pool_pages": -1}, halo.HALO_ERR_INVALID_ARGUMENT)])
+def test_pool_bytes_status(bad, status):
+    """A size that is refused has the status that the page calls give."""
+    lib = halo.load_library()
+    p = halo.make_params(8, 2, 64, torch.bfloat16, 10, 0.125)
+    for k, v in bad.items():
+        setattr(p, k, v)
+    for call in (lambda: halo.kvq_pool_bytes(p, halo.HALO_POOL_K), lambda: halo.alloc_kvq_pools(p, "cpu")):
+        with pytest.raises(halo.HaloError) as e:
+            call()
+        assert e.value.status == status
+    assert lib.halo_last_error_status() == status
+    assert halo.kvq_pool_bytes(halo.make_params(8, 2, 64, torch.bfloat16, 10, 0.125), halo.HALO_POOL_V) > 0
+    assert lib.halo_last_error_status() == halo.HALO_OK
