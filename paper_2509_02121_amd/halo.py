@@ -1223,26 +1223,27 @@ class PrefixAttention:
 
     @property
     def workspace(self):
-        """The workspace of this object's calls on the current stream (None if
-        the plan needs none)."""
+        """The workspace of this object's calls on the current stream, over
+        pools of either kind (None if the plan needs none)."""
         return self._workspace_on(None)
 
-    def _workspace_on(self, stream, kvq=False):
+    def _workspace_on(self, stream):
         """The workspace of a call on `stream` (None: the current stream): the
         stream's own, or, while it is being captured, a new one from the
-        graph's pool. kvq: of a call over 4-bit pools."""
+        graph's pool. It holds what calls over 4-bit pools need, which is
+        never less than others (4 bytes a partial row of a bf16 output)."""
         import torch
-        if not self.plan.workspace_bytes:
+        if not self.plan.kvq_workspace_bytes:
             return None
         if stream is None:
-            return self._current_workspace(torch.cuda.current_stream(self.device), kvq)
+            return self._current_workspace(torch.cuda.current_stream(self.device))
         with torch.cuda.stream(stream):
-            return self._current_workspace(stream, kvq)
+            return self._current_workspace(stream)
 
-    def _current_workspace(self, s, kvq=False):
+    def _current_workspace(self, s):
         """_workspace_on(s) for the current stream s."""
         import torch
-        n = self.plan.kvq_workspace_bytes if kvq else self.plan.workspace_bytes
+        n = self.plan.kvq_workspace_bytes
         if not n:
             return None
         if torch.cuda.is_current_stream_capturing():
@@ -1277,9 +1278,9 @@ class PrefixAttention:
         fn = getattr(_LIB, ("halo_prefix_attn_prefill" if self.plan.is_prefill else "halo_prefix_attn_decode") +
                      ("_kvq" if kvq else ""))
         capturing = torch.cuda.is_current_stream_capturing
-        n = self.plan.kvq_workspace_bytes if kvq else self.plan.workspace_bytes
+        n = self.plan.kvq_workspace_bytes
         # (bound during a capture: the graph's memory is not for eager calls)
-        ws = None if capturing() else self._workspace_on(stream, kvq)
+        ws = None if capturing() else self._workspace_on(stream)
         _check_run(self.plan, self.meta, q, k_pool, v_pool, o, lse, ws, library_workspace=ws is None, kvq=kvq)
         s = self._before_run(stream)
         self._bound[self._cur].add(s)
@@ -1329,7 +1330,7 @@ class PrefixAttention:
         else:
             fn = prefix_attn_prefill if self.plan.is_prefill else prefix_attn_decode
         s = self._before_run(stream)
-        ws = self._current_workspace(s, kvq) if stream is None else self._workspace_on(s, kvq)
+        ws = self._current_workspace(s) if stream is None else self._workspace_on(s)
         with self._enqueue:
             fn(self.plan, self.meta, q, k_pool, v_pool, o, lse, ws, s)
         self._after_run(s)
