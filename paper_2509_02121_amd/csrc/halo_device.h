@@ -192,11 +192,30 @@ __device__ __forceinline__ void store4(__bf16* dst, f32x4_t v) {
 __device__ __forceinline__ void store4_part(__bf16* dst, f32x4_t v) { store4(dst, v); }
 
 // Partial results over 4-bit pools with a bf16 output: as long as bf16 ones, but in
-// fp16 with a power of two for each row, the largest element's, so that each is off
+// fp16 with a power of two for each row, the largest finite element's (an infinity
+// stays one in fp16, and leaves the row's other dims as they are), so that each is off
 // by at most 2^-11 of itself (or 2^-25 of the row's largest) where bf16 is by 2^-8:
 // rows of three or more partials were otherwise further off than the output's
 // rounding (70B-shaped decode: 0.0027 of the row, 0.0022 so; 64 requests on 2048 keys
 // 0.0024 and 0.0018). The scale stands beside the row's LSE, one load for both.
+template <typename V, int N>
+__device__ __forceinline__ float largest_finite(const V (&acc)[N]) {
+  constexpr int kPer = sizeof(V) / 4;
+  const float inf = -kNegInf;
+  float top = 0.f;
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) top = fmaxf(top, fabsf(acc[b][j]));
+  if (__any(top == inf)) {
+    top = 0.f;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) top = fmaxf(top, fabsf(acc[b][j]) == inf ? 0.f : fabsf(acc[b][j]));
+  }
+  return top;
+}
 __device__ __forceinline__ float row_scale(float top) {
   const uint32_t e = min(__float_as_uint(top) & 0x7f800000u, 0x7e800000u);
   return __uint_as_float(e ? e : 0x3f800000u);
@@ -351,12 +370,7 @@ __device__ __forceinline__ void finish_item(const AttnArgs& a, const Item& it, c
       for (int b = 0; b < NB; ++b) store4(dst + 16 * b, acc[b] * inv);
       if (grp == 0) reinterpret_cast<int*>(a.part_lse)[prow] = part_lse_bits(lse2, lsum);
     } else if constexpr (HALF) {
-      float top = 0.f;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) top = fmaxf(top, fabsf(acc[b][j]));
-      const float scale = row_scale(rows_max(top) * inv), x = inv * reciprocal_of_scale(scale);
+      const float scale = row_scale(rows_max(largest_finite(acc)) * inv), x = inv * reciprocal_of_scale(scale);
       if (has_row) {
         const int64_t prow = row.slot;
         uint16_t* dst = static_cast<uint16_t*>(a.part_o) + prow * D + 4 * grp;
@@ -992,13 +1006,7 @@ __device__ __forceinline__ void wide_item(const AttnArgs& a, int item_id, uint8_
   const float l = halves_sum(lsum);
   constexpr bool kHalf = KVQ && sizeof(TO) == 2;   // partial results by store_half
   float top = 0.f;
-  if constexpr (kHalf) {
-#pragma unroll
-    for (int b = 0; b < NO; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(acc[b][i]));
-    top = halves_max(top);
-  }
+  if constexpr (kHalf) top = halves_max(largest_finite(acc));
   if (computes && r < it.n_rows) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
     const float lse2 = l > 0.f ? m + __log2f(l) : kNegInf;
