@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import oracle
-from kvq_helpers import assert_close, expected, fill_pools, run, values
+from kvq_helpers import assert_close, check, expected, fill_pools, run, values
 from paper_2509_02121_amd import halo
 from workloads import build_workload
 
@@ -118,3 +118,56 @@ def test_nan_in_cut_keys(gpu_lib, cut, D, kind):
     assert np.isnan(o[sees]).all()
     assert np.array_equal(o[~sees], clean[~sees]) and np.array_equal(lse[~sees], lse0[~sees])
     assert np.array_equal(lse[sees], lse0[sees]) if kind else np.isneginf(lse[sees]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_gather_at_the_ends_of_the_range(gpu_lib, D, dtype):
+    """All codes at the smallest and largest scales read back exactly:
+    subnormals (2^-127 is one in either type) stay, 2^128 and more are
+    infinities."""
+    exps = [1, 2, 253, 254]
+    rng = np.random.default_rng(D)
+    pools, want = [], []
+    for kind in (0, 1):
+        tile = rng.integers(0, 256, (1, 1, oracle.paged_kvq.tile_bytes(kind, D)), dtype=np.uint8)
+        if kind == halo.HALO_POOL_K:
+            tile[0, 0, D * 8:] = np.resize(exps, D // 2)
+        else:
+            tile[0, 0, D * 8:] = (np.resize(exps, 16).astype(np.uint16) << 7).view(np.uint8)
+        pools.append(torch.from_numpy(tile).cuda())
+        x = np.stack([oracle.paged_kvq.read_token(tile[0, 0], kind, D, t) for t in range(16)])
+        want.append(np.where(np.abs(x) >= 2.0 ** 128, np.copysign(np.inf, x), x))
+        assert np.isinf(want[-1]).any() and (np.abs(want[-1]) == 2.0 ** -127).any()
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    outs = [torch.full((16, 1, D), 3.0, dtype=dtype, device="cuda") for _ in range(2)]
+    params = halo.make_params(1, 1, D, dtype, 1, 0.125)
+    halo.kvq_page_gather_kv(*pools, params, one, torch.tensor([0, 1], dtype=torch.int32, device="cuda"), one + 16,
+                            one.long(), *outs)
+    for got, x in zip(outs, want):
+        assert np.array_equal(got.double().cpu().numpy()[:, 0], x)
+
+
+@pytest.mark.parametrize("out", [BF16, FP32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_narrow(gpu_lib, D, out):
+    """bf16 chunks as narrow items."""
+    q_len = [257, 40, 100, 1]
+    w = _w([300, 70] + q_len, [[0, 2], [1, 3], [4], [0, 5]], q_len, heads=(4, 1), D=D)
+    att, _ = check(w, out, {"wide": 0}, f"narrow prefill d{D}")
+    assert att.plan.stats()["num_wide_items"] == 0
+
+
+@pytest.mark.parametrize("prefill", [False, True])
+def test_calls_repeat_themselves(gpu_lib, prefill):
+    """Two calls give the same bits (no result depends on an order of
+    workgroups), with other work between them."""
+    q_len = [200, 33] if prefill else None
+    w = _w([1500, 300, 900] + (q_len or []), [[0, 1, 3], [0, 2, 4]] if prefill else [[0, 1], [0, 2]] * 20, q_len,
+           heads=(16, 2))
+    pools = fill_pools(w)
+    o, lse, att = run(w, pools, BF16)
+    for _ in range(5):
+        torch.randn(1 << 22, device="cuda").sum()
+        o2, lse2 = att.run(w.q, *pools)
+        assert np.array_equal(o2.double().cpu().numpy(), o) and np.array_equal(lse2.double().cpu().numpy(), lse)
