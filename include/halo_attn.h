@@ -406,7 +406,7 @@ size_t halo_plan_kvq_workspace_bytes(const halo_plan_t* plan);
 /* halo_prefix_attn_decode and halo_prefix_attn_prefill over 4-bit pools, with the
  * same plans, metadata and errors, and a workspace of halo_plan_kvq_workspace_bytes
  * (prefill: as there, none runs the items uncut): k_pool and v_pool hold
- * halo_kvq_pool_bytes each, kv_dtype is the type of q. The result is that of
+ * halo_kvq_pool_bytes each (a plan whose params that refuses is refused here too), kv_dtype is the type of q. The result is that of
  * attention over the values the pools stand for, in fp32 for an fp32 output (4-bit
  * values are exact in bf16, so fp32 queries, and softmax weights for an fp32
  * output, are multiplied in three bf16 parts); for a bf16 output the weights are

@@ -830,6 +830,8 @@ halo_status_t run_attention(const halo_plan_t* plan, bool want_prefill, bool kvq
   if (!aligned16(q) || !aligned16(k_pool) || !aligned16(v_pool) || !aligned16(o) ||
       (reinterpret_cast<uintptr_t>(device_meta) & 255) != 0)
     return fail(HALO_ERR_INVALID_ARGUMENT, "q, k_pool, v_pool, o must be 16-byte aligned, device_meta 256-byte");
+  // (the kernels over 4-bit pools step by 32-bit page sizes)
+  if (kvq && halo_kvq_pool_bytes(&plan->params, HALO_POOL_K) < 0) return last_status();
   // a prefill without the workspace of its pieces runs its items uncut
   const bool whole = plan->prefill && plan->n_merge_items > 0 &&
                      (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 ||

@@ -6,6 +6,7 @@ import gc
 import os
 import weakref
 
+import numpy as np
 import pytest
 import torch
 
@@ -90,3 +91,22 @@ def test_pool_bytes_status(bad, status):
     assert lib.halo_last_error_status() == status
     assert halo.kvq_pool_bytes(halo.make_params(8, 2, 64, torch.bfloat16, 10, 0.125), halo.HALO_POOL_V) > 0
     assert lib.halo_last_error_status() == halo.HALO_OK
+
+
+@pytest.mark.parametrize("prefill", [False, True])
+def test_attention_over_pools_that_are_not_built(prefill):
+    """A plan of more heads than a 4-bit pool has: the kernels' page offsets
+    would pass 32 bits for some of them, so the call refuses it, like
+    halo_kvq_pool_bytes."""
+    lib = halo.load_library()
+    n = 65537
+    csr = {"seg_len": np.array([1], np.int32), "seg_page_indptr": np.array([0, 1], np.int32),
+           "seg_page_ids": np.array([0], np.int32), "req_seg_indptr": np.array([0, 1], np.int32),
+           "req_seg_ids": np.array([0], np.int32), "q_len": np.array([1], np.int32) if prefill else None}
+    plan = halo.Plan.from_csr(halo.make_params(n, n, 64, torch.bfloat16, 1, 0.125), csr)
+    assert plan.is_prefill == prefill
+    fn = lib.halo_prefix_attn_prefill_kvq if prefill else lib.halo_prefix_attn_decode_kvq
+    keep = np.zeros(128, np.int64)
+    at = (keep.ctypes.data + 255) // 256 * 256
+    assert fn(plan._handle, at, at, at, at, at, at, at, 1 << 40, None) == halo.HALO_ERR_UNSUPPORTED
+    assert b"65536" in lib.halo_last_error_message()
