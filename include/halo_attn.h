@@ -367,9 +367,8 @@ halo_status_t halo_kv_page_copy(void* pool, const halo_attn_params_t* params,
  * v_pool. */
 
 /* Bytes of a 4-bit pool (-1, an error message and halo_last_error_status for
- * params that are refused). Of
- * params num_kv_heads (up to 65536), head_dim, page_size, num_pool_pages (up to
- * 2^31 - 1) and kv_dtype are looked at. */
+ * params that are refused). Of params num_kv_heads (up to 65536), head_dim,
+ * page_size, num_pool_pages (up to 2^31 - 1) and kv_dtype are looked at. */
 int64_t halo_kvq_pool_bytes(const halo_attn_params_t* params, halo_pool_kind_t pool_kind);
 
 /* halo_kv_page_scatter_kv into 4-bit pools: the tokens (of kv_dtype) are
@@ -406,11 +405,16 @@ size_t halo_plan_kvq_workspace_bytes(const halo_plan_t* plan);
 /* halo_prefix_attn_decode and halo_prefix_attn_prefill over 4-bit pools, with the
  * same plans, metadata and errors, and a workspace of halo_plan_kvq_workspace_bytes
  * (prefill: as there, none runs the items uncut): k_pool and v_pool hold
- * halo_kvq_pool_bytes each (a plan whose params that refuses is refused here too), kv_dtype is the type of q. The result is that of
- * attention over the values the pools stand for, in fp32 for an fp32 output (4-bit
- * values are exact in bf16, so fp32 queries, and softmax weights for an fp32
- * output, are multiplied in three bf16 parts); for a bf16 output the weights are
- * rounded to bf16. Slots past a segment's length may hold any bytes. */
+ * halo_kvq_pool_bytes each (a plan whose params that refuses is refused here
+ * too), kv_dtype is the type of q. The result is that of attention over the
+ * values the pools stand for, in fp32 for an fp32 output (4-bit values are exact
+ * in bf16, so fp32 queries, and softmax weights for an fp32 output, are
+ * multiplied in three bf16 parts). For a bf16 output the weights are rounded to
+ * bf16, and the parts of a row whose keys a decode plan cuts are held in fp16
+ * times a power of two each (off by 2^-11 of an element, or 2^-25 of the largest
+ * finite one). A value of 2^128 is an infinity or, where its weight keeps the
+ * product in fp32's range, 2^128. Slots past a segment's length may hold any
+ * bytes. */
 halo_status_t halo_prefix_attn_decode_kvq(const halo_plan_t* plan, const void* device_meta,
                                           const void* q, const void* k_pool, const void* v_pool,
                                           void* o, float* lse,
@@ -436,7 +440,8 @@ halo_status_t halo_prefix_attn_prefill_kvq(const halo_plan_t* plan, const void* 
  *   seq_start, seq_count, seq_end [num_seqs]: seq_len, seq_new and their sum;
  *   in_token_offset [num_seqs] int64: tokens of the sequences before;
  *   positions [max_tokens] int32, slots [max_tokens] int64: of each new token,
- *     its place in its sequence, and page * page_size + place in the page (-1
+ *     its place in its sequence (in the pages of its own row: behind a shared
+ *     prefix the caller adds the prefix's length for halo_rope_qk), and page * page_size + place in the page (-1
  *     for a negative page id); behind the last token 0 and -1, as for the
  *     padding of a captured step. Either may be NULL;
  *   free_next [1]: the first page that is still free.
@@ -514,7 +519,7 @@ void halo_rope_params_default(halo_rope_params_t* rope, int32_t head_dim);
 
 /* The angles of one position (host only): turns[i], i < rotary_dim / 2, is
  * w_i / (2 pi) with 64 bits after the point, which halo_rope_qk multiplies by the
- * position exactly. Made once and copied to the GPU by the caller. */
+ * position; of a turn's fraction it uses 32 bits. Made once and copied to the GPU by the caller. */
 halo_status_t halo_rope_turns(const halo_rope_params_t* rope, uint64_t* turns, float* amplitude);
 
 /* Turn the queries and keys of num_tokens tokens by their positions, in one

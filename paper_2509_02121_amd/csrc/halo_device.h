@@ -1,5 +1,5 @@
 // Device code that the attention kernels over bf16 / fp32 pools
-// (halo_kernels.hip) and over 4-bit ones (halo_kv4_attn.hip) share: fragments
+// (halo_kernels.hip) and over 4-bit ones (halo_kvq_attn.hip) share: fragments
 // and MFMA wrappers, reductions inside a wave, spans and steps, and the wide
 // items.
 #pragma once
@@ -447,7 +447,7 @@ template <int D, int S> constexpr int wide_ring_bytes() { return S * (D / 16 + 2
 // converted once for the workgroup's rows. K is one conversion per two values. V
 // scales run along the keys of a dim: see kvq_decode_keys. (On the softmax's weights
 // instead, 16 products and 4 LDS reads a step for every wave, they took registers
-// that had to be spilled: chunked prefill 1765 us, at the conversion 1290.) Only in a
+// that had to be spilled inside the loop: chunked prefill 1765 us, at the conversion 1290.) Only in a
 // step with masked keys, whose scales may be NaN, are they put on the weights, with
 // the masked ones at 0. The conversion has no branch and runs between the MFMAs of
 // the step before: with a K or a V tile to a wave, ahead of them, it cost 280 of

@@ -6,9 +6,10 @@
 //   V = v_scale * v_code, codes E2M1 and scales powers of two.
 //
 // A K code times its scale is exact in bf16 and takes one conversion per two
-// values. A V scale belongs to a key, i.e. runs along the contraction of P V, so
-// it is multiplied onto P (exactly) after the sum of P is taken, and V codes are
-// converted with scale 1.
+// values. A V scale belongs to a key, i.e. runs along the contraction of P V.
+// Narrow items multiply it onto P (exactly) after the sum of P is taken, and
+// convert V codes with scale 1; wide items put it into V at the conversion, but in
+// steps with masked keys onto P too.
 //
 // Narrow items convert in registers, between the loads and the MFMAs; wide items
 // once per workgroup, on the way into LDS (wide_item). Per step of 32 keys and
@@ -19,17 +20,23 @@
 // What bounds them (d 128, bf16): narrow items over private keys read at the rate of
 // the memory (1024 requests of 256-2048 keys, 1.24 GB: 252 us, 4.9 TB/s), those over
 // shared keys wait for their instructions (VALU 926 cycles a step and SIMD); wide
-// items for products and VALU instructions together, which take 95% of the cycles
-// (32 chunks of 512 tokens on 4096 keys 1190 us, 0.98 PFLOP/s, 8 prefixes of 8192
-// under 1024 requests 300 us). A launch of both kinds takes nearly the sum of the two
-// (70B-shaped decode 492 us); small calls are chains of dependent loads in two
-// launches (8 requests of 300 keys 6.8 us).
+// items for products (busy 42% of the cycles) and VALU instructions (54%), which
+// overlap little (32 chunks of 512 tokens on 4096 keys 1184-1257 us by the card, 0.93
+// to 0.99 PFLOP/s, 8 prefixes of 8192 under 1024 requests 300 us). A launch of both
+// kinds takes nearly the sum of the two (70B-shaped decode 492-518 us); small calls
+// are chains of dependent loads in two launches (8 requests of 300 keys 6.8-7.6 us).
 //
 // fp32 queries and outputs: K and V are exact in bf16, so products with fp32
 // accuracy need only q (fp32 queries) and P (fp32 outputs) split into three bf16
 // parts each (8 + 8 + 8 bits): three MFMAs of 16x16x32 in place of eight 16x16x4
 // fp32 ones (4 requests of 12000-24000 keys 32 us: 16 steps in a chain, of 0.9 us
-// alone on a SIMD and 1.4 where two share it).
+// alone on a SIMD and 1.4 where two share it). With bf16 queries and fp32 outputs P V
+// is three products for one: 32 chunks of 512 tokens on 4096 keys 2080 us, 70B-shaped
+// decode 753.
+//
+// Registers: at d 128 the wide kernels use all 256. With bf16 outputs 7 (8 in a launch
+// of both kinds) are stored to scratch before the loop and loaded after it, none
+// inside; with fp32 outputs 14 (9), of which 4 (1) are loaded again in each step.
 
 #include <hip/hip_runtime.h>
 

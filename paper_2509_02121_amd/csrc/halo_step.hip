@@ -220,8 +220,9 @@ __device__ __forceinline__ u32x4_t pack(const float (&v)[8]) {
 // every slots-th head.
 //
 // The angle in turns, position * f mod 1, is a product of integers: f is held
-// as 64 bits after the point, so it is exact to 2^-33 of a turn at any
-// position, where a product in fp32 is off by whole radians at 10^6.
+// as 64 bits after the point, and the product is cut to 32, so that it is less than
+// 2^-32 of a turn (1.5e-9 rad) short, and off by f's rounding (up to 2^-34 at
+// position 2^31), where a product in fp32 is off by whole radians at 10^6.
 // Products and sums in fp32, rounded once to the output's type. Bound by HBM:
 // q and k read and written once (16384 tokens of 32 + 8 heads, d 128, bf16: 336 MB
 // in 67.7 us, 4.96 TB/s, where a device copy reaches 5.17).
