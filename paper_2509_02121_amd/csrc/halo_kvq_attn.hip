@@ -21,7 +21,7 @@
 // the memory (1024 requests of 256-2048 keys, 1.24 GB: 252 us, 4.9 TB/s), those over
 // shared keys wait for their instructions (VALU 926 cycles a step and SIMD); wide
 // items for products (busy 42% of the cycles) and VALU instructions (54%), which
-// overlap little (32 chunks of 512 tokens on 4096 keys 1184-1257 us by the card, 0.93
+// overlap little (32 chunks of 512 tokens on 4096 keys 1175-1257 us by the card, 0.93
 // to 0.99 PFLOP/s, 8 prefixes of 8192 under 1024 requests 300 us). A launch of both
 // kinds takes nearly the sum of the two (70B-shaped decode 492-518 us); small calls
 // are chains of dependent loads in two launches (8 requests of 300 keys 6.8-7.6 us).
@@ -31,8 +31,8 @@
 // parts each (8 + 8 + 8 bits): three MFMAs of 16x16x32 in place of eight 16x16x4
 // fp32 ones (4 requests of 12000-24000 keys 32 us: 16 steps in a chain, of 0.9 us
 // alone on a SIMD and 1.4 where two share it). With bf16 queries and fp32 outputs P V
-// is three products for one: 32 chunks of 512 tokens on 4096 keys 2080 us, 70B-shaped
-// decode 753.
+// is three products for one: 32 chunks of 512 tokens on 4096 keys 2061-2080
+// us, 70B-shaped decode 740-753.
 //
 // Registers: at d 128 the wide kernels use all 256. With bf16 outputs 7 (8 in a launch
 // of both kinds) are stored to scratch before the loop and loaded after it, none
