@@ -881,8 +881,9 @@ kv4_page_copy, bind_kv4_page_copy = kvq_page_copy, bind_kvq_page_copy
 class StepTables:
     """The outputs of kv_step_tables (torch tensors on one GPU): the page
     lists, ranges and offsets that kv_page_scatter_kv and kv_page_gather take,
-    positions and slots of up to max_tokens new tokens, page lists of up to
-    max_pages pages. seq_end is the next step's seq_len and free_next its
+    positions (in the sequence's own pages: behind a shared prefix its length
+    is to be added for rope_qk) and slots of up to max_tokens new tokens, page
+    lists of up to max_pages pages. seq_end is the next step's seq_len and free_next its
     free_next (copy them there: a call's outputs must not be its inputs)."""
 
     def __init__(self, num_seqs, max_tokens, max_pages, device="cuda"):
