@@ -1288,6 +1288,7 @@ class PrefixAttention:
         tensors = (self.plan._handle, self.meta.data_ptr(), q.data_ptr(), k_pool.data_ptr(),
                    v_pool.data_ptr(), o.data_ptr(), lse.data_ptr() if lse is not None else None)
         handle = _stream_handle(s)
+        keep = (self.plan, self.meta)   # (live as long as the callable, whatever becomes of this object)
         enqueue = self._enqueue
         if not n:
             args = (*tensors, None, 0, handle)
@@ -1296,6 +1297,7 @@ class PrefixAttention:
                 st = fn(*args)
                 if st != HALO_OK:
                     _check(st)
+            call.keep = keep
             return call
 
         def new_workspace():
@@ -1319,6 +1321,7 @@ class PrefixAttention:
                 st = fn(*args)
             if st != HALO_OK:
                 _check(st)
+        call.keep = keep
         return call
 
     def run(self, q, k_pool, v_pool, o=None, lse=None, stream=None):

@@ -1,6 +1,9 @@
 """GPU checks of calls over 4-bit pools that stand beside each other: the
 workspace, values at the ends of the range, cuts that must not show."""
 
+import gc
+import weakref
+
 import numpy as np
 import pytest
 import torch
@@ -171,3 +174,25 @@ def test_calls_repeat_themselves(gpu_lib, prefill):
         torch.randn(1 << 22, device="cuda").sum()
         o2, lse2 = att.run(w.q, *pools)
         assert np.array_equal(o2.double().cpu().numpy(), o) and np.array_equal(lse2.double().cpu().numpy(), lse)
+
+
+@pytest.mark.parametrize("seg_len", [[20], [600, 33]])
+def test_bound_call_holds_its_plan(gpu_lib, seg_len):
+    """bind() of an object that is dropped: the plan and its metadata live as
+    long as the callable, with a workspace and without one."""
+    w = _w(seg_len, [[*range(len(seg_len))]])
+    pools = fill_pools(w)
+    o, lse, att = run(w, pools, FP32)
+    assert bool(att.plan.workspace_bytes) == (len(seg_len) > 1)
+    out = att.alloc_outputs(w.q)
+    call = att.bind(w.q, *pools, *out)
+    held = [weakref.ref(att.plan), weakref.ref(att.meta)]
+    del att
+    gc.collect()
+    assert all(x() is not None for x in held)
+    call()
+    torch.cuda.synchronize()
+    assert np.array_equal(out[0].double().cpu().numpy(), o) and np.array_equal(out[1].double().cpu().numpy(), lse)
+    del call
+    gc.collect()
+    assert all(x() is None for x in held)
