@@ -538,6 +538,209 @@ halo_status_t halo_rope_qk(const halo_rope_params_t* rope, float amplitude, cons
                            void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
                            void* stream);
 
+/* What stays in the cache between steps: attention weights and eviction. */
+
+typedef struct {
+  int32_t num_seqs;
+  int32_t num_rows;      /* tokens of q and lse */
+  int32_t num_entries;   /* elements of rows and row_end */
+  int32_t width;         /* tokens of a row of the weights */
+} halo_weight_sizes_t;
+
+/* The attention weight that cached tokens got from the queries of a step, added
+ * to what they had. weights and weights_out are [num_seqs][num_kv_heads][width]
+ * float32; for t < seq_end[i]
+ *   weights_out[i][h][t] = (t < seq_start[i] ? decay * weights[i][h][t] : 0) +
+ *     sum over entries e of sequence i with t < row_end[e] and q heads g of kv head h
+ *       exp(sm_scale * <q[rows[e]][g], k_t> - lse[rows[e]][g])
+ * and elements from seq_end[i] on are left as they were. lse is what the attention
+ * calls give; a row with lse = -inf (it saw no key) adds nothing. Sequence i is a
+ * page list as in halo_kv_page_gather (at least ceil(seq_end[i] / page_size)
+ * pages): a request's own pages, or a prefix with the rows of every request that
+ * shares it. Its entries are row_indptr[i] .. row_indptr[i + 1] - 1; rows[e] is a
+ * token of q and lse ([num_rows][num_q_heads][head_dim] of kv_dtype and
+ * [num_rows][num_q_heads]) and row_end[e] how many of the sequence's tokens it
+ * sees. rows NULL: entry e is token e. row_end NULL: an entry sees seq_end[i].
+ * row_indptr NULL: sequence i has one entry, i (a decode step). seq_start NULL:
+ * no token is new. weights may be weights_out, or NULL where decay is 0; then what
+ * was there is not read.
+ * All pointers but params and sizes are DEVICE pointers; of params all but
+ * out_dtype is used; k_pool, q 16-byte aligned; decay >= 0. Scores, exponentials and sums are
+ * in fp32 (fp32 queries: products as exact as in fp32). Sums have one order,
+ * whatever runs beside the call. A sequence whose seq_end is
+ * negative, past width or past its pages is skipped whole, a page whose id is
+ * outside [0, num_pool_pages) and an entry whose row is outside [0, num_rows) by
+ * itself, and one whose entries are no range of [0, num_entries) has none; 1 is then
+ * written to error_flag (may be NULL; 0 never is). */
+halo_status_t halo_kv_page_weights(const void* k_pool, const halo_attn_params_t* params,
+                                   const halo_weight_sizes_t* sizes,
+                                   const int32_t* page_ids, const int32_t* seq_page_indptr,
+                                   const int32_t* seq_start, const int32_t* seq_end,
+                                   const int32_t* row_indptr, const int32_t* rows, const int32_t* row_end,
+                                   const void* q, const float* lse, float decay,
+                                   const float* weights, float* weights_out, int32_t* error_flag, void* stream);
+
+/* halo_kv_page_weights over a 4-bit K pool (kv_dtype: the type of q). */
+halo_status_t halo_kvq_page_weights(const void* k_pool, const halo_attn_params_t* params,
+                                    const halo_weight_sizes_t* sizes,
+                                    const int32_t* page_ids, const int32_t* seq_page_indptr,
+                                    const int32_t* seq_start, const int32_t* seq_end,
+                                    const int32_t* row_indptr, const int32_t* rows, const int32_t* row_end,
+                                    const void* q, const float* lse, float decay,
+                                    const float* weights, float* weights_out, int32_t* error_flag, void* stream);
+
+typedef struct {
+  int32_t num_seqs;
+  int32_t num_kv_heads;
+  int32_t width;      /* tokens of a row of the weights */
+  int32_t budget;     /* tokens that an evicted sequence keeps, >= 1 */
+  int32_t trigger;    /* longer sequences are evicted (>= budget) */
+  int32_t sinks;      /* the first tokens, always kept */
+  int32_t recent;     /* the last tokens, always kept (sinks + recent <= budget) */
+} halo_evict_sizes_t;
+
+/* Which tokens stay. Of a sequence with seq_len[i] > trigger each head keeps
+ * budget tokens: the first `sinks`, the last `recent` and, of those between, the
+ * ones of the largest weights (equal weights: the earlier token; a NaN counts as
+ * less than any number, -0 as 0). kept[i][h] [budget] lists them in order, and
+ * weights_out[i][h][j] = weights[i][h][kept[i][h][j]]; new_len[i] = budget. Any
+ * other sequence stays whole: new_len[i] = seq_len[i], weights_out its weights, kept
+ * as it was. Elements of weights_out from new_len[i] on are left as they were,
+ * unless it is weights, where they may hold anything. All arrays are DEVICE
+ * arrays, weights, weights_out [num_seqs][num_kv_heads][width], kept
+ * [num_seqs][num_kv_heads][budget]. weights_out may be weights; no other output
+ * may overlap an array. A sequence with a negative length or one past width is
+ * left alone (new_len[i] = seq_len[i]) and 1 written to error_flag (may be NULL). */
+halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, const float* weights, const int32_t* seq_len,
+                                   int32_t* kept, float* weights_out, int32_t* new_len, int32_t* error_flag,
+                                   void* stream);
+
+/* The kept tokens' keys and values to the front: for a sequence with new_len[i] <
+ * seq_len[i], token j of head h of the page list dst becomes token kept[i][h][j]
+ * of the page list src, j < new_len[i]; any other sequence is copied whole (in
+ * place: left alone). kept is [num_seqs][num_kv_heads][kept_width], ascending in a
+ * row, bits are copied unchanged. dst_page_ids == page_ids with dst_page_indptr ==
+ * seq_page_indptr moves in place; otherwise no page of dst may be a page of src or
+ * listed twice (beams that share pages are evicted to pages of their own). A page
+ * list holds at least the pages of its tokens; slots past new_len[i] keep what
+ * they hold. All pointers but params are DEVICE pointers, pools 16-byte aligned.
+ * A sequence whose lengths do not fit its pages or each other (new_len[i] > kept_width where
+ * it is less than seq_len[i]) is skipped whole, a token whose kept index is outside [0,
+ * seq_len[i]) or a page of which is outside [0, num_pool_pages) by itself; 1 is then
+ * written to error_flag (may be NULL). */
+halo_status_t halo_kv_page_keep_kv(void* k_pool, void* v_pool, const halo_attn_params_t* params,
+                                   const int32_t* page_ids, const int32_t* seq_page_indptr,
+                                   const int32_t* seq_len, const int32_t* new_len,
+                                   const int32_t* kept, int32_t kept_width,
+                                   const int32_t* dst_page_ids, const int32_t* dst_page_indptr,
+                                   int32_t num_seqs, int32_t* error_flag, void* stream);
+
+/* halo_kv_page_keep_kv in 4-bit pools: codes and scales are moved. */
+halo_status_t halo_kvq_page_keep_kv(void* k_pool, void* v_pool, const halo_attn_params_t* params,
+                                    const int32_t* page_ids, const int32_t* seq_page_indptr,
+                                    const int32_t* seq_len, const int32_t* new_len,
+                                    const int32_t* kept, int32_t kept_width,
+                                    const int32_t* dst_page_ids, const int32_t* dst_page_indptr,
+                                    int32_t num_seqs, int32_t* error_flag, void* stream);
+
+/* Pages back on the free list, the inverse of halo_kv_step_tables: of row i of
+ * block_table the pages past ceil(new_len[i] / 16), up to ceil(seq_len[i] / 16). They
+ * are entered in front of what is still free, in the order of the sequences and of
+ * their pages: with n of them, free_pages_out[free_next - n .. free_next), and
+ * free_next_out = free_next - n. free_pages_out may be free_pages; otherwise
+ * free_pages[free_next .. num_free) is copied to it too, and the rest of it left as
+ * it was. sizes as for halo_kv_step_tables (max_tokens and max_pages are not looked
+ * at). DEVICE arrays; block_table is only read. A sequence with lengths that are
+ * negative, grow or do not fit its row releases nothing; a call that does not fit
+ * (free_next outside [0, num_free], or n > free_next) releases nothing at all
+ * (free_next_out = free_next). Either way 1 is written to error_flag (may be NULL).
+ * No array that is written may overlap another one, but free_pages_out free_pages. */
+halo_status_t halo_kv_release_pages(const halo_step_sizes_t* sizes, const int32_t* block_table,
+                                    const int32_t* seq_len, const int32_t* new_len,
+                                    const int32_t* free_pages, const int32_t* free_next,
+                                    int32_t* free_pages_out, int32_t* free_next_out,
+                                    int32_t* error_flag, void* stream);
+
+/* Beam search. A request (item) has num_beams beams; beam w of item i is row
+ * i * num_beams + w of the logits, of the scores and of the page table. */
+
+typedef struct {
+  int32_t num_items;
+  int32_t num_beams;       /* 1 .. 64 */
+  int32_t vocab;           /* 1 .. 2^24 */
+  int32_t num_best;        /* candidates per item, 1 .. 64 */
+  int64_t logits_stride;   /* elements from a row of the logits to the next, >= vocab */
+  halo_dtype_t dtype;      /* of the logits */
+} halo_beam_sizes_t;
+
+/* The workspace (bytes) of halo_beam_select; -1 and an error for sizes that are
+ * refused. */
+int64_t halo_beam_workspace_bytes(const halo_beam_sizes_t* sizes);
+
+/* The best num_best candidates (beam w, token v) of each item by
+ *   scores[w] + logits[w][v] - ln sum_u exp(logits[w][u]),
+ * best first (ties: the lower beam, then the lower token): out_scores (float32),
+ * out_tokens and out_parents (the beam) [num_items][num_best]. A logit of -inf is
+ * no candidate, nor is any of a beam whose score is not finite or whose logits
+ * hold a NaN or +inf. A beam with ended[w] != 0 (ended may be NULL) offers its
+ * end_token at its own score and nothing else. Where there are fewer candidates, the rest is -inf, -1, -1.
+ * Candidates are compared in 64 bits (the exponentials are in fp32, their sums joined in 64). DEVICE
+ * pointers; logits need only their elements' alignment; no output and no part of the
+ * workspace (256-byte aligned, its contents on entry do not matter) may overlap another array. */
+halo_status_t halo_beam_select(const halo_beam_sizes_t* sizes, const void* logits, const float* scores,
+                               const int32_t* ended, int32_t end_token,
+                               float* out_scores, int32_t* out_tokens, int32_t* out_parents,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int32_t num_items;
+  int32_t num_beams;        /* 1 .. 64 */
+  int32_t page_size;        /* 16 */
+  int32_t table_width;      /* pages of a row of the tables */
+  int32_t num_free;         /* elements of free_pages and free_pages_out */
+  int32_t parents_stride;   /* elements from an item's parents to the next one's, >= num_beams */
+} halo_beam_table_sizes_t;
+
+typedef struct {
+  int32_t* block_table;   /* [num_items * num_beams][table_width] */
+  int32_t* seq_len;       /* [num_items * num_beams] */
+  int32_t* free_pages;    /* [num_free] */
+  int32_t* free_next;     /* [1] */
+  int32_t* copy_src;      /* [num_items * num_beams] */
+  int32_t* copy_dst;
+} halo_beam_tables_t;
+
+/* The workspace (bytes) of halo_kv_beam_tables; -1 and an error for sizes that are
+ * refused. */
+int64_t halo_beam_tables_workspace_bytes(const halo_beam_table_sizes_t* sizes);
+
+/* The cache follows the beams: beam k of item i becomes a child of beam p =
+ * parents[i * parents_stride + k] of the same item (-1: it is given up, its row is
+ * empty). It gets its parent's length and pages. Pages are shared; only a last page that
+ * is partly filled belongs to the parent's first child alone, and every further
+ * child gets a page of its own out of the free list: copy_src[row], copy_dst[row]
+ * say which page to copy there (-1, -1: none; halo_kv_page_copy passes over
+ * them). Pages of block_table that no beam holds any more go to the free list.
+ * With T pages taken and F freed, tables->free_next = free_next + T - F, the freed
+ * ones are entered before free_next + T (by item, place in the row, beam) and
+ * tables->free_pages from there on is what free_pages was. Elements of
+ * tables->block_table past a row's pages and of tables->free_pages before its
+ * free_next are left as they were.
+ * The rows of one item may share pages, in the same place of their rows, as this
+ * call makes them; those of different items must not. A prefix shared by several
+ * items is no part of the rows (a segment of its own, see halo_forest_t).
+ * DEVICE arrays; none that is written may overlap another one. An item with a parent
+ * outside [-1, num_beams) or a length that does not fit its row stays as it is
+ * (every beam its own child, a row with such a length without pages); a call that
+ * does not fit (free_next outside [0, num_free], too few free pages, or more freed
+ * ones than free_next + T) leaves every item as it is. Either way 1 is written to
+ * error_flag (may be NULL). */
+halo_status_t halo_kv_beam_tables(const halo_beam_table_sizes_t* sizes, const int32_t* parents,
+                                  const int32_t* seq_len, const int32_t* block_table,
+                                  const int32_t* free_pages, const int32_t* free_next,
+                                  const halo_beam_tables_t* tables, void* workspace, size_t workspace_bytes,
+                                  int32_t* error_flag, void* stream);
+
 /* Prefix forest from token ids (host only, no device work). The prompts of
  * a batch that share prefixes (§2 intra-batch prefix sharing: a shared
  * prefix is computed once and its KV cache reused; §1: recurring prompts are

@@ -26,7 +26,8 @@ reads kv head h // (H_q / H_kv)).
 ``paged_kv`` holds the reference of the paged-KV write path (token scatter
 into the pool layouts, page copy for copy-on-write); ``forest`` the prefix
 forest of a batch of token-id prompts, by brute force; ``paged_kvq`` the 4-bit
-cache format.
+cache format; ``upkeep`` the operators between two steps (eviction by attention
+weight, beam search).
 """
 
 from .attention import (  # noqa: F401
@@ -40,3 +41,4 @@ from .attention import (  # noqa: F401
 from . import paged_kv  # noqa: F401,E402
 from . import forest  # noqa: F401,E402
 from . import paged_kvq  # noqa: F401,E402
+from . import upkeep  # noqa: F401,E402

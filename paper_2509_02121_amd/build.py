@@ -37,8 +37,12 @@ HIP_FLAGS = [
     "-Wall", "-Wno-unused-function",
 ]
 
+# what tells NaN from numbers by arithmetic, or hands it on
+SOURCE_FLAGS = {src: ["-fhonor-nans"] for src in ("halo_weights.hip", "halo_keep.hip", "halo_beam.hip")}
+
 HOST_SOURCES = ["halo_plan.cpp", "halo_forest.cpp", "halo_rope.cpp"]
-HIP_SOURCES = ["halo_kernels.hip", "halo_pages.hip", "halo_step.hip", "halo_kvq_attn.hip", "halo_kvq_pages.hip"]
+HIP_SOURCES = ["halo_kernels.hip", "halo_pages.hip", "halo_step.hip", "halo_kvq_attn.hip", "halo_kvq_pages.hip",
+               "halo_weights.hip", "halo_keep.hip", "halo_beam.hip"]
 PROBE_SOURCES = ["halo_probe.hip"]
 
 
@@ -54,7 +58,7 @@ def build(verbose=True):
         objs, procs = {}, []
         for src in HOST_SOURCES + HIP_SOURCES + PROBE_SOURCES:
             objs[src] = os.path.join(tmp, src + ".o")
-            cc = ["g++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-Wextra"] if src in HOST_SOURCES else [HIPCC] + HIP_FLAGS
+            cc = ["g++", "-std=c++17", "-O2", "-fPIC", "-Wall", "-Wextra"] if src in HOST_SOURCES else [HIPCC] + HIP_FLAGS + SOURCE_FLAGS.get(src, [])
             procs.append(subprocess.Popen(cc + ["-I", INCLUDE, "-c", os.path.join(CSRC, src), "-o", objs[src]]))
         rcs = [p.wait() for p in procs]
         if any(rcs):

@@ -1,0 +1,662 @@
+// gfx950 kernels and entry points of the C ABI for beam search:
+// beam_scan_kernel, beam_pick_kernel: the best candidates (beam, token) of each
+//   request by score + logit - ln sum exp(logits);
+// beam_freed_kernel, beam_rows_kernel: the beams' rows of the page table follow
+//   their parents.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <string>
+#include <type_traits>
+
+#include "halo_host.h"
+#include "halo_internal.h"
+#include "halo_pages_device.h"
+
+using namespace halo;
+
+namespace {
+
+constexpr int kMaxBeams = 64;
+constexpr int kMaxBest = 64;
+constexpr int kMaxVocab = 1 << 24;
+constexpr float kLowest = -3.4028234663852886e38f;
+constexpr float kMinusInf = -__builtin_huge_valf();
+
+// ---------------------------------------------------------------- one pass over the logits
+
+// What a wave found in its part of a row.
+struct BeamPart {
+  float top;      // the largest logit, or the lowest finite number
+  float sum;      // of exp(logit - top)
+  int32_t count;  // candidates it names
+  int32_t pad;
+};
+struct Candidate {
+  float value;
+  int32_t token;
+};
+
+struct BeamArgs {
+  const void* logits;
+  const float* scores;
+  const int32_t* ended;
+  BeamPart* parts;         // [rows][parts]
+  Candidate* candidates;   // [rows][parts][best]
+  float* out_scores;
+  int32_t* out_tokens;
+  int32_t* out_parents;
+  int64_t stride;
+  int32_t beams, vocab, best, end_token;
+  int32_t per;             // elements of a part, a multiple of 512
+  int32_t num_parts;
+};
+
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+__device__ __forceinline__ bool is_finite(double x) {
+  return ((uint64_t)__double_as_longlong(x) & 0x7ff0000000000000ull) != 0x7ff0000000000000ull;
+}
+// Larger numbers have larger keys; of -0 and 0 the same.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float from_order_key(uint32_t k) {
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+
+// The largest number of which at least n of the wave's N keys a lane are no
+// smaller, between lo (which has as many) and the largest key. Bit by bit, from the
+// keys' ballots.
+template <int N>
+__device__ __forceinline__ uint32_t wave_nth_key(const uint32_t (&key)[N], int n, uint32_t lo) {
+  uint32_t t = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t next = t | 1u << bit;
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) c += __popcll(__ballot(key[j] >= next));
+    if (c >= n) t = next;
+  }
+  return max(t, lo);
+}
+
+constexpr int kTile = 512;        // elements a wave looks at together
+constexpr int kListCap = 1024;    // candidates a wave holds
+
+// Keeps the `best` first of the list's n candidates (by value, then token).
+__device__ __forceinline__ int prune(float* value, int32_t* token, int n, int best, int lane) {
+  constexpr int N = kListCap / 64;
+  uint32_t key[N], id[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = 64 * j + lane;
+    key[j] = i < n ? order_key(value[i]) : 0;
+    id[j] = i < n ? ~(uint32_t)token[i] : 0;
+  }
+  if (n <= best) return n;
+  const uint32_t least = wave_nth_key(key, best, 0);
+  int above = 0, ties = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    above += __popcll(__ballot(key[j] > least));
+    ties += __popcll(__ballot(key[j] == least));
+  }
+  uint32_t last = 0;   // of the ties the tokens up to this one (of ~token: from it on)
+  if (above + ties > best) {
+    uint32_t of_ties[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) of_ties[j] = key[j] == least ? id[j] : 0;
+    last = wave_nth_key(of_ties, best - above, 0);
+  }
+  int at = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const bool keep = key[j] > least || (key[j] == least && id[j] >= last && id[j] != 0);
+    const uint64_t mask = __ballot(keep);
+    if (keep) {
+      const int to = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+      value[to] = from_order_key(key[j]);
+      token[to] = (int32_t)~id[j];
+    }
+    at += __popcll(mask);
+  }
+  return at;
+}
+
+// Elements x[0 .. 511] of a row, eight a lane, of which those from n on are -inf. Loads
+// are of 16 bytes at any alignment of the row, so that which lane adds what goes by
+// the token alone: two beams of the same logits have the same sum.
+template <typename T>
+__device__ __forceinline__ void load_tile(const T* x, int64_t n, int lane, float (&v)[8]) {
+  constexpr int E = 16 / (int)sizeof(T);
+#pragma unroll
+  for (int u = 0; u < 8 / E; ++u) {
+    const int i = (u * 64 + lane) * E;
+    T w[E];
+    if (i + E <= n) {
+      __builtin_memcpy(w, x + i, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) w[j] = i + j < n ? x[i + j] : (T)kMinusInf;
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) v[u * E + j] = (float)w[j];
+  }
+}
+// Place of element v[k] of a lane in its tile.
+template <typename T>
+__device__ __forceinline__ int place_in_tile(int k, int lane) {
+  constexpr int E = 16 / (int)sizeof(T);
+  return ((k / E) * 64 + lane) * E + k % E;
+}
+
+// A wave passes its part of a row once. A lane follows the largest of its logits and
+// the sum of their exponentials (fp32; the lanes' are joined in 64 bits). Candidates go to a
+// list in LDS: after the first tile those at or above the best-th largest lane maximum (as many
+// lanes have one), later those above the list's best-th, which is found anew when
+// the list has grown; ties with that are later tokens and no candidates.
+template <typename T>
+__global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
+  __shared__ float list_value[4][kListCap];
+  __shared__ int32_t list_token[4][kListCap];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int row = (int)blockIdx.y, part = (int)blockIdx.x * 4 + wave;
+  if (part >= a.num_parts) return;
+  BeamPart* out = a.parts + (int64_t)row * a.num_parts + part;
+  // (a beam that has ended or is dead: its logits are not looked at)
+  if ((a.ended && a.ended[row]) || !is_finite(a.scores[row])) {
+    if (lane == 0) *out = BeamPart{kLowest, 0.f, 0, 0};
+    return;
+  }
+  const T* x = static_cast<const T*>(a.logits) + (int64_t)row * a.stride;
+  const int64_t begin = (int64_t)part * a.per, end = min(begin + a.per, (int64_t)a.vocab);
+  float* value = list_value[wave];
+  int32_t* token = list_token[wave];
+  float top = kLowest, sum = 0.f, bound = kMinusInf;
+  int n = 0;
+  for (int64_t t = begin; t < end; t += kTile) {
+    float v[8];
+    load_tile<T>(x + t, end - t, lane, v);
+    float most = v[0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) most = fmaxf(most, v[k]);
+    const float now = fmaxf(top, most);
+    sum *= __builtin_amdgcn_exp2f((top - now) * 1.44269504088896340736f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f((v[k] - now) * 1.44269504088896340736f);
+    top = now;
+    if (t == begin) {
+      const uint32_t key[1] = {order_key(most)};
+      // just below the best-th largest lane maximum, not below -inf
+      uint32_t k = wave_nth_key(key, a.best, order_key(kMinusInf) + 1) - 1;
+      if (k == order_key(0.f) - 1) --k;   // (the key of -0)
+      bound = from_order_key(k);
+    }
+    if (!__any(most > bound)) continue;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool hit = v[k] > bound;
+      const uint64_t mask = __ballot(hit);
+      if (hit) {
+        const int to = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+        value[to] = v[k];
+        token[to] = (int32_t)t + place_in_tile<T>(k, lane);
+      }
+      n += __popcll(mask);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    if (n > kListCap - kTile || t == begin) {
+      n = prune(value, token, n, a.best, lane);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      if (n >= a.best) {
+        // (n = best: the list's smallest)
+        float least = -kMinusInf;
+        for (int i = lane; i < n; i += 64) least = fminf(least, value[i]);
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) least = fminf(least, __shfl_xor(least, m));
+        bound = least;
+      } else {
+        bound = kMinusInf;
+      }
+    }
+  }
+  n = prune(value, token, n, a.best, lane);
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  Candidate* c = a.candidates + ((int64_t)row * a.num_parts + part) * a.best;
+  for (int i = lane; i < n; i += 64) c[i] = Candidate{value[i], token[i]};
+  float most = top;
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+  double s = (double)sum * exp2((double)(top - most) * 1.44269504088896340736);
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
+  if (lane == 0) *out = BeamPart{most, (float)s, n, 0};
+}
+
+// ---------------------------------------------------------------- the best of an item
+
+__device__ __forceinline__ uint64_t order_key(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+  return u & 0x8000000000000000ull ? ~u : u | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double from_order_key(uint64_t k) {
+  return __longlong_as_double((long long)(k & 0x8000000000000000ull ? k & 0x7fffffffffffffffull : ~k));
+}
+
+// A workgroup for each item: ln sum exp of every beam from its parts, then `best`
+// rounds, each of which finds the first of the candidates behind the last round's.
+__global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
+  __shared__ double lse[kMaxBeams];
+  __shared__ int32_t live[kMaxBeams];   // 0 dead, 1 live, 2 ended
+  __shared__ uint64_t best_key[4], best_id[4];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int item = (int)blockIdx.x, W = a.beams, P = a.num_parts;
+  for (int b = wave; b < W; b += 4) {
+    const int row = item * W + b;
+    const BeamPart* parts = a.parts + (int64_t)row * P;
+    const bool open = is_finite(a.scores[row]);
+    const bool ended = a.ended && a.ended[row];
+    float most = kLowest;
+    for (int p = lane; p < P; p += 64) most = fmaxf(most, parts[p].top);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
+    double s = 0;
+    for (int p = lane; p < P; p += 64) s += (double)parts[p].sum * exp2((double)(parts[p].top - most) * 1.44269504088896340736);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
+    if (lane == 0) {
+      // (a NaN or +inf among the logits makes the sum no number)
+      const bool sound = is_finite(s) && s > 0 && is_finite(most);
+      lse[b] = sound ? (double)most + log(s) : 0;
+      live[b] = !open ? 0 : ended ? 2 : sound ? 1 : 0;
+    }
+  }
+  __syncthreads();
+  uint64_t last_key = ~0ull, last_id = 0;   // candidates are in order of falling keys, rising ids
+  const int per_row = P * a.best;
+  for (int r = 0; r < a.best; ++r) {
+    uint64_t key = 0, id = ~0ull;
+    for (int i = tid; i < W * per_row; i += 256) {
+      const int b = i / per_row, j = i % per_row, p = j / a.best, c = j % a.best;
+      const int64_t at = ((int64_t)(item * W + b) * P + p);
+      double v;
+      int32_t tok;
+      if (live[b] == 1) {
+        if (c >= a.parts[at].count) continue;
+        const Candidate x = a.candidates[at * a.best + c];
+        v = ((double)x.value - lse[b]) + (double)a.scores[item * W + b];
+        tok = x.token;
+      } else if (live[b] == 2 && j == 0) {
+        v = (double)a.scores[item * W + b];
+        tok = a.end_token;
+      } else {
+        continue;
+      }
+      const uint64_t k = order_key(v), d = (uint64_t)b << 32 | (uint32_t)tok;
+      const bool behind = k < last_key || (k == last_key && d > last_id);
+      if (behind && (k > key || (k == key && d < id))) {
+        key = k;
+        id = d;
+      }
+    }
+    auto better = [&](uint64_t k, uint64_t d) {
+      if (k > key || (k == key && d < id)) {
+        key = k;
+        id = d;
+      }
+    };
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) better(__shfl_xor(key, m), __shfl_xor(id, m));
+    __syncthreads();
+    if (lane == 0) {
+      best_key[wave] = key;
+      best_id[wave] = id;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) better(best_key[w], best_id[w]);
+    if (tid == 0) {
+      const int64_t to = (int64_t)item * a.best + r;
+      const bool any = key != 0;
+      a.out_scores[to] = any ? (float)from_order_key(key) : kMinusInf;
+      a.out_tokens[to] = any ? (int32_t)(uint32_t)id : -1;
+      a.out_parents[to] = any ? (int32_t)(id >> 32) : -1;
+    }
+    last_key = key;
+    last_id = id;
+  }
+}
+
+// ---------------------------------------------------------------- the tables
+
+struct ItemCount {
+  int32_t taken, freed, bad, pad;
+};
+
+struct BeamTableArgs {
+  halo_beam_table_sizes_t s;
+  halo_beam_tables_t out;
+  const int32_t* parents;
+  const int32_t* seq_len;
+  const int32_t* block_table;
+  const int32_t* free_pages;
+  const int32_t* free_next;
+  ItemCount* counts;   // [items]
+  int32_t* freed;      // [items][beams * width]
+  int32_t* error_flag;
+  int32_t splits;
+};
+
+// An item's beams in LDS: parents, lengths, and which beam is its parent's first
+// child. One that is malformed is its own parents' item, with no pages in a row whose
+// length does not fit.
+struct ItemBeams {
+  int32_t parent[kMaxBeams], len[kMaxBeams], pages[kMaxBeams], copied[kMaxBeams], mother[kMaxBeams], bad;
+  __device__ __forceinline__ void load(const BeamTableArgs& a, int item, bool as_it_is) {
+    const int tid = threadIdx.x, W = a.s.num_beams;
+    if (tid == 0) bad = 0;
+    __syncthreads();
+    if (tid < W) {
+      const int p = a.parents[(int64_t)item * a.s.parents_stride + tid], n = a.seq_len[(int64_t)item * W + tid];
+      const bool fits = n >= 0 && (int64_t)n <= (int64_t)a.s.table_width * 16;
+      parent[tid] = p;
+      len[tid] = n;
+      pages[tid] = fits ? (int)(((int64_t)n + 15) >> 4) : 0;
+      mother[tid] = 0;
+      if (p < -1 || p >= W || !fits) bad = 1;
+    }
+    __syncthreads();
+    if (tid < W) {
+      if (bad || as_it_is) parent[tid] = tid;
+    }
+    __syncthreads();
+    if (tid < W) {
+      const int p = parent[tid];
+      bool later = false;
+      for (int k = 0; k < tid; ++k) later |= parent[k] == p;
+      copied[tid] = p >= 0 && later && (len[p] & 15) != 0;
+      if (p >= 0) mother[p] = 1;   // (the same value from every child)
+    }
+    __syncthreads();
+  }
+};
+
+// A workgroup for each item: how many pages it takes, and which ones it frees. Beams
+// of an item share pages only in the same place of their rows, so a page of a
+// beam without children is free if no beam with children has it there, nor an
+// earlier beam without: each place of the rows is looked at by itself, W x W
+// comparisons, without counts of references.
+__global__ __launch_bounds__(256) void beam_freed_kernel(BeamTableArgs a) {
+  __shared__ ItemBeams m;
+  __shared__ int sums[4];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, item = (int)blockIdx.x, W = a.s.num_beams;
+  m.load(a, item, false);
+  const int32_t* table = a.block_table + (int64_t)item * W * a.s.table_width;
+  int32_t* list = a.freed + (int64_t)item * W * a.s.table_width;
+  int most = 0;
+  for (int b = 0; b < W; ++b) most = max(most, m.mother[b] ? 0 : m.pages[b]);
+  int done = 0;
+  for (int c0 = 0; c0 < most; c0 += 256) {
+    const int c = c0 + tid;
+    uint64_t gone = 0;
+    for (int b = 0; b < W; ++b) {
+      if (m.mother[b] || c >= m.pages[b]) continue;
+      const int page = table[(int64_t)b * a.s.table_width + c];
+      bool held = false;
+      for (int k = 0; k < W; ++k)
+        if ((m.mother[k] || k < b) && c < m.pages[k]) held |= table[(int64_t)k * a.s.table_width + c] == page;
+      gone |= held ? 0ull : 1ull << b;
+    }
+    const int mine = __popcll(gone), upto = wave_inclusive_sum(mine);
+    __syncthreads();
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int at = done + upto - mine;
+    for (int w = 0; w < 4; ++w) {
+      at += w < wave ? sums[w] : 0;
+      done += sums[w];
+    }
+    while (gone) {
+      const int b = __builtin_ctzll(gone);
+      gone &= gone - 1;
+      list[at++] = table[(int64_t)b * a.s.table_width + c];
+    }
+  }
+  if (tid == 0) {
+    int taken = 0;
+    for (int k = 0; k < W; ++k) taken += m.copied[k];
+    a.counts[item] = ItemCount{taken, done, m.bad, 0};
+  }
+}
+
+// The items' rows, copies and freed pages at their places: sums over the items before
+// each one, which every workgroup makes itself.
+__global__ __launch_bounds__(256) void beam_rows_kernel(BeamTableArgs a) {
+  __shared__ ItemBeams m;
+  __shared__ int64_t sums[4][5];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, W = a.s.num_beams;
+  const int item = (int)(blockIdx.x / a.splits), split = (int)(blockIdx.x % a.splits);
+  int64_t s[5] = {0, 0, 0, 0, 0};   // taken and freed before the item, of all; malformed items
+  for (int i = tid; i < a.s.num_items; i += 256) {
+    const ItemCount c = a.counts[i];
+    s[2] += c.taken;
+    s[3] += c.freed;
+    s[4] += c.bad;
+    if (i < item) {
+      s[0] += c.taken;
+      s[1] += c.freed;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 5; ++k) {
+#pragma unroll
+    for (int x = 32; x >= 1; x >>= 1) s[k] += __shfl_xor(s[k], x);
+    if (lane == 0) sums[wave][k] = s[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 5; ++k) s[k] = sums[0][k] + sums[1][k] + sums[2][k] + sums[3][k];
+  const int first = a.free_next[0];
+  const bool in = first >= 0 && first <= a.s.num_free;
+  const bool fits = in && s[2] <= a.s.num_free - first && first + s[2] - s[3] >= 0;
+  const int64_t rest = fits ? first + s[2] : first;   // from here on the free list stays
+  if (blockIdx.x == 0 && tid == 0) {
+    a.out.free_next[0] = (int)(fits ? rest - s[3] : first);
+    if ((s[4] || !fits) && a.error_flag) a.error_flag[0] = 1;
+  }
+  if (in)
+    for (int64_t j = rest + (int64_t)blockIdx.x * 256 + tid; j < a.s.num_free; j += (int64_t)gridDim.x * 256)
+      a.out.free_pages[j] = a.free_pages[j];
+  if (item >= a.s.num_items) return;
+  m.load(a, item, !fits);
+  if (fits) {
+    const int32_t* list = a.freed + (int64_t)item * W * a.s.table_width;
+    const int n = a.counts[item].freed;
+    for (int64_t j = (int64_t)split * 256 + tid; j < n; j += (int64_t)a.splits * 256)
+      a.out.free_pages[rest - s[3] + s[1] + j] = list[j];
+  }
+  int64_t next = first + s[0];   // the page that the item's next copy takes
+  for (int k = 0; k < W; ++k) {
+    const int p = m.parent[k];
+    const int64_t row = (int64_t)item * W + k;
+    const int pages = p < 0 ? 0 : m.pages[p];
+    const bool copied = m.copied[k] && fits;
+    const int32_t* from = a.block_table + ((int64_t)item * W + max(p, 0)) * a.s.table_width;
+    int32_t* to = a.out.block_table + row * a.s.table_width;
+    const int32_t fresh = copied ? a.free_pages[next] : -1;
+    for (int64_t c = (int64_t)split * 256 + tid; c < pages; c += (int64_t)a.splits * 256)
+      to[c] = copied && c == pages - 1 ? fresh : from[c];
+    if (split == 0 && tid == 0) {
+      a.out.seq_len[row] = p < 0 ? 0 : m.len[p];
+      a.out.copy_src[row] = copied ? from[pages - 1] : -1;
+      a.out.copy_dst[row] = fresh;
+    }
+    next += copied;
+  }
+}
+
+// ---------------------------------------------------------------- host side
+
+halo_status_t check_sizes(const halo_beam_sizes_t* s) {
+  if (!s) return fail(HALO_ERR_INVALID_ARGUMENT, "sizes must not be NULL");
+  if (s->num_items < 0) return fail(HALO_ERR_INVALID_ARGUMENT, "num_items must be >= 0");
+  if (s->num_beams < 1 || s->vocab < 1 || s->num_best < 1)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "num_beams, vocab and num_best must be >= 1");
+  if (s->num_beams > kMaxBeams || s->num_best > kMaxBest || s->vocab > kMaxVocab)
+    return fail(HALO_ERR_UNSUPPORTED, "at most 64 beams, 64 candidates and 2^24 tokens");
+  if (s->logits_stride < s->vocab) return fail(HALO_ERR_INVALID_ARGUMENT, "logits_stride must be >= vocab");
+  if (s->dtype != HALO_F32 && s->dtype != HALO_BF16)
+    return fail(HALO_ERR_UNSUPPORTED, "dtype must be HALO_F32 or HALO_BF16");
+  if ((int64_t)s->num_items * s->num_beams > 65535)
+    return fail(HALO_ERR_UNSUPPORTED, "num_items * num_beams must be at most 65535");
+  return HALO_OK;
+}
+
+// Elements of a wave's part of a row, and the parts of a row: about 8192 waves in
+// all, of at least four tiles each.
+void parts_of(const halo_beam_sizes_t* s, int32_t& per, int32_t& parts) {
+  const int64_t rows = std::max<int64_t>((int64_t)s->num_items * s->num_beams, 1);
+  const int64_t span = s->vocab;
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(8192 / rows, (span + 2047) / 2048));
+  per = (int32_t)((span + want * kTile - 1) / (want * kTile) * kTile);
+  parts = (int32_t)((span + per - 1) / per);
+}
+
+int64_t parts_bytes(const halo_beam_sizes_t* s, int32_t parts) {
+  return ((int64_t)s->num_items * s->num_beams * parts * (int64_t)sizeof(BeamPart) + 255) / 256 * 256;
+}
+
+halo_status_t check_sizes(const halo_beam_table_sizes_t* s) {
+  if (!s) return fail(HALO_ERR_INVALID_ARGUMENT, "sizes must not be NULL");
+  if (s->num_items < 0 || s->table_width < 0 || s->num_free < 0)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "num_items, table_width and num_free must be >= 0");
+  if (s->num_beams < 1) return fail(HALO_ERR_INVALID_ARGUMENT, "num_beams must be >= 1");
+  if (s->num_beams > kMaxBeams) return fail(HALO_ERR_UNSUPPORTED, "at most 64 beams");
+  if (s->page_size != 16) return fail(HALO_ERR_UNSUPPORTED, "page_size must be 16");
+  if (s->parents_stride < s->num_beams)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "parents_stride must be >= num_beams");
+  if ((int64_t)s->num_items * s->num_beams * s->table_width > INT32_MAX || s->num_items > 1 << 20)
+    return fail(HALO_ERR_UNSUPPORTED, "at most 2^20 items and 2^31 - 1 elements of a table");
+  return HALO_OK;
+}
+
+int64_t counts_bytes(const halo_beam_table_sizes_t* s) {
+  return ((int64_t)s->num_items * (int64_t)sizeof(ItemCount) + 255) / 256 * 256;
+}
+
+bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255) == 0; }
+
+}  // namespace
+
+extern "C" int64_t halo_beam_workspace_bytes(const halo_beam_sizes_t* sizes) {
+  clear_error();
+  if (check_sizes(sizes) != HALO_OK) return -1;
+  int32_t per, parts;
+  parts_of(sizes, per, parts);
+  return parts_bytes(sizes, parts) +
+         (int64_t)sizes->num_items * sizes->num_beams * parts * sizes->num_best * (int64_t)sizeof(Candidate);
+}
+
+extern "C" halo_status_t halo_beam_select(const halo_beam_sizes_t* sizes, const void* logits, const float* scores,
+                                          const int32_t* ended, int32_t end_token, float* out_scores,
+                                          int32_t* out_tokens, int32_t* out_parents, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+  clear_error();
+  const halo_status_t st = check_sizes(sizes);
+  if (st != HALO_OK) return st;
+  if (ended && (end_token < 0 || end_token >= sizes->vocab))
+    return fail(HALO_ERR_INVALID_ARGUMENT, "end_token must be in [0, vocab)");
+  if (sizes->num_items == 0) return HALO_OK;
+  if (!logits || !scores || !out_scores || !out_tokens || !out_parents || !workspace)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "only ended may be NULL");
+  const int elt = sizes->dtype == HALO_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(logits) % elt) return fail(HALO_ERR_INVALID_ARGUMENT, "logits must be aligned to their elements");
+  if (!aligned256(workspace)) return fail(HALO_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
+  const int64_t need = halo_beam_workspace_bytes(sizes);
+  if (workspace_bytes < (size_t)need)
+    return fail(HALO_ERR_WORKSPACE_TOO_SMALL, "workspace has " + std::to_string(workspace_bytes) + " bytes, needs " +
+                                                  std::to_string(need));
+  const int64_t rows = (int64_t)sizes->num_items * sizes->num_beams, out = (int64_t)sizes->num_items * sizes->num_best * 4;
+  const halo_status_t lap = check_overlaps(
+      {{"logits", logits, ((rows - 1) * sizes->logits_stride + sizes->vocab) * elt}, {"scores", scores, rows * 4},
+       {"ended", ended, rows * 4}},
+      {{"out_scores", out_scores, out}, {"out_tokens", out_tokens, out}, {"out_parents", out_parents, out},
+       {"workspace", workspace, need}});
+  if (lap != HALO_OK) return lap;
+  BeamArgs g{};
+  g.logits = logits;
+  g.scores = scores;
+  g.ended = ended;
+  parts_of(sizes, g.per, g.num_parts);
+  g.parts = static_cast<BeamPart*>(workspace);
+  g.candidates = reinterpret_cast<Candidate*>(static_cast<uint8_t*>(workspace) + parts_bytes(sizes, g.num_parts));
+  g.out_scores = out_scores;
+  g.out_tokens = out_tokens;
+  g.out_parents = out_parents;
+  g.stride = sizes->logits_stride;
+  g.beams = sizes->num_beams;
+  g.vocab = sizes->vocab;
+  g.best = sizes->num_best;
+  g.end_token = end_token;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  const dim3 grid((unsigned)((g.num_parts + 3) / 4), (unsigned)rows);
+  if (sizes->dtype == HALO_BF16) hipLaunchKernelGGL(beam_scan_kernel<__bf16>, grid, dim3(256), 0, s, g);
+  else hipLaunchKernelGGL(beam_scan_kernel<float>, grid, dim3(256), 0, s, g);
+  hipLaunchKernelGGL(beam_pick_kernel, dim3(sizes->num_items), dim3(256), 0, s, g);
+  return hip_check("beam selection launch");
+}
+
+extern "C" int64_t halo_beam_tables_workspace_bytes(const halo_beam_table_sizes_t* sizes) {
+  clear_error();
+  if (check_sizes(sizes) != HALO_OK) return -1;
+  return counts_bytes(sizes) + (int64_t)sizes->num_items * sizes->num_beams * sizes->table_width * 4;
+}
+
+extern "C" halo_status_t halo_kv_beam_tables(const halo_beam_table_sizes_t* sizes, const int32_t* parents,
+                                             const int32_t* seq_len, const int32_t* block_table,
+                                             const int32_t* free_pages, const int32_t* free_next,
+                                             const halo_beam_tables_t* tables, void* workspace,
+                                             size_t workspace_bytes, int32_t* error_flag, void* stream) {
+  clear_error();
+  const halo_status_t st = check_sizes(sizes);
+  if (st != HALO_OK) return st;
+  if (!tables) return fail(HALO_ERR_INVALID_ARGUMENT, "tables must not be NULL");
+  const int64_t items = sizes->num_items, rows = items * sizes->num_beams, cells = rows * sizes->table_width * 4;
+  if (!free_next || !tables->free_next ||
+      (rows > 0 && (!parents || !seq_len || !tables->seq_len || !tables->copy_src || !tables->copy_dst || !workspace)) ||
+      (cells > 0 && (!block_table || !tables->block_table)) ||
+      (sizes->num_free > 0 && (!free_pages || !tables->free_pages)))
+    return fail(HALO_ERR_INVALID_ARGUMENT, "only error_flag (and arrays of no elements) may be NULL");
+  if (!aligned256(workspace)) return fail(HALO_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
+  const int64_t need = halo_beam_tables_workspace_bytes(sizes);
+  if (workspace_bytes < (size_t)need)
+    return fail(HALO_ERR_WORKSPACE_TOO_SMALL, "workspace has " + std::to_string(workspace_bytes) + " bytes, needs " +
+                                                  std::to_string(need));
+  const int64_t free_bytes = 4 * (int64_t)sizes->num_free;
+  const halo_status_t lap = check_overlaps(
+      {{"parents", parents, items ? ((items - 1) * sizes->parents_stride + sizes->num_beams) * 4 : 0},
+       {"seq_len", seq_len, 4 * rows}, {"block_table", block_table, cells}, {"free_pages", free_pages, free_bytes},
+       {"free_next", free_next, 4}},
+      {{"tables' block_table", tables->block_table, cells}, {"tables' seq_len", tables->seq_len, 4 * rows},
+       {"tables' free_pages", tables->free_pages, free_bytes}, {"tables' free_next", tables->free_next, 4},
+       {"tables' copy_src", tables->copy_src, 4 * rows}, {"tables' copy_dst", tables->copy_dst, 4 * rows},
+       {"workspace", workspace, need}, {"error_flag", error_flag, 4}});
+  if (lap != HALO_OK) return lap;
+  BeamTableArgs g{*sizes, *tables, parents, seq_len, block_table, free_pages, free_next,
+                  static_cast<ItemCount*>(workspace),
+                  reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + counts_bytes(sizes)), error_flag, 1};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  if (items > 0) hipLaunchKernelGGL(beam_freed_kernel, dim3((unsigned)items), dim3(256), 0, s, g);
+  hipLaunchKernelGGL(beam_rows_kernel, dim3((unsigned)std::max<int64_t>(items, 1)), dim3(256), 0, s, g);
+  return hip_check("beam tables launch");
+}

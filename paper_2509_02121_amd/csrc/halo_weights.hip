@@ -1,0 +1,308 @@
+// gfx950 kernels and entry points of the C ABI for the attention weight that
+// cached tokens get from the queries of a step:
+//
+//   w[i, h, t] = decay * w[i, h, t] + sum over rows r that see t, heads g of h:
+//                exp(scale q[r, g] . k[t, h] - lse[r, g])
+//
+// lse is known (attention has run), so there is no maximum to follow and no V:
+// a wave holds the keys of a few pages in registers and passes the rows by them,
+// 16 at a time, and each key is read once. A key's sum stays with its lanes from
+// the first row to the last, so it has one order and needs no atomics.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <string>
+#include <type_traits>
+
+#include "halo_device.h"
+#include "halo_host.h"
+#include "halo_internal.h"
+#include "halo_kvq_format.h"
+#include "halo_pages_device.h"
+
+using namespace halo;
+
+namespace {
+
+struct WeightArgs {
+  const void* k_pool;
+  const void* q;
+  const float* lse;
+  const float* weights;
+  float* weights_out;
+  const int32_t* page_ids;
+  const int32_t* seq_page_indptr;
+  const int32_t* seq_start;
+  const int32_t* seq_end;
+  const int32_t* row_indptr;
+  const int32_t* rows;
+  const int32_t* row_end;
+  int32_t* error_flag;
+  int64_t num_pool_pages;
+  int32_t num_seqs, num_rows, num_entries, width;
+  int32_t num_kv_heads, group;   // group: q heads of a kv head
+  float scale_log2, decay;
+};
+
+// How keys lie in the pool and what they become: fragments of the products.
+// bf16 queries and keys: one product of bf16 fragments. fp32 ones: fp32 products.
+// 4-bit keys are exact in bf16, so fp32 queries go there in three bf16 parts.
+template <typename T, bool KVQ, int D>
+struct KeyFormat {
+  static constexpr int kParts = KVQ && sizeof(T) == 4 ? 3 : 1;
+  using F = typename std::conditional<KVQ, bf16x8_t, typename FragOf<T>::type>::type;
+  static constexpr int64_t kTile = KVQ ? kvq_k_tile<D>() : 16 * D * (int)sizeof(T);
+
+  // The fragments of the 16 keys of a tile: lane (key = lane & 15, grp) holds dims
+  // 32 s + 8 grp .. + 7 of its key.
+  static __device__ __forceinline__ void load_keys(const uint8_t* tile, int lane, F (&k)[D / 32]) {
+    const int key = lane & 15, grp = lane >> 4;
+    if constexpr (KVQ) {
+      uint32_t codes[D / 32], scales;
+      const uint8_t* at = tile + (grp * 16 + key) * (D / 8);
+      const uint8_t* sc = tile + D * 8 + key * (D / 32);
+      if constexpr (D == 128) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(at);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) codes[s] = x[s];
+        scales = *reinterpret_cast<const uint32_t*>(sc);
+      } else {
+        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(at);
+        codes[0] = x[0];
+        codes[1] = x[1];
+        scales = *reinterpret_cast<const uint16_t*>(sc);
+      }
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) k[s] = kvq_decode_bf16(codes[s], kvq_scale_byte(scales, s));
+    } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s)
+        k[s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(tile + ((4 * s + grp) * 16 + key) * 16));
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 32; ++s) k[s] = load_k8<false>(reinterpret_cast<const float*>(tile), key, 32 * s + 8 * grp);
+    }
+  }
+
+  // A row's fragments, dims 32 s + 8 grp .. + 7.
+  static __device__ __forceinline__ void load_query(const T* row, int grp, F (&q)[kParts][D / 32]) {
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      const auto x = load8(row + 32 * s + 8 * grp);
+      if constexpr (kParts == 1) {
+        q[0][s] = x;
+      } else {
+        float v[8];
+        bf16x8_t f[kParts];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = x[j];
+        split(v, f);
+#pragma unroll
+        for (int n = 0; n < kParts; ++n) q[n][s] = f[n];
+      }
+    }
+  }
+};
+
+// Keys that a wave holds at a time.
+template <typename T, bool KVQ, int D>
+constexpr int weight_pages() { return sizeof(T) == 4 && !KVQ && D == 128 ? 2 : 4; }
+
+// One sequence as the call gives it.
+struct WeightSeq {
+  int base, next, end, start, e0, e1;
+  bool bad, bad_rows;   // (entries that are no range of the list: none)
+  __device__ __forceinline__ WeightSeq(const WeightArgs& a, int seq) {
+    base = a.seq_page_indptr[seq];
+    next = a.seq_page_indptr[seq + 1];
+    end = a.seq_end[seq];
+    start = a.seq_start ? a.seq_start[seq] : end;
+    bad = end < 0 || end > a.width || (int64_t)(next - base) * 16 < end;
+    e0 = a.row_indptr ? a.row_indptr[seq] : seq;
+    e1 = a.row_indptr ? a.row_indptr[seq + 1] : seq + 1;
+    bad_rows = a.row_indptr && (e0 < 0 || e1 < e0 || e1 > a.num_entries);
+    if (bad_rows) e0 = e1 = 0;
+  }
+};
+
+// The (page slot, head) tiles are dealt to the waves in jobs of `run` slots of one
+// head, which may span sequences; of a job a wave takes up to NP pages of one
+// sequence at a time, and passes all its rows by them. Rows are the A operand and keys the B
+// operand of 16x16x32 MFMAs, so that a lane has four rows of one key: their
+// exponentials are summed in the lane, and the four lane groups once at the end.
+template <typename T, bool KVQ, int D>
+__global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
+  using Fmt = KeyFormat<T, KVQ, D>;
+  using F = typename Fmt::F;
+  constexpr int NS = D / 32, NP = weight_pages<T, KVQ, D>(), PARTS = Fmt::kParts;
+  const int lane = threadIdx.x & 63, key = lane & 15, grp = lane >> 4;
+  const int H = a.num_kv_heads, G = a.group;
+  const int first = a.seq_page_indptr[0];
+  const int64_t slots = (int64_t)a.seq_page_indptr[a.num_seqs] - first;
+  const int64_t waves = (int64_t)gridDim.x * 4, wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  // as many slots a job as keep every wave busy once, whole groups of NP pages
+  const int64_t run = min((int64_t)64, max((int64_t)NP, ((slots * H + waves - 1) / waves + NP - 1) / NP * NP));
+  const int64_t jobs = (slots + run - 1) / run * H;
+  for (int64_t job = wave; job < jobs; job += waves) {
+    const int h = (int)(job % H);
+    int64_t slot = job / H * run;
+    const int64_t last = min(slots, slot + run);
+    int seq = last_at_or_below(a.seq_page_indptr, a.num_seqs, first + slot, lane);
+    int loaded = -1;   // the sequence whose only tile of rows is in q
+    F q[PARTS][NS];
+    float l2[4];
+    int sees[4];
+    while (slot < last) {
+      while (first + slot >= a.seq_page_indptr[seq + 1]) ++seq;   // (ends at num_seqs - 1: slot < slots)
+      const WeightSeq s(a, seq);
+      const int from = (int)(first + slot - s.base);              // the page's place in its list
+      const int n = (int)min(min(last - slot, (int64_t)(s.next - s.base - from)), (int64_t)(NP - from % NP));
+      slot += n;
+      if ((s.bad || s.bad_rows || a.num_pool_pages == 0) && lane == 0 && a.error_flag) a.error_flag[0] = 1;
+      if (s.bad || a.num_pool_pages == 0) continue;
+      const int t0 = from * 16;
+      if (t0 >= s.end) continue;
+      F k[NP][NS];
+      bool ok[NP];
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int pid = p < n && t0 + 16 * p < s.end ? a.page_ids[s.base + from + p] : -2;
+        ok[p] = pid >= 0 && pid < a.num_pool_pages;
+        if (!ok[p] && pid != -2 && lane == 0 && a.error_flag) a.error_flag[0] = 1;
+        // (a page that is none is read as page 0 and not written)
+        Fmt::load_keys(static_cast<const uint8_t*>(a.k_pool) + ((int64_t)(ok[p] ? pid : 0) * H + h) * Fmt::kTile, lane, k[p]);
+      }
+      float sum[NP] = {};
+      const int64_t rows = (int64_t)(s.e1 - s.e0) * G;
+      for (int64_t r0 = 0; r0 < rows; r0 += 16) {
+        if (rows > 16 || loaded != seq) {
+          loaded = seq;
+          // lane (row = lane & 15) brings its row's fragments; then rows 4 grp + i
+          auto row_of = [&](int64_t r, int& e) {
+            e = (int)(s.e0 + r / G);
+            if (r >= rows) return -1;
+            const int at = a.rows ? a.rows[e] : e;
+            return at >= 0 && at < a.num_rows ? at : -1;
+          };
+          int e;
+          const int64_t r = r0 + key;
+          const int at = row_of(r, e);
+          if (r < rows && at < 0 && a.error_flag) a.error_flag[0] = 1;
+          const T* qp = static_cast<const T*>(a.q) + ((int64_t)max(at, 0) * H * G + (int64_t)h * G + r % G) * D;
+          if (at >= 0) Fmt::load_query(qp, grp, q);
+          else
+#pragma unroll
+            for (int x = 0; x < PARTS; ++x)
+#pragma unroll
+              for (int y = 0; y < NS; ++y) q[x][y] = zero_frag<F>();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int64_t ri = r0 + 4 * grp + i;
+            const int ai = row_of(ri, e);
+            const float l = ai >= 0 ? a.lse[(int64_t)ai * H * G + (int64_t)h * G + ri % G] : kNegInf;
+            sees[i] = l == kNegInf ? 0 : a.row_end ? min(a.row_end[e], s.end) : s.end;
+            l2[i] = l == kNegInf ? 0.f : l * kLog2e;
+          }
+        }
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+          f32x4_t x = {};
+#pragma unroll
+          for (int m = 0; m < PARTS; ++m)
+#pragma unroll
+            for (int y = 0; y < NS; ++y) x = mma(q[PARTS - 1 - m][y], k[p][y], x);
+          const int t = t0 + 16 * p + key;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, -l2[i]));
+            sum[p] += t < sees[i] ? w : 0.f;
+          }
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const float w = rows_sum(sum[p]);
+        const int t = t0 + 16 * p + key;
+        if (ok[p] && p < n && t < s.end && grp == 0) {
+          const int64_t at = ((int64_t)seq * H + h) * a.width + t;
+          const bool old = t < s.start && a.decay != 0.f;
+          a.weights_out[at] = old ? __builtin_fmaf(a.decay, a.weights[at], w) : w;
+        }
+      }
+    }
+  }
+}
+
+halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_t* params,
+                           const halo_weight_sizes_t* sizes, const int32_t* page_ids, const int32_t* seq_page_indptr,
+                           const int32_t* seq_start, const int32_t* seq_end, const int32_t* row_indptr,
+                           const int32_t* rows, const int32_t* row_end, const void* q, const float* lse, float decay,
+                           const float* weights, float* weights_out, int32_t* error_flag, void* stream) {
+  clear_error();
+  if (!params || !sizes) return fail(HALO_ERR_INVALID_ARGUMENT, "params and sizes must not be NULL");
+  if (sizes->num_seqs < 0 || sizes->num_rows < 0 || sizes->num_entries < 0 || sizes->width < 0)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "every size must be >= 0");
+  const halo_status_t st = check_cache_params(params);
+  if (st != HALO_OK) return st;
+  const int H = params->num_kv_heads;
+  if (params->num_q_heads < H || params->num_q_heads % H != 0)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "num_q_heads must be a multiple of num_kv_heads");
+  if (!finite(params->sm_scale) || params->sm_scale <= 0.f)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "sm_scale must be positive and finite");
+  if (!finite(decay) || decay < 0.f) return fail(HALO_ERR_INVALID_ARGUMENT, "decay must be finite and >= 0");
+  if (sizes->num_seqs == 0 || sizes->width == 0) return HALO_OK;
+  if (!k_pool || !page_ids || !seq_page_indptr || !seq_end || !weights_out || (sizes->num_rows > 0 && (!q || !lse)))
+    return fail(HALO_ERR_INVALID_ARGUMENT,
+                "k_pool, page_ids, seq_page_indptr, seq_end, q, lse, weights_out must not be NULL");
+  if (!weights && decay != 0.f) return fail(HALO_ERR_INVALID_ARGUMENT, "weights must not be NULL unless decay is 0");
+  if (!row_indptr && (rows || row_end) && sizes->num_entries < sizes->num_seqs)
+    return fail(HALO_ERR_INVALID_ARGUMENT, "without row_indptr, rows and row_end have an element for each sequence");
+  if (!aligned16(k_pool) || !aligned16(q)) return fail(HALO_ERR_INVALID_ARGUMENT, "k_pool and q must be 16-byte aligned");
+  const int64_t n = sizes->num_seqs, cells = n * H * sizes->width * 4, elt = params->kv_dtype == HALO_BF16 ? 2 : 4;
+  const int64_t rows_h = (int64_t)sizes->num_rows * params->num_q_heads, entries = 4 * (int64_t)sizes->num_entries;
+  const int64_t tile = kvq ? params->head_dim * 8 + params->head_dim / 2 : 16 * params->head_dim * elt;
+  const halo_status_t lap = check_overlaps(
+      {{"k_pool", k_pool, params->num_pool_pages * H * tile}, {"q", q, rows_h * params->head_dim * elt},
+       {"lse", lse, rows_h * 4}, {"weights", weights == weights_out ? nullptr : weights, cells},
+       {"seq_page_indptr", seq_page_indptr, 4 * (n + 1)}, {"seq_start", seq_start, 4 * n}, {"seq_end", seq_end, 4 * n},
+       {"row_indptr", row_indptr, 4 * (n + 1)}, {"rows", rows, entries}, {"row_end", row_end, entries}},
+      {{"weights_out", weights_out, cells}, {"error_flag", error_flag, 4}});
+  if (lap != HALO_OK) return lap;
+  WeightArgs g{k_pool, q, lse, weights, weights_out, page_ids, seq_page_indptr, seq_start, seq_end, row_indptr, rows,
+               row_end, error_flag, params->num_pool_pages, sizes->num_seqs, sizes->num_rows, sizes->num_entries,
+               sizes->width, H, params->num_q_heads / H, params->sm_scale * kLog2e, decay};
+  (void)hipGetLastError();
+  by_type_and_dim(params, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    const dim3 grid(2048), block(256);
+    if (kvq) hipLaunchKernelGGL((weights_kernel<T, true, D>), grid, block, 0, static_cast<hipStream_t>(stream), g);
+    else hipLaunchKernelGGL((weights_kernel<T, false, D>), grid, block, 0, static_cast<hipStream_t>(stream), g);
+  });
+  return hip_check("attention weights launch");
+}
+
+}  // namespace
+
+extern "C" halo_status_t halo_kv_page_weights(const void* k_pool, const halo_attn_params_t* params,
+                                              const halo_weight_sizes_t* sizes, const int32_t* page_ids,
+                                              const int32_t* seq_page_indptr, const int32_t* seq_start,
+                                              const int32_t* seq_end, const int32_t* row_indptr, const int32_t* rows,
+                                              const int32_t* row_end, const void* q, const float* lse, float decay,
+                                              const float* weights, float* weights_out, int32_t* error_flag,
+                                              void* stream) {
+  return page_weights(false, k_pool, params, sizes, page_ids, seq_page_indptr, seq_start, seq_end, row_indptr, rows,
+                      row_end, q, lse, decay, weights, weights_out, error_flag, stream);
+}
+
+extern "C" halo_status_t halo_kvq_page_weights(const void* k_pool, const halo_attn_params_t* params,
+                                               const halo_weight_sizes_t* sizes, const int32_t* page_ids,
+                                               const int32_t* seq_page_indptr, const int32_t* seq_start,
+                                               const int32_t* seq_end, const int32_t* row_indptr, const int32_t* rows,
+                                               const int32_t* row_end, const void* q, const float* lse, float decay,
+                                               const float* weights, float* weights_out, int32_t* error_flag,
+                                               void* stream) {
+  return page_weights(true, k_pool, params, sizes, page_ids, seq_page_indptr, seq_start, seq_end, row_indptr, rows,
+                      row_end, q, lse, decay, weights, weights_out, error_flag, stream);
+}

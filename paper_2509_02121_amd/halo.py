@@ -90,6 +90,9 @@ EXPORTED_SYMBOLS = (
     "halo_plan_kvq_workspace_bytes", "halo_prefix_attn_decode_kvq", "halo_prefix_attn_prefill_kvq",
     "halo_kvq_pool_bytes", "halo_kvq_page_scatter_kv", "halo_kvq_page_gather_kv", "halo_kvq_page_copy",
     "halo_kv_step_tables", "halo_rope_params_default", "halo_rope_turns", "halo_rope_qk",
+    "halo_kv_page_weights", "halo_kvq_page_weights", "halo_kv_evict_select", "halo_kv_page_keep_kv",
+    "halo_kvq_page_keep_kv", "halo_kv_release_pages",
+    "halo_beam_workspace_bytes", "halo_beam_select", "halo_beam_tables_workspace_bytes", "halo_kv_beam_tables",
     "halo_prefix_tree_build", "halo_prefix_tree_get", "halo_prefix_tree_destroy",
     "halo_status_string", "halo_last_error_message", "halo_last_error_status",
 )
@@ -109,6 +112,30 @@ class StepSizes(ctypes.Structure):
 class _StepTables(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("seq_page_indptr", "page_ids", "seq_start", "seq_count", "seq_end",
                                                "in_token_offset", "positions", "slots", "free_next")]
+
+
+class WeightSizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_seqs", "num_rows", "num_entries", "width")]
+
+
+class EvictSizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_seqs", "num_kv_heads", "width", "budget", "trigger", "sinks",
+                                              "recent")]
+
+
+class BeamSizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_items", "num_beams", "vocab", "num_best")] + [
+        ("logits_stride", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class BeamTableSizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_items", "num_beams", "page_size", "table_width", "num_free",
+                                              "parents_stride")]
+
+
+class _BeamTables(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("block_table", "seq_len", "free_pages", "free_next", "copy_src",
+                                               "copy_dst")]
 
 
 class RopeParams(ctypes.Structure):
@@ -220,6 +247,29 @@ def load_library(require_gpu=False):
                                  ctypes.c_int32, ctypes.c_int, vp, ctypes.c_int64, vp, ctypes.c_int64, vp,
                                  ctypes.c_int64, vp, ctypes.c_int64, vp]
     lib.halo_rope_qk.restype = ctypes.c_int
+    for name in ("halo_kv_page_weights", "halo_kvq_page_weights"):
+        fn = getattr(lib, name)
+        fn.argtypes = [vp, ctypes.POINTER(AttnParams), ctypes.POINTER(WeightSizes), vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                       ctypes.c_float, vp, vp, vp, vp]
+        fn.restype = ctypes.c_int
+    lib.halo_kv_evict_select.argtypes = [ctypes.POINTER(EvictSizes), vp, vp, vp, vp, vp, vp, vp]
+    lib.halo_kv_evict_select.restype = ctypes.c_int
+    for name in ("halo_kv_page_keep_kv", "halo_kvq_page_keep_kv"):
+        fn = getattr(lib, name)
+        fn.argtypes = [vp, vp, ctypes.POINTER(AttnParams), vp, vp, vp, vp, vp, ctypes.c_int32, vp, vp, ctypes.c_int32,
+                       vp, vp]
+        fn.restype = ctypes.c_int
+    lib.halo_kv_release_pages.argtypes = [ctypes.POINTER(StepSizes), vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.halo_kv_release_pages.restype = ctypes.c_int
+    lib.halo_beam_workspace_bytes.argtypes = [ctypes.POINTER(BeamSizes)]
+    lib.halo_beam_workspace_bytes.restype = ctypes.c_int64
+    lib.halo_beam_select.argtypes = [ctypes.POINTER(BeamSizes), vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, sz, vp]
+    lib.halo_beam_select.restype = ctypes.c_int
+    lib.halo_beam_tables_workspace_bytes.argtypes = [ctypes.POINTER(BeamTableSizes)]
+    lib.halo_beam_tables_workspace_bytes.restype = ctypes.c_int64
+    lib.halo_kv_beam_tables.argtypes = [ctypes.POINTER(BeamTableSizes), vp, vp, vp, vp, vp, ctypes.POINTER(_BeamTables),
+                                        vp, sz, vp, vp]
+    lib.halo_kv_beam_tables.restype = ctypes.c_int
     lib.halo_prefix_tree_build.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(vp),
                                            ctypes.POINTER(PrefixTreeInfo)]
     lib.halo_prefix_tree_build.restype = ctypes.c_int
@@ -1064,6 +1114,381 @@ def bind_rope_qk(q, k, positions, rope, q_out=None, k_out=None, stream=None):
     holds rope's angles."""
     load_library()
     return _bound(_LIB.halo_rope_qk, _rope_args(q, k, positions, rope, q_out, k_out, stream), rope.turns)
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _weights_args(kvq, weights, k_pool, params, page_ids, seq_page_indptr, seq_start, seq_end, q, lse, row_indptr,
+                  rows, row_end, decay, weights_out, error_flag, stream):
+    import torch
+    i32 = torch.int32
+    weights_out = weights if weights_out is None else weights_out
+    n = _page_lists(page_ids, seq_page_indptr)
+    heads, d = params.num_kv_heads, params.head_dim
+    for t, name in ((weights, "weights"), (weights_out, "weights_out")):
+        if t is None and decay == 0:
+            continue
+        _gpu(t, name, torch.float32)
+        if t.dim() != 3 or t.shape[0] < n or t.shape[1] != heads or t.shape[2] != weights_out.shape[2]:
+            raise ValueError(f"{name} must be [{n} or more, {heads}, tokens], got {tuple(t.shape)}")
+    if weights_out is None:
+        raise TypeError("weights_out must be a torch tensor where weights is None")
+    if kvq:
+        _gpu(k_pool, "k_pool", torch.uint8, kvq_pool_bytes(params, HALO_POOL_K))
+    else:
+        _gpu(k_pool, "k_pool", _torch_dtype(params.kv_dtype), _pool_elems(params))
+    if seq_start is not None:
+        _gpu(seq_start, "seq_start", i32, n)
+    _gpu(seq_end, "seq_end", i32, n)
+    _gpu(q, "q", _torch_dtype(params.kv_dtype))
+    if q.dim() != 3 or tuple(q.shape[1:]) != (params.num_q_heads, d):
+        raise ValueError(f"q must be [tokens, {params.num_q_heads}, {d}], got {tuple(q.shape)}")
+    _gpu(lse, "lse", torch.float32, q.shape[0] * params.num_q_heads)
+    lists = [(t, name) for t, name in ((rows, "rows"), (row_end, "row_end")) if t is not None]
+    entries = min((t.numel() for t, _ in lists), default=q.shape[0])
+    if row_indptr is not None:
+        _gpu(row_indptr, "row_indptr", i32, n + 1)
+    for t, name in lists:
+        _gpu(t, name, i32, n if row_indptr is None else 0)
+    used = [weights_out, k_pool, page_ids, seq_page_indptr, seq_end, q, lse]
+    used += [t for t in (weights, seq_start, row_indptr, rows, row_end) if t is not None]
+    _one_gpu(used + _flag(error_flag), stream)
+    sizes = WeightSizes(n, q.shape[0], entries, weights_out.shape[2])
+    return (k_pool.data_ptr(), ctypes.byref(params), ctypes.byref(sizes), page_ids.data_ptr(),
+            seq_page_indptr.data_ptr(), _address(seq_start), seq_end.data_ptr(), _address(row_indptr), _address(rows),
+            _address(row_end), q.data_ptr(), lse.data_ptr(), float(decay), _address(weights), weights_out.data_ptr(),
+            _address(error_flag), _stream_handle(stream))
+
+
+def kv_page_weights(weights, k_pool, params, page_ids, seq_page_indptr, seq_start, seq_end, q, lse, row_indptr=None,
+                    rows=None, row_end=None, decay=1.0, weights_out=None, error_flag=None, stream=None):
+    """halo_kv_page_weights on torch tensors: the attention weight that q
+    [tokens, q heads, head_dim] (with the lse that attention gave) puts on each
+    cached token, added to decay * weights [sequences, kv heads, tokens], into
+    weights_out (None: in place)."""
+    load_library()
+    _check(_LIB.halo_kv_page_weights(*_weights_args(False, weights, k_pool, params, page_ids, seq_page_indptr,
+                                                    seq_start, seq_end, q, lse, row_indptr, rows, row_end, decay,
+                                                    weights_out, error_flag, stream)))
+
+
+def bind_kv_page_weights(weights, k_pool, params, page_ids, seq_page_indptr, seq_start, seq_end, q, lse,
+                         row_indptr=None, rows=None, row_end=None, decay=1.0, weights_out=None, error_flag=None,
+                         stream=None):
+    """kv_page_weights as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kv_page_weights,
+                  _weights_args(False, weights, k_pool, params, page_ids, seq_page_indptr, seq_start, seq_end, q, lse,
+                                row_indptr, rows, row_end, decay, weights_out, error_flag, stream))
+
+
+def kvq_page_weights(weights, k_pool, params, page_ids, seq_page_indptr, seq_start, seq_end, q, lse, row_indptr=None,
+                     rows=None, row_end=None, decay=1.0, weights_out=None, error_flag=None, stream=None):
+    """kv_page_weights over a 4-bit K pool (uint8, see alloc_kvq_pools)."""
+    load_library()
+    _check(_LIB.halo_kvq_page_weights(*_weights_args(True, weights, k_pool, params, page_ids, seq_page_indptr,
+                                                     seq_start, seq_end, q, lse, row_indptr, rows, row_end, decay,
+                                                     weights_out, error_flag, stream)))
+
+
+def bind_kvq_page_weights(weights, k_pool, params, page_ids, seq_page_indptr, seq_start, seq_end, q, lse,
+                          row_indptr=None, rows=None, row_end=None, decay=1.0, weights_out=None, error_flag=None,
+                          stream=None):
+    """kvq_page_weights as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kvq_page_weights,
+                  _weights_args(True, weights, k_pool, params, page_ids, seq_page_indptr, seq_start, seq_end, q, lse,
+                                row_indptr, rows, row_end, decay, weights_out, error_flag, stream))
+
+
+def _evict_args(weights, seq_len, kept, new_len, trigger, sinks, recent, weights_out, error_flag, stream):
+    import torch
+    weights_out = weights if weights_out is None else weights_out
+    _gpu(weights, "weights", torch.float32)
+    if weights.dim() != 3:
+        raise ValueError(f"weights must be [sequences, kv heads, tokens], got {tuple(weights.shape)}")
+    _gpu(weights_out, "weights_out", torch.float32)
+    if weights_out.shape != weights.shape:
+        raise ValueError(f"weights_out must be {tuple(weights.shape)}, got {tuple(weights_out.shape)}")
+    n, heads, width = weights.shape
+    _gpu(seq_len, "seq_len", torch.int32, n)
+    _gpu(new_len, "new_len", torch.int32, n)
+    _gpu(kept, "kept", torch.int32)
+    if kept.dim() != 3 or tuple(kept.shape[:2]) != (n, heads):
+        raise ValueError(f"kept must be [{n}, {heads}, budget], got {tuple(kept.shape)}")
+    budget = kept.shape[2]
+    _one_gpu([weights, weights_out, seq_len, kept, new_len] + _flag(error_flag), stream)
+    sizes = EvictSizes(n, heads, width, budget, budget if trigger is None else trigger, sinks, recent)
+    return (ctypes.byref(sizes), weights.data_ptr(), seq_len.data_ptr(), kept.data_ptr(), weights_out.data_ptr(),
+            new_len.data_ptr(), _address(error_flag), _stream_handle(stream))
+
+
+def kv_evict_select(weights, seq_len, kept, new_len, trigger=None, sinks=0, recent=0, weights_out=None,
+                    error_flag=None, stream=None):
+    """halo_kv_evict_select on torch tensors: which tokens each head of a
+    sequence of more than `trigger` (None: the budget) tokens keeps, into kept
+    [sequences, kv heads, budget], and their weights into weights_out (None: in
+    place)."""
+    load_library()
+    _check(_LIB.halo_kv_evict_select(*_evict_args(weights, seq_len, kept, new_len, trigger, sinks, recent, weights_out,
+                                                  error_flag, stream)))
+
+
+def bind_kv_evict_select(weights, seq_len, kept, new_len, trigger=None, sinks=0, recent=0, weights_out=None,
+                         error_flag=None, stream=None):
+    """kv_evict_select as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kv_evict_select,
+                  _evict_args(weights, seq_len, kept, new_len, trigger, sinks, recent, weights_out, error_flag,
+                              stream))
+
+
+def _keep_args(kvq, k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, new_len, kept, dst_page_ids,
+               dst_page_indptr, error_flag, stream):
+    import torch
+    if (dst_page_ids is None) != (dst_page_indptr is None):
+        raise ValueError("dst_page_ids and dst_page_indptr are given together")
+    if dst_page_ids is None:
+        dst_page_ids, dst_page_indptr = page_ids, seq_page_indptr
+    if kvq:
+        _kvq_pools(k_pool, v_pool, params)
+    else:
+        for t, name in ((k_pool, "k_pool"), (v_pool, "v_pool")):
+            _gpu(t, name, _torch_dtype(params.kv_dtype), _pool_elems(params))
+    n = _page_lists(page_ids, seq_page_indptr)
+    _gpu(dst_page_ids, "dst_page_ids", torch.int32)
+    _gpu(dst_page_indptr, "dst_page_indptr", torch.int32, n + 1)
+    _gpu(seq_len, "seq_len", torch.int32, n)
+    _gpu(new_len, "new_len", torch.int32, n)
+    _gpu(kept, "kept", torch.int32)
+    if kept.dim() != 3 or kept.shape[0] < n or kept.shape[1] != params.num_kv_heads:
+        raise ValueError(f"kept must be [{n} or more, {params.num_kv_heads}, budget], got {tuple(kept.shape)}")
+    _one_gpu([k_pool, v_pool, page_ids, seq_page_indptr, seq_len, new_len, kept, dst_page_ids, dst_page_indptr] +
+             _flag(error_flag), stream)
+    return (k_pool.data_ptr(), v_pool.data_ptr(), ctypes.byref(params), page_ids.data_ptr(),
+            seq_page_indptr.data_ptr(), seq_len.data_ptr(), new_len.data_ptr(), kept.data_ptr(), kept.shape[2],
+            dst_page_ids.data_ptr(), dst_page_indptr.data_ptr(), n, _address(error_flag), _stream_handle(stream))
+
+
+def kv_page_keep_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, new_len, kept, dst_page_ids=None,
+                    dst_page_indptr=None, error_flag=None, stream=None):
+    """halo_kv_page_keep_kv on torch tensors: the tokens kept [sequences, kv
+    heads, budget] of each page list into another one (None: to the front of
+    their own)."""
+    load_library()
+    _check(_LIB.halo_kv_page_keep_kv(*_keep_args(False, k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len,
+                                                 new_len, kept, dst_page_ids, dst_page_indptr, error_flag, stream)))
+
+
+def bind_kv_page_keep_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, new_len, kept, dst_page_ids=None,
+                         dst_page_indptr=None, error_flag=None, stream=None):
+    """kv_page_keep_kv as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kv_page_keep_kv,
+                  _keep_args(False, k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, new_len, kept,
+                             dst_page_ids, dst_page_indptr, error_flag, stream))
+
+
+def kvq_page_keep_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, new_len, kept, dst_page_ids=None,
+                     dst_page_indptr=None, error_flag=None, stream=None):
+    """kv_page_keep_kv in 4-bit pools (uint8, see alloc_kvq_pools)."""
+    load_library()
+    _check(_LIB.halo_kvq_page_keep_kv(*_keep_args(True, k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len,
+                                                  new_len, kept, dst_page_ids, dst_page_indptr, error_flag, stream)))
+
+
+def bind_kvq_page_keep_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, new_len, kept, dst_page_ids=None,
+                          dst_page_indptr=None, error_flag=None, stream=None):
+    """kvq_page_keep_kv as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kvq_page_keep_kv,
+                  _keep_args(True, k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, new_len, kept,
+                             dst_page_ids, dst_page_indptr, error_flag, stream))
+
+
+def _release_args(block_table, seq_len, new_len, free_pages, free_next, free_pages_out, free_next_out, error_flag,
+                  stream):
+    import torch
+    _gpu(block_table, "block_table", torch.int32)
+    if block_table.dim() != 2:
+        raise ValueError(f"block_table must be [sequences, pages], got {tuple(block_table.shape)}")
+    n = block_table.shape[0]
+    _gpu(seq_len, "seq_len", torch.int32, n)
+    _gpu(new_len, "new_len", torch.int32, n)
+    _gpu(free_pages, "free_pages", torch.int32)
+    _gpu(free_pages_out, "free_pages_out", torch.int32, free_pages.numel())
+    _gpu(free_next, "free_next", torch.int32, 1)
+    _gpu(free_next_out, "free_next_out", torch.int32, 1)
+    _one_gpu([block_table, seq_len, new_len, free_pages, free_next, free_pages_out, free_next_out] +
+             _flag(error_flag), stream)
+    sizes = StepSizes(n, 16, block_table.shape[1], free_pages.numel(), 0, 0)
+    return (ctypes.byref(sizes), block_table.data_ptr(), seq_len.data_ptr(), new_len.data_ptr(), free_pages.data_ptr(),
+            free_next.data_ptr(), free_pages_out.data_ptr(), free_next_out.data_ptr(), _address(error_flag),
+            _stream_handle(stream))
+
+
+def kv_release_pages(block_table, seq_len, new_len, free_pages, free_next, free_pages_out, free_next_out,
+                     error_flag=None, stream=None):
+    """halo_kv_release_pages on torch tensors: the pages of each row of
+    block_table [sequences, pages] past its new length go back to the free list
+    (free_pages_out may be free_pages)."""
+    load_library()
+    _check(_LIB.halo_kv_release_pages(*_release_args(block_table, seq_len, new_len, free_pages, free_next,
+                                                     free_pages_out, free_next_out, error_flag, stream)))
+
+
+def bind_kv_release_pages(block_table, seq_len, new_len, free_pages, free_next, free_pages_out, free_next_out,
+                          error_flag=None, stream=None):
+    """kv_release_pages as a zero-argument callable (see bind_kv_page_scatter)."""
+    load_library()
+    return _bound(_LIB.halo_kv_release_pages, _release_args(block_table, seq_len, new_len, free_pages, free_next,
+                                                            free_pages_out, free_next_out, error_flag, stream))
+
+
+def _workspace(nbytes, device):
+    import torch
+    if nbytes < 0:
+        _check(_LIB.halo_last_error_status())
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+class BeamSelect:
+    """The outputs of beam_select (torch tensors on one GPU) for num_items
+    requests of num_beams beams: scores, tokens and parents [items, num_best]
+    (None: num_beams), and its workspace. Calls with one object write the same
+    arrays: those on several streams, or of several graphs that may run beside
+    each other, take an object each."""
+
+    def __init__(self, num_items, num_beams, vocab, num_best=None, device="cuda"):
+        import torch
+        lib = load_library()
+        self.num_items, self.num_beams, self.vocab = int(num_items), int(num_beams), int(vocab)
+        self.num_best = self.num_beams if num_best is None else int(num_best)
+        sizes = BeamSizes(self.num_items, self.num_beams, self.vocab, self.num_best, self.vocab, HALO_F32)
+        self.workspace = _workspace(lib.halo_beam_workspace_bytes(ctypes.byref(sizes)), device)
+        shape = (self.num_items, self.num_best)
+        self.scores = torch.zeros(shape, dtype=torch.float32, device=device)
+        self.tokens, self.parents = (torch.zeros(shape, dtype=torch.int32, device=device) for _ in range(2))
+
+
+def _beam_select_args(out, logits, scores, ended, end_token, stream):
+    import torch
+    rows = out.num_items * out.num_beams
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch tensor")
+    if logits.dim() != 2 or tuple(logits.shape) != (rows, out.vocab):
+        raise ValueError(f"logits must be [{rows}, {out.vocab}], got {tuple(logits.shape)}")
+    if logits.numel() and (logits.stride(1) != 1 and out.vocab > 1):
+        raise ValueError("the logits of a row must be contiguous")
+    code = _dtype_code(logits.dtype)
+    stride = logits.stride(0) if rows > 1 else out.vocab
+    if stride < out.vocab:
+        raise ValueError("the rows of logits must not overlap")
+    if not logits.is_cuda:
+        raise ValueError("logits must be on the GPU")
+    _gpu(scores, "scores", torch.float32, rows)
+    if ended is not None:
+        _gpu(ended, "ended", torch.int32, rows)
+    best = out.num_items * out.num_best
+    _gpu(out.scores, "out.scores", torch.float32, best)
+    _gpu(out.tokens, "out.tokens", torch.int32, best)
+    _gpu(out.parents, "out.parents", torch.int32, best)
+    _gpu(out.workspace, "out.workspace")
+    _one_gpu([logits, scores, out.scores, out.tokens, out.parents, out.workspace] +
+             ([] if ended is None else [ended]), stream)
+    sizes = BeamSizes(out.num_items, out.num_beams, out.vocab, out.num_best, stride, code)
+    return (ctypes.byref(sizes), logits.data_ptr(), scores.data_ptr(), _address(ended), int(end_token),
+            out.scores.data_ptr(), out.tokens.data_ptr(), out.parents.data_ptr(), out.workspace.data_ptr(),
+            _nbytes(out.workspace), _stream_handle(stream))
+
+
+def beam_select(out, logits, scores, ended=None, end_token=0, stream=None):
+    """halo_beam_select on torch tensors: fills `out` (a BeamSelect) from logits
+    [items * beams, vocab] (rows any stride apart, bf16 or fp32), scores (float32)
+    and ended (int32, beams that offer only end_token)."""
+    load_library()
+    _check(_LIB.halo_beam_select(*_beam_select_args(out, logits, scores, ended, end_token, stream)))
+
+
+def bind_beam_select(out, logits, scores, ended=None, end_token=0, stream=None):
+    """beam_select as a zero-argument callable (see bind_kv_page_scatter), which
+    holds the arrays of `out`."""
+    load_library()
+    return _bound(_LIB.halo_beam_select, _beam_select_args(out, logits, scores, ended, end_token, stream),
+                  list(vars(out).values()))
+
+
+class BeamTables:
+    """The outputs of kv_beam_tables (torch tensors on one GPU): block_table
+    [items * beams, pages], seq_len, free_pages and free_next as the next step
+    takes them, copy_src and copy_dst for kv_page_copy (without an error flag: rows
+    that copy nothing hold -1), and its workspace. A call's outputs must not be
+    its inputs: two objects take turns, or the outputs are copied. Calls with one
+    object write the same arrays."""
+
+    def __init__(self, num_items, num_beams, table_width, num_free, device="cuda"):
+        import torch
+
+        def ints(*shape):
+            return torch.full(shape, -1, dtype=torch.int32, device=device)
+
+        lib = load_library()
+        self.num_items, self.num_beams = int(num_items), int(num_beams)
+        self.table_width, self.num_free = int(table_width), int(num_free)
+        rows = self.num_items * self.num_beams
+        sizes = BeamTableSizes(self.num_items, self.num_beams, 16, self.table_width, self.num_free, self.num_beams)
+        self.workspace = _workspace(lib.halo_beam_tables_workspace_bytes(ctypes.byref(sizes)), device)
+        self.block_table, self.seq_len = ints(rows, self.table_width), ints(rows)
+        self.free_pages, self.free_next = ints(self.num_free), ints(1)
+        self.copy_src, self.copy_dst = ints(rows), ints(rows)
+
+
+def _beam_tables_args(out, parents, seq_len, block_table, free_pages, free_next, error_flag, stream):
+    import torch
+    i32, n, w = torch.int32, out.num_items, out.num_beams
+    rows = n * w
+    _gpu(parents, "parents", i32)
+    if parents.dim() != 2 or parents.shape[0] != n or parents.shape[1] < w:
+        raise ValueError(f"parents must be [{n}, {w} or more], got {tuple(parents.shape)}")
+    _gpu(seq_len, "seq_len", i32, rows)
+    _gpu(block_table, "block_table", i32)
+    if tuple(block_table.shape) != (rows, out.table_width):
+        raise ValueError(f"block_table must be [{rows}, {out.table_width}], got {tuple(block_table.shape)}")
+    _gpu(free_pages, "free_pages", i32)
+    if free_pages.numel() != out.num_free:
+        raise ValueError(f"free_pages has {free_pages.numel()} elements, expected {out.num_free}")
+    _gpu(free_next, "free_next", i32, 1)
+    ptrs, used = {}, [parents, seq_len, block_table, free_pages, free_next, out.workspace]
+    for name, numel in (("block_table", rows * out.table_width), ("seq_len", rows), ("free_pages", out.num_free),
+                        ("free_next", 1), ("copy_src", rows), ("copy_dst", rows)):
+        t = _gpu(getattr(out, name), f"out.{name}", i32, numel)
+        ptrs[name] = t.data_ptr()
+        used.append(t)
+    _gpu(out.workspace, "out.workspace")
+    _one_gpu(used + _flag(error_flag), stream)
+    sizes = BeamTableSizes(n, w, 16, out.table_width, out.num_free, parents.shape[1])
+    return (ctypes.byref(sizes), parents.data_ptr(), seq_len.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+            free_next.data_ptr(), ctypes.byref(_BeamTables(**ptrs)), out.workspace.data_ptr(), _nbytes(out.workspace),
+            _address(error_flag), _stream_handle(stream))
+
+
+def kv_beam_tables(out, parents, seq_len, block_table, free_pages, free_next, error_flag=None, stream=None):
+    """halo_kv_beam_tables on torch tensors: fills `out` (a BeamTables) with the
+    rows of the page table after every beam has become a child of parents
+    [items, beams or more] (those of a BeamSelect, best first)."""
+    load_library()
+    _check(_LIB.halo_kv_beam_tables(*_beam_tables_args(out, parents, seq_len, block_table, free_pages, free_next,
+                                                       error_flag, stream)))
+
+
+def bind_kv_beam_tables(out, parents, seq_len, block_table, free_pages, free_next, error_flag=None, stream=None):
+    """kv_beam_tables as a zero-argument callable (see bind_kv_page_scatter), which
+    holds the arrays of `out`."""
+    load_library()
+    return _bound(_LIB.halo_kv_beam_tables, _beam_tables_args(out, parents, seq_len, block_table, free_pages,
+                                                              free_next, error_flag, stream), list(vars(out).values()))
 
 
 class PrefixAttention:
