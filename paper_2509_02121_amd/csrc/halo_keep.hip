@@ -39,35 +39,58 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kEvictThreads = 1024;
+constexpr int kBins = 2048;      // 11 bits
+constexpr int kListed = 4096;    // keys of one bin that are looked at in LDS
 
-// The sum of x over the workgroup, and of the threads before this one.
-__device__ __forceinline__ int block_exclusive_sum(int x, int& total, int (&sums)[kEvictThreads / 64]) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int upto = wave_inclusive_sum(x);
-  __syncthreads();
+// The largest of the kBins counts' places with `left` or more at or above it, and how
+// many of `left` fall into it, by the whole workgroup.
+template <int W>
+__device__ __forceinline__ void find_bin(const int (&count)[kBins], int (&sums)[W], int (&found)[2], int& left, int& bin) {
+  constexpr int N = kBins / (64 * W);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  int c[N], mine = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) mine += c[j] = count[kBins - 1 - (N * tid + j)];
+  const int upto = wave_inclusive_sum(mine);
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
-  int before = 0;
-  total = 0;
+  int above = upto - mine;
 #pragma unroll
-  for (int w = 0; w < kEvictThreads / 64; ++w) {
-    before += w < wave ? sums[w] : 0;
-    total += sums[w];
+  for (int v = 0; v < W; ++v) above += v < wave ? sums[v] : 0;
+  if (above < left && above + mine >= left) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (above < left && above + c[j] >= left) {
+        found[0] = kBins - 1 - (N * tid + j);
+        found[1] = left - above;
+        above = INT32_MAX / 2;
+      } else {
+        above += c[j];
+      }
+    }
   }
-  return before + upto - x;
+  __syncthreads();
+  bin = found[0];
+  left = found[1];
 }
 
-// A workgroup for each (sequence, head). Of the tokens between the sinks and the recent
-// ones m stay: the m-th largest key is found byte by byte from the top, by
-// counting how many keys with the bytes found so far have each next one. Then the
-// tokens are passed in order: those of a larger key stay, and of those of the same
-// key the first ones.
-__global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a) {
-  __shared__ int count[256];
-  __shared__ int sums[kEvictThreads / 64];
-  __shared__ int found[2];
-  const int tid = threadIdx.x, H = a.s.num_kv_heads;
+// A workgroup of W waves for each (sequence, head); wave v has tokens v * 64 R .. + 64 R - 1 of
+// each chunk of 64 R W, R of them a lane, and a row of one chunk stays in its
+// registers. Of the tokens between the sinks and the recent ones `left` stay. The
+// left-th largest key is found from the top: the keys are counted by their first 11
+// bits, and those of the bin that holds it, few as a rule, go to a list in LDS,
+// which the next 11 and the last 10 bits are counted from (a bin that
+// holds more is counted from the row again). Then the
+// tokens are written in order: those of a larger key stay, and of those of the same
+// key the first ones. A wave knows its places from what the waves before it count.
+template <int W, int R>
+__global__ __launch_bounds__(64 * W) void evict_kernel(EvictArgs a) {
+  constexpr int T = 64 * W, kChunk = T * R;
+  __shared__ int count[kBins];
+  __shared__ uint32_t list[kListed];
+  __shared__ int sums[W], stay[W], same[W];
+  __shared__ int found[2], listed;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, H = a.s.num_kv_heads;
   const int seq = (int)(blockIdx.x / H), h = (int)(blockIdx.x % H);
   const int len = a.seq_len[seq];
   const int64_t row = ((int64_t)seq * H + h) * a.s.width;
@@ -81,68 +104,138 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(EvictArgs a) {
   if (bad) return;
   if (len <= a.s.trigger) {
     if (a.weights != a.weights_out)
-      for (int t = tid; t < len; t += kEvictThreads) out[t] = w[t];
+      for (int t = tid; t < len; t += T) out[t] = w[t];
     return;
   }
-  const int lo = a.s.sinks, hi = len - a.s.recent;
-  int left = a.s.budget - a.s.sinks - a.s.recent;   // of the tokens lo .. hi - 1
-  uint32_t key = 0;   // the left-th largest key's bytes found so far
+  const bool one = len <= kChunk;
+  const int mine = wave * 64 * R + lane;   // a lane's first token of a chunk; the others are 64 apart
+  float x[R];
+  // the tokens of a chunk, and those of them between the sinks and the recent ones
+  int n, lo, hi;
+  auto load = [&](int64_t t0) {
+    const int64_t rest = len - t0;
+    n = (int)min((int64_t)kChunk, rest);
+    lo = (int)min(max((int64_t)a.s.sinks - t0, (int64_t)0), (int64_t)kChunk);
+    hi = (int)min(max(rest - a.s.recent, (int64_t)0), (int64_t)kChunk);
+    const float* at = w + t0 + mine;
+    if (n == kChunk) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) x[i] = at[64 * i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < R; ++i) x[i] = mine + 64 * i < n ? at[64 * i] : 0.f;
+    }
+  };
+  load(0);
+  int left = a.s.budget - a.s.sinks - a.s.recent;
   const bool chosen = left > 0;
+  uint32_t key = 0;   // the left-th largest key
   if (chosen) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      __syncthreads();
-      if (tid < 256) count[tid] = 0;
-      __syncthreads();
-      for (int t = lo + tid; t < hi; t += kEvictThreads) {
-        const uint32_t k = weight_key(w[t]);
-        if (shift == 24 || (k ^ key) >> (shift + 8) == 0) atomicAdd(&count[(k >> shift) & 255], 1);
-      }
-      __syncthreads();
-      // the largest byte with `left` or more keys at or above it
-      if (tid < 64) {
-        int c[4], mine = 0;
+    // counts the keys that begin with `key` above bit `top` by the bits from `shift` up to there
+    auto count_row = [&](int top, int shift, int bins) {
+      for (int64_t t0 = 0; t0 < len; t0 += kChunk) {
+        if (!one) load(t0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mine += c[j] = count[255 - (4 * tid + j)];
-        const int upto = wave_inclusive_sum(mine);
-        int above = upto - mine;
-        if (above < left && upto >= left) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (above < left && above + c[j] >= left) {
-              found[0] = 255 - (4 * tid + j);
-              found[1] = left - above;
-              above = INT32_MAX / 2;
-            } else {
-              above += c[j];
-            }
-          }
+        for (int i = 0; i < R; ++i) {
+          const int t = mine + 64 * i;
+          const uint32_t k = weight_key(x[i]);
+          if (t >= lo && t < hi && (top == 32 || (k ^ key) >> (top & 31) == 0)) atomicAdd(&count[(k >> shift) & (bins - 1)], 1);
         }
       }
+    };
+    int bin;
+    for (int i = tid; i < kBins; i += T) count[i] = 0;
+    if (tid == 0) listed = 0;
+    __syncthreads();
+    count_row(32, 21, kBins);
+    __syncthreads();
+    find_bin<W>(count, sums, found, left, bin);
+    key = (uint32_t)bin << 21;
+    const int in_bin = count[bin];
+    const bool short_list = in_bin <= kListed;
+    if (short_list) {
+      for (int64_t t0 = 0; t0 < len; t0 += kChunk) {
+        if (!one) load(t0);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const int t = mine + 64 * i;
+          const uint32_t k = weight_key(x[i]);
+          if (t >= lo && t < hi && (k ^ key) >> 21 == 0) list[atomicAdd(&listed, 1)] = k;
+        }
+      }
+    }
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+      const int top = step == 0 ? 21 : 10, shift = step == 0 ? 10 : 0, bins = step == 0 ? kBins : kBins / 2;
+      __syncthreads();   // (the counts have been read, the list is whole)
+      for (int i = tid; i < kBins; i += T) count[i] = 0;
       __syncthreads();
-      key |= (uint32_t)found[0] << shift;
-      left = found[1];
+      if (short_list) {
+        for (int i = tid; i < in_bin; i += T) {
+          const uint32_t k = list[i];
+          if ((k ^ key) >> top == 0) atomicAdd(&count[(k >> shift) & (bins - 1)], 1);
+        }
+      } else {
+        count_row(top, shift, bins);
+      }
+      __syncthreads();
+      find_bin<W>(count, sums, found, left, bin);
+      key |= (uint32_t)bin << shift;
     }
   }
-  // in order: of the tokens with this key the first `left`
   int32_t* kept = a.kept + ((int64_t)seq * H + h) * a.s.budget;
-  int done = 0, equal_done = 0;
-  for (int t0 = 0; t0 < len; t0 += kEvictThreads) {
-    const int t = t0 + tid;
-    const bool in = t < len, between = t >= lo && t < hi;
-    const float x = in ? w[t] : 0.f;
-    const uint32_t k = weight_key(x);
-    const bool equal = chosen && in && between && k == key;
-    int equals, total;
-    const int rank = block_exclusive_sum(equal, equals, sums);
-    const bool keep = in && (!between || (chosen && (k > key || (equal && equal_done + rank < left))));
-    const int at = done + block_exclusive_sum(keep, total, sums);
-    // (every read of this round is done: the places written are behind them)
-    if (keep && at < a.s.budget) {
-      kept[at] = t;
-      out[at] = x;
+  int at = 0;   // tokens written so far; left: of the ones with the key still to take
+  for (int64_t t0 = 0; t0 < len; t0 += kChunk) {
+    if (!one) load(t0);
+    // what stays whatever its order, and those of the key
+    int n_stay = 0, n_same = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int t = mine + 64 * i;
+      const uint32_t k = weight_key(x[i]);
+      const bool between = t >= lo && t < hi;
+      n_stay += __popcll(__ballot(t < n && (!between || (chosen && k > key))));
+      n_same += __popcll(__ballot(between && chosen && k == key));
     }
-    done += total;
-    equal_done += equals;
+    if (lane == 0) {
+      stay[wave] = n_stay;
+      same[wave] = n_same;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();   // (every read of this chunk has ended: in place, what is written lies before the next one)
+    int to = at, rest = left;
+#pragma unroll
+    for (int v = 0; v < W; ++v) {
+      const int take = min(same[v], left);
+      if (v < wave) {
+        to += stay[v] + take;
+        rest -= take;
+      }
+      at += stay[v] + take;
+      left -= take;
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int t = mine + 64 * i;
+      const uint32_t k = weight_key(x[i]);
+      const bool between = t >= lo && t < hi;
+      const bool equal = between && chosen && k == key;
+      const uint64_t equals = __ballot(equal);
+      bool keep = t < n && (!between || (chosen && k > key));
+      if (equals) {
+        const int rank = __builtin_amdgcn_mbcnt_hi((uint32_t)(equals >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)equals, 0));
+        keep |= equal && rank < rest;
+        rest -= min((int)__popcll(equals), rest);
+      }
+      const uint64_t keeps = __ballot(keep);
+      if (keep) {
+        const int place = to + __builtin_amdgcn_mbcnt_hi((uint32_t)(keeps >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)keeps, 0));
+        kept[place] = (int32_t)(t0 + t);
+        out[place] = x[i];
+      }
+      to += __popcll(keeps);
+    }
+    __syncthreads();   // (the counts are overwritten)
   }
 }
 
@@ -160,160 +253,314 @@ struct KeepArgs {
   const int32_t* dst_page_indptr;
   int32_t* error_flag;
   int64_t num_pool_pages;
-  int32_t num_kv_heads, kept_width;
-  bool in_place;
+  int32_t num_seqs, num_kv_heads, kept_width;
 };
 
-// Where one token of a sequence comes from.
-struct Source {
-  int64_t page;   // -1: nowhere
-  int slot;       // its place in the page
+// A sequence as the call gives it.
+struct KeepSeq {
+  int len, count, base, to;
+  bool bad, whole;
+  __device__ __forceinline__ KeepSeq(const KeepArgs& a, int seq) {
+    len = a.seq_len[seq];
+    count = a.new_len[seq];
+    base = a.seq_page_indptr[seq];
+    to = a.dst_page_indptr[seq];
+    const int64_t have = (int64_t)(a.seq_page_indptr[seq + 1] - base) * 16;
+    const int64_t room = (int64_t)(a.dst_page_indptr[seq + 1] - to) * 16;
+    bad = len < 0 || count < 0 || count > len || len > have || count > room || (count < len && count > a.kept_width);
+    whole = count == len;
+  }
 };
 
+// One (page, head) tile of a new list, and where its 16 tokens come from: lanes 0 .. 15
+// have a token each, the others repeat them. The kept indices, the source pages'
+// ids and the tokens are loads that need each other, so each is a step of its own, and
+// a wave takes the first ones of its next tiles before the last of this one.
+struct TileSource {
+  int base, len, h;
+  int token;         // of the sequence; -1: none is to come here
+  int page, slot;    // page -1: the place stays as it is
+  int dst_page;
+  bool asked;
+  __device__ __forceinline__ void find_tokens(const KeepArgs& a, const KeepSeq& s, int seq, int head, int p, int lane) {
+    base = s.base;
+    len = s.len;
+    h = head;
+    dst_page = a.dst_page_ids[s.to + p];
+    const int j = 16 * p + (lane & 15);
+    token = j;
+    if (j >= s.count) token = -1;
+    else if (!s.whole) token = a.kept[((int64_t)seq * a.num_kv_heads + head) * a.kept_width + j];
+    if (j < s.count && token < 0) token = -2;
+  }
+  __device__ __forceinline__ void find_pages(const KeepArgs& a) {
+    page = -1;
+    slot = token & 15;
+    asked = dst_page >= 0 && dst_page < a.num_pool_pages && token >= 0 && token < len;
+    if (asked) page = a.page_ids[base + token / 16];
+    else if (token != -1 && a.error_flag) a.error_flag[0] = 1;
+  }
+  __device__ __forceinline__ void check(const KeepArgs& a) {
+    if (asked && (page < 0 || page >= a.num_pool_pages)) {
+      page = -1;
+      if (a.error_flag) a.error_flag[0] = 1;
+    }
+  }
+};
+
+__device__ __forceinline__ int lane_of(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
+// K tiles: a token's dims lie in 16-byte units (4-bit codes: units of D / 8 bytes), a unit's 16 tokens next to
+// each other. Lane (token, g) moves units g, g + 4, ... of its token.
 template <typename T, bool KVQ, int D>
-struct KeepFormat {
-  static constexpr int kK = KVQ ? kvq_k_tile<D>() : 16 * D * (int)sizeof(T);
-  static constexpr int kV = KVQ ? kvq_v_tile<D>() : 16 * D * (int)sizeof(T);
+struct KTile {
+  static constexpr int kUnit = KVQ ? D / 8 : 16;
+  static constexpr int kUnits = KVQ ? 4 : D * (int)sizeof(T) / 16;
+  static constexpr int kBytes = KVQ ? kvq_k_tile<D>() : 16 * D * (int)sizeof(T);
+  using Unit = typename std::conditional<kUnit == 16, u32x4_t, uint64_t>::type;
+  using Scale = typename std::conditional<D == 128, uint32_t, uint16_t>::type;
+  Unit x[kUnits / 4];
+  Scale scale;
+  __device__ __forceinline__ void load(const KeepArgs& a, const TileSource& s, int lane) {
+    if (s.page < 0) return;
+    const uint8_t* src = a.k_pool + ((int64_t)s.page * a.num_kv_heads + s.h) * kBytes;
+#pragma unroll
+    for (int i = 0; i < kUnits / 4; ++i)
+      x[i] = *reinterpret_cast<const Unit*>(src + (((lane >> 4) + 4 * i) * 16 + s.slot) * kUnit);
+    if constexpr (KVQ) scale = reinterpret_cast<const Scale*>(src + D * 8)[s.slot];
+  }
+  __device__ __forceinline__ void store(const KeepArgs& a, const TileSource& s, int lane) const {
+    if (s.page < 0) return;
+    uint8_t* dst = a.k_pool + ((int64_t)s.dst_page * a.num_kv_heads + s.h) * kBytes;
+#pragma unroll
+    for (int i = 0; i < kUnits / 4; ++i)
+      *reinterpret_cast<Unit*>(dst + (((lane >> 4) + 4 * i) * 16 + (lane & 15)) * kUnit) = x[i];
+    if constexpr (KVQ)
+      if (lane < 16) reinterpret_cast<Scale*>(dst + D * 8)[lane] = scale;
+  }
 };
 
-__device__ __forceinline__ int v_slot_of_token(int t) { return v_token_at_slot(t); }   // (its own inverse)
+// V tiles: a dim's 16 tokens lie next to each other, so a token is one element of
+// every row, and every row of each source page is read whole. A lane has the rows of
+// D / 64 dims. The tokens come from few pages, in order (a page's are next to each other): one
+// after the other, the page's rows are loaded and the tokens that are in it are
+// picked, the same slot in every lane, so that a row's word is chosen by a uniform index.
+template <typename T, bool KVQ, int D>
+struct VTile {
+  static constexpr int kBytes = 16 * D * (int)sizeof(T);
+  static constexpr int N = D / 64, W = 4 * (int)sizeof(T);   // rows a lane, words a row
+  typedef uint32_t words_t __attribute__((ext_vector_type(W)));
+  words_t x[N];
+  uint64_t live;   // the tokens that come from somewhere
+  // 16-byte loads and stores of a wave are contiguous. Of a bf16 tile's that gives each lane of
+  // a pair a half of two rows; they swap, so that the even one has row 64 n + lane / 2 whole and
+  // the odd one that row + 32.
+  static __device__ __forceinline__ void swap_halves(u32x4_t& p, u32x4_t& q, bool odd) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int got = __builtin_amdgcn_update_dpp(0, (int)(odd ? p[i] : q[i]), 0xB1, 0xf, 0xf, true);   // quad_perm 1,0,3,2
+      p[i] = odd ? (uint32_t)got : p[i];
+      q[i] = odd ? q[i] : (uint32_t)got;
+    }
+  }
+  static __device__ __forceinline__ void load_rows(const uint8_t* tile, int lane, words_t (&y)[N]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if constexpr (sizeof(T) == 2) {
+        u32x4_t p = reinterpret_cast<const u32x4_t*>(tile)[128 * n + lane];
+        u32x4_t q = reinterpret_cast<const u32x4_t*>(tile)[128 * n + 64 + lane];
+        swap_halves(p, q, lane & 1);
+        y[n] = __builtin_shufflevector(p, q, 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
+        y[n] = reinterpret_cast<const words_t*>(tile)[64 * n + lane];
+      }
+    }
+  }
+  __device__ __forceinline__ void load(const KeepArgs& a, const TileSource& s, int lane) {
+    live = __ballot(s.page >= 0) & 0xffff;
+    if (!live) return;
+    // (slots that get no token keep what they hold)
+    if (live != 0xffff) load_rows(a.v_pool + ((int64_t)s.dst_page * a.num_kv_heads + s.h) * kBytes, lane, x);
+    uint64_t rest = live;
+    while (rest) {
+      const int page = lane_of(s.page, __builtin_ctzll(rest));
+      const uint64_t here = __ballot(s.page == page) & rest;
+      rest &= ~here;
+      words_t y[N];
+      load_rows(a.v_pool + ((int64_t)page * a.num_kv_heads + s.h) * kBytes, lane, y);
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        if (!(here >> t & 1)) continue;
+        const int from = v_token_at_slot(lane_of(s.slot, t));   // (the map is its own inverse)
+        const int to = (t & 3) | ((t & 4) << 1) | ((t & 8) >> 1);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int n = 0; n < N; ++n) x[n][to] = y[n][from];
+        } else {
+          // half `from & 1` of a word becomes half `to & 1` of another
+          const uint32_t pick = to & 1 ? (from & 1 ? 0x07060100u : 0x05040100u) : (from & 1 ? 0x03020706u : 0x03020504u);
+#pragma unroll
+          for (int n = 0; n < N; ++n) x[n][to / 2] = __builtin_amdgcn_perm(y[n][from / 2], x[n][to / 2], pick);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(const KeepArgs& a, const TileSource& s, int lane) const {
+    if (!live) return;
+    uint8_t* dst = a.v_pool + ((int64_t)s.dst_page * a.num_kv_heads + s.h) * kBytes;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if constexpr (sizeof(T) == 2) {
+        u32x4_t p = __builtin_shufflevector(x[n], x[n], 0, 1, 2, 3), q = __builtin_shufflevector(x[n], x[n], 4, 5, 6, 7);
+        swap_halves(p, q, lane & 1);
+        reinterpret_cast<u32x4_t*>(dst)[128 * n + lane] = p;
+        reinterpret_cast<u32x4_t*>(dst)[128 * n + 64 + lane] = q;
+      } else {
+        reinterpret_cast<words_t*>(dst)[64 * n + lane] = x[n];
+      }
+    }
+  }
+};
 
-// A workgroup for each (sequence, head, pool), which goes through the new pages in
-// order. Kept indices are ascending, so what is written to a page has already been
-// read for every page before it, and the pages behind it read only what lies
-// further back: between the loads of a page and its stores there is one barrier,
-// and no other workgroup touches these tiles, so that it works in place.
+// 4-bit values: a word holds the codes of 8 slots of a dim, [D / 64][half][64 dims]. Of
+// every token the words of its half are loaded, all at once, and its code put into
+// place; a place that stays takes its own.
+template <typename T, int D>
+struct VTile<T, true, D> {
+  static constexpr int kBytes = kvq_v_tile<D>();
+  static constexpr int N = D / 64;
+  uint32_t x[N][2];
+  uint16_t scale;
+  bool any;
+  __device__ __forceinline__ void load(const KeepArgs& a, const TileSource& s, int lane) {
+    any = __ballot(s.page >= 0) != 0;
+    if (!any) return;
+    const int page = s.page >= 0 ? s.page : s.dst_page, slot = s.page >= 0 ? s.slot : lane & 15;
+    scale = reinterpret_cast<const uint16_t*>(a.v_pool + ((int64_t)page * a.num_kv_heads + s.h) * kBytes + D * 8)[v_token_at_slot(slot)];
+    uint32_t y[16][N];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      const uint8_t* src = a.v_pool + ((int64_t)lane_of(page, t) * a.num_kv_heads + s.h) * kBytes;
+      const int half = v_token_at_slot(lane_of(slot, t)) >> 3;
+#pragma unroll
+      for (int n = 0; n < N; ++n) y[t][n] = reinterpret_cast<const uint32_t*>(src)[(2 * n + half) * 64 + lane];
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n][0] = x[n][1] = 0;
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+      const int from = 4 * (v_token_at_slot(lane_of(slot, t)) & 7);
+      const int to = (t & 3) | ((t & 4) << 1) | ((t & 8) >> 1);
+#pragma unroll
+      for (int n = 0; n < N; ++n) x[n][to >> 3] |= (y[t][n] >> from & 15) << (4 * (to & 7));
+    }
+  }
+  __device__ __forceinline__ void store(const KeepArgs& a, const TileSource& s, int lane) const {
+    if (!any) return;
+    uint8_t* dst = a.v_pool + ((int64_t)s.dst_page * a.num_kv_heads + s.h) * kBytes;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) reinterpret_cast<uint32_t*>(dst)[(2 * n + half) * 64 + lane] = x[n][half];
+    if (lane < 16) reinterpret_cast<uint16_t*>(dst + D * 8)[v_token_at_slot(lane)] = scale;
+  }
+};
+
+// To other pages: the new lists' (slot, head) tiles are cut into equal runs, one a
+// wave, as in the gather; every other wave moves K tiles, the others V tiles. The ids of the
+// next two tiles are on their way while one is moved.
 template <typename T, bool KVQ, int D>
 __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
-  using Fmt = KeepFormat<T, KVQ, D>;
-  __shared__ int64_t from[16];   // byte offset of the source tile
-  __shared__ int at[16];         // place in it; -1: none
-  const int tid = threadIdx.x, H = a.num_kv_heads;
+  const int lane = threadIdx.x & 63, H = a.num_kv_heads;
+  const int first = a.dst_page_indptr[0];
+  const int64_t total = ((int64_t)a.dst_page_indptr[a.num_seqs] - first) * H;
+  const int64_t waves = (int64_t)gridDim.x * 2, wave = (int64_t)blockIdx.x * 2 + (threadIdx.x >> 7);
+  const bool values = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 1;
+  const int64_t per = (total + waves - 1) / waves;
+  const int64_t begin = wave * per;
+  int64_t left = min(total, begin + per) - begin;   // tiles of the run that are still to come
+  if (blockIdx.x == 0 && threadIdx.x < 64) {
+    // (a malformed sequence may have no new page to be found by)
+    for (int i = lane; i < a.num_seqs; i += 64)
+      if (KeepSeq(a, i).bad && a.error_flag) a.error_flag[0] = 1;
+  }
+  if (left <= 0) return;
+  int slot = first + (int)(begin / H), h = (int)(begin % H) - 1;
+  int seq = last_at_or_below(a.dst_page_indptr, a.num_seqs, slot, lane), next = a.dst_page_indptr[seq + 1];
+  KeepSeq s(a, seq);
+  // goes to the run's next tile that gets a token
+  auto advance = [&] {
+    while (left-- > 0) {
+      if (++h == H) {
+        h = 0;
+        ++slot;
+      }
+      if (slot >= next) {
+        while (slot >= next) next = a.dst_page_indptr[++seq + 1];   // (ends at num_seqs - 1)
+        s = KeepSeq(a, seq);
+      }
+      if (!s.bad && (int64_t)(slot - s.to) * 16 < s.count) return true;
+    }
+    return false;
+  };
+  TileSource now, soon, then;
+  bool has_now = false, has_soon = false, has_then = true;
+  while (has_now || has_soon || has_then) {
+    if (has_then) has_then = advance();
+    if (has_then) then.find_tokens(a, s, seq, h, slot - s.to, lane);
+    if (has_soon) soon.find_pages(a);
+    if (has_now) {
+      now.check(a);
+      if (values) {
+        VTile<T, KVQ, D> v;
+        v.load(a, now, lane);
+        v.store(a, now, lane);
+      } else {
+        KTile<T, KVQ, D> k;
+        k.load(a, now, lane);
+        k.store(a, now, lane);
+      }
+    }
+    now = soon;
+    soon = then;
+    has_now = has_soon;
+    has_soon = has_then;
+  }
+}
+
+// In place: a workgroup for each (sequence, head, pool) goes through the pages in order, a
+// page a wave. Kept indices are ascending, so a page reads only what lies at it or
+// behind it: the pages of one round are loaded, and stored when all are; what the next
+// round reads lies behind all of these.
+constexpr int kInPlaceWaves = 16;
+template <typename T, bool KVQ, int D>
+__global__ __launch_bounds__(64 * kInPlaceWaves) void keep_in_place_kernel(KeepArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, H = a.num_kv_heads;
   const int z = (int)(blockIdx.x % 2), h = (int)(blockIdx.x / 2 % H), seq = (int)(blockIdx.x / 2 / H);
-  const int len = a.seq_len[seq], count = a.new_len[seq];
-  const int base = a.seq_page_indptr[seq], to = a.dst_page_indptr[seq];
-  const int64_t have = (int64_t)(a.seq_page_indptr[seq + 1] - base) * 16;
-  const int64_t room = (int64_t)(a.dst_page_indptr[seq + 1] - to) * 16;
-  if (len < 0 || count < 0 || count > len || len > have || count > room || (count < len && count > a.kept_width)) {
-    if (z == 0 && h == 0 && tid == 0 && a.error_flag) a.error_flag[0] = 1;
+  const KeepSeq s(a, seq);
+  if (s.bad) {
+    if (threadIdx.x == 0 && a.error_flag) a.error_flag[0] = 1;
     return;
   }
-  const bool whole = count == len;
-  if (whole && a.in_place) return;
-  const int32_t* kept = a.kept + ((int64_t)seq * H + h) * a.kept_width;
-  uint8_t* pool = z ? a.v_pool : a.k_pool;
-  const int tile = z ? Fmt::kV : Fmt::kK;
-  for (int p = 0; p * 16 < count; ++p) {
-    const int page = a.dst_page_ids[to + p];
-    const bool there = page >= 0 && page < a.num_pool_pages;
-    if (tid < 16) {
-      const int j = 16 * p + tid;
-      int src = -1;
-      bool bad = !there;
-      if (j < count) {
-        const int t = whole ? j : kept[j];
-        bad |= t < 0 || t >= len;
-        if (t >= 0 && t < len) {
-          const int id = a.page_ids[base + t / 16];
-          if (id >= 0 && id < a.num_pool_pages) {
-            src = t & 15;
-            from[tid] = ((int64_t)id * H + h) * tile;
-          } else {
-            bad = true;
-          }
-        }
-        if (bad && a.error_flag) a.error_flag[0] = 1;
+  if (s.whole) return;
+  auto move = [&](auto tile) {
+    for (int64_t p0 = 0; p0 * 16 < s.count; p0 += kInPlaceWaves) {
+      const int64_t p = p0 + wave;
+      const bool mine = p * 16 < s.count;
+      TileSource src;
+      if (mine) {
+        src.find_tokens(a, s, seq, h, (int)p, lane);
+        src.find_pages(a);
+        src.check(a);
+        tile.load(a, src, lane);
       }
-      at[tid] = src;
+      __builtin_amdgcn_s_waitcnt(0x0f70);   // every load has ended, not only begun
+      __syncthreads();
+      if (mine) tile.store(a, src, lane);
     }
-    __syncthreads();
-    if (!there) continue;
-    uint8_t* dst = pool + ((int64_t)page * H + h) * tile;
-    if constexpr (!KVQ) {
-      constexpr int E = 16 / (int)sizeof(T), U = D / E, N = 16 * U / 256;   // 16-byte units a thread moves
-      constexpr int M = N > 0 ? N : 1;
-      u32x4_t x[M];
-      bool live[M];
-#pragma unroll
-      for (int i = 0; i < M; ++i) {
-        const int u = tid + 256 * i;
-        live[i] = false;
-        if (u >= 16 * U) continue;
-        if (z == 0) {   // unit u / 16 of token u % 16
-          const int s = at[u & 15];
-          live[i] = s >= 0;
-          if (live[i]) x[i] = *reinterpret_cast<const u32x4_t*>(pool + from[u & 15] + ((u >> 4) * 16 + s) * 16);
-        } else {        // E slots of a dim
-          const int dim = u / (16 / E), part = u % (16 / E);
-          // (slots that get no token keep what they hold)
-          x[i] = *reinterpret_cast<const u32x4_t*>(dst + u * 16);
-          T* e = reinterpret_cast<T*>(&x[i]);
-#pragma unroll
-          for (int j = 0; j < E; ++j) {
-            const int tok = v_token_at_slot(part * E + j), s = at[tok];
-            if (s >= 0) e[j] = reinterpret_cast<const T*>(pool + from[tok])[dim * 16 + v_slot_of_token(s)];
-            live[i] |= s >= 0;
-          }
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < M; ++i) {
-        const int u = tid + 256 * i;
-        if (live[i]) *reinterpret_cast<u32x4_t*>(dst + u * 16) = x[i];
-      }
-    } else if (z == 0) {
-      // codes: 4 groups of D / 8 bytes a token; scales: D / 32 bytes a token
-      constexpr int W = D / 32;   // dwords of a token's codes in a group
-      uint32_t c[W] = {};
-      uint32_t sc = 0;
-      const int tok = tid & 15, g = tid >> 4;   // (64 threads)
-      const int s = tid < 64 ? at[tok] : -1;
-      if (s >= 0) {
-        const uint8_t* src = pool + from[tok];
-#pragma unroll
-        for (int i = 0; i < W; ++i) c[i] = reinterpret_cast<const uint32_t*>(src + (g * 16 + s) * (D / 8))[i];
-        if (g == 0) {
-          if constexpr (D == 128) sc = *reinterpret_cast<const uint32_t*>(src + D * 8 + s * 4);
-          else sc = *reinterpret_cast<const uint16_t*>(src + D * 8 + s * 2);
-        }
-      }
-      __syncthreads();
-      if (s >= 0) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) reinterpret_cast<uint32_t*>(dst + (g * 16 + tok) * (D / 8))[i] = c[i];
-        if (g == 0) {
-          if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst + D * 8 + tok * 4) = sc;
-          else *reinterpret_cast<uint16_t*>(dst + D * 8 + tok * 2) = (uint16_t)sc;
-        }
-      }
-    } else {
-      // a dword: the codes of 8 slots of a dim; [D / 64][half][16][4] of them
-      uint32_t x = 0;
-      uint16_t sc = 0;
-      bool live = false;
-      if (tid < D * 2) {
-        const int half = (tid >> 6) & 1, in_half = (tid >> 7) * 128 + (tid & 63);
-        x = reinterpret_cast<const uint32_t*>(dst)[tid];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int tok = v_token_at_slot(8 * half + j), s = at[tok];
-          if (s < 0) continue;
-          const int slot = v_slot_of_token(s);
-          const uint32_t w = (pool + from[tok])[(in_half + 64 * (slot >> 3)) * 4 + ((slot & 7) >> 1)];
-          const uint32_t code = slot & 1 ? w >> 4 : w & 15;
-          x = (x & ~(15u << (4 * j))) | code << (4 * j);
-          live = true;
-        }
-      }
-      const int s = tid < 16 ? at[v_token_at_slot(tid)] : -1;
-      if (s >= 0) sc = reinterpret_cast<const uint16_t*>(pool + from[v_token_at_slot(tid)] + D * 8)[v_slot_of_token(s)];
-      __syncthreads();
-      if (live) reinterpret_cast<uint32_t*>(dst)[tid] = x;
-      if (s >= 0) reinterpret_cast<uint16_t*>(dst + D * 8)[tid] = sc;
-    }
-    __syncthreads();
-  }
+  };
+  if (z == 0) move(KTile<T, KVQ, D>{});
+  else move(VTile<T, KVQ, D>{});
 }
 
 // ---------------------------------------------------------------- pages given back
@@ -328,7 +575,8 @@ struct ReleaseArgs {
   int32_t* free_next_out;
   int32_t* error_flag;
   int32_t num_seqs, table_width, num_free;
-  int32_t per;   // sequences of a workgroup
+  int32_t per;      // sequences of a group
+  int32_t splits;   // workgroups of a group, which share its rows
 };
 
 __device__ __forceinline__ uint32_t sum_sat(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
@@ -350,7 +598,8 @@ struct Released {
 __global__ __launch_bounds__(256) void release_kernel(ReleaseArgs a) {
   __shared__ uint32_t sums[4][3];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int first = (int)min((int64_t)a.num_seqs, (int64_t)blockIdx.x * a.per);
+  const int group = (int)blockIdx.x / a.splits, split = (int)blockIdx.x % a.splits;
+  const int first = (int)min((int64_t)a.num_seqs, (int64_t)group * a.per);
   const int last = (int)min((int64_t)a.num_seqs, (int64_t)first + a.per);
   uint32_t s[3] = {0, 0, 0};   // pages before the group, of all; malformed ones
   for (int64_t i = tid; i < a.num_seqs; i += 256) {
@@ -380,7 +629,7 @@ __global__ __launch_bounds__(256) void release_kernel(ReleaseArgs a) {
     for (int i = first; i < last; ++i) {
       const Released r(a, i);
       const int32_t* row = a.block_table + (int64_t)i * a.table_width + r.first;
-      for (int j = tid; j < r.count; j += 256) a.free_pages_out[at + j] = row[j];
+      for (int j = split * 256 + tid; j < r.count; j += a.splits * 256) a.free_pages_out[at + j] = row[j];
       at += r.count;
     }
   }
@@ -411,17 +660,24 @@ halo_status_t page_keep(bool kvq, void* k_pool, void* v_pool, const halo_attn_pa
   const int64_t blocks = (int64_t)num_seqs * params->num_kv_heads * 2;
   if (blocks > 1 << 24) return fail(HALO_ERR_UNSUPPORTED, "num_seqs * num_kv_heads must be at most 2^23");
   KeepArgs g{static_cast<uint8_t*>(k_pool), static_cast<uint8_t*>(v_pool), page_ids, seq_page_indptr, seq_len, new_len,
-             kept, dst_page_ids, dst_page_indptr, error_flag, params->num_pool_pages, params->num_kv_heads, kept_width,
-             dst_page_ids == page_ids};
+             kept, dst_page_ids, dst_page_indptr, error_flag, params->num_pool_pages, num_seqs, params->num_kv_heads,
+             kept_width};
   (void)hipGetLastError();
   by_type_and_dim(params, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
     using W = typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type;
-    const dim3 grid((unsigned)blocks), block(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (!kvq) hipLaunchKernelGGL((keep_kernel<W, false, D>), grid, block, 0, s, g);
-    else hipLaunchKernelGGL((keep_kernel<uint8_t, true, D>), grid, block, 0, s, g);
+    auto launch = [&](auto t, auto kvq) {
+      using U = decltype(t);
+      constexpr bool Q = decltype(kvq)::value;
+      if (dst_page_ids == page_ids)
+        hipLaunchKernelGGL((keep_in_place_kernel<U, Q, D>), dim3((unsigned)blocks), dim3(64 * kInPlaceWaves), 0, s, g);
+      else
+        hipLaunchKernelGGL((keep_kernel<U, Q, D>), dim3(4096), dim3(256), 0, s, g);
+    };
+    if (kvq) launch(uint8_t{}, std::true_type{});
+    else launch(W{}, std::false_type{});
   });
   return hip_check("keep launch");
 }
@@ -451,7 +707,14 @@ extern "C" halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, c
   if (lap != HALO_OK) return lap;
   EvictArgs g{*sizes, weights, seq_len, kept, weights_out, new_len, error_flag};
   (void)hipGetLastError();
-  hipLaunchKernelGGL(evict_kernel, dim3((unsigned)rows), dim3(kEvictThreads), 0, static_cast<hipStream_t>(stream), g);
+  // as many tokens in registers as the rows may hold
+  auto launch = [&](auto waves, auto per_lane) {
+    constexpr int W = decltype(waves)::value, R = decltype(per_lane)::value;
+    hipLaunchKernelGGL((evict_kernel<W, R>), dim3((unsigned)rows), dim3(64 * W), 0, static_cast<hipStream_t>(stream), g);
+  };
+  if (sizes->width <= 1024) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
+  else if (sizes->width <= 4096) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
+  else launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{});
   return hip_check("evict launch");
 }
 
@@ -496,12 +759,14 @@ extern "C" halo_status_t halo_kv_release_pages(const halo_step_sizes_t* sizes, c
       {{"free_pages_out", free_pages_out, 4 * (int64_t)sizes->num_free}, {"free_next_out", free_next_out, 4},
        {"error_flag", error_flag, 4}});
   if (lap != HALO_OK) return lap;
-  // up to 256 workgroups, a group of sequences each; without sequences one copies the list
-  const int want = std::max((int)n, (int)std::min<int64_t>(64, (sizes->num_free + 2047) / 2048));
-  const int blocks = std::min(std::max(want, 1), kNumCUs);
+  // up to 256 groups of sequences, and more workgroups for one where rows or the
+  // list are long and sequences few
+  const int groups = std::min(std::max((int)n, 1), kNumCUs);
   ReleaseArgs g{block_table, seq_len, new_len, free_pages, free_next, free_pages_out, free_next_out, error_flag,
-                sizes->num_seqs, sizes->table_width, sizes->num_free, (int)((n + blocks - 1) / blocks)};
+                sizes->num_seqs, sizes->table_width, sizes->num_free, (int)((n + groups - 1) / groups), 1};
+  const int64_t longest = std::max<int64_t>((sizes->table_width + 511) / 512, sizes->num_free / 512 / groups);
+  g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(longest, kNumCUs / groups));
   (void)hipGetLastError();
-  hipLaunchKernelGGL(release_kernel, dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(stream), g);
+  hipLaunchKernelGGL(release_kernel, dim3(groups * g.splits), dim3(256), 0, static_cast<hipStream_t>(stream), g);
   return hip_check("release launch");
 }
