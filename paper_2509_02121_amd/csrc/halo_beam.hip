@@ -28,14 +28,12 @@ constexpr float kMinusInf = -__builtin_huge_valf();
 
 // What a wave found in its part of a row.
 struct BeamPart {
-  float top;      // the largest logit, or the lowest finite number
-  float sum;      // of exp(logit - top)
-  int32_t count;  // candidates it names
-  int32_t pad;
+  float top;   // the largest logit, or the lowest finite number
+  float sum;   // of exp(logit - top)
 };
 struct Candidate {
   float value;
-  int32_t token;
+  int32_t token;   // -1: none
 };
 
 struct BeamArgs {
@@ -66,57 +64,71 @@ __device__ __forceinline__ float from_order_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// The largest number of which at least n of the wave's N keys a lane are no
-// smaller, between lo (which has as many) and the largest key. Bit by bit, from the
-// keys' ballots.
-template <int N>
-__device__ __forceinline__ uint32_t wave_nth_key(const uint32_t (&key)[N], int n, uint32_t lo) {
+// A number that at least n of the wave's N keys a lane are no smaller than (0 if there
+// are fewer keys), and as few more as ties allow: the n-th largest key, or one between it and the
+// next smaller. Bit by bit from the top, from the keys' ballots, until it is as
+// good (or, of the upper bits alone, no larger than that).
+template <int LOWEST_BIT = 0, int N>
+__device__ __forceinline__ uint32_t wave_nth_key(const uint32_t (&key)[N], int n) {
   uint32_t t = 0;
-  for (int bit = 31; bit >= 0; --bit) {
+  for (int bit = 31; bit >= LOWEST_BIT; --bit) {
     const uint32_t next = t | 1u << bit;
     int c = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) c += __popcll(__ballot(key[j] >= next));
     if (c >= n) t = next;
+    if (c == n) break;
   }
-  return max(t, lo);
+  return t;
 }
 
-constexpr int kTile = 512;        // elements a wave looks at together
-constexpr int kListCap = 1024;    // candidates a wave holds
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+// LDS that a wave alone writes and reads: what was written can be read by its other lanes.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
-// Keeps the `best` first of the list's n candidates (by value, then token).
-__device__ __forceinline__ int prune(float* value, int32_t* token, int n, int best, int lane) {
-  constexpr int N = kListCap / 64;
-  uint32_t key[N], id[N];
+constexpr int kBoundBit = 14;    // of a bound on logits the bits from here on
+constexpr int kTile = 512;       // elements a wave looks at together
+constexpr int kListCap = 640;    // candidates a wave holds
+constexpr int kListFull = kListCap - kTile;
+
+// Keeps the `best` first of the list's n candidates (by value, then token), N a lane.
+template <int N>
+__device__ __forceinline__ int prune_of(float* value, int32_t* token, int n, int best, int lane) {
+  uint32_t key[N], id[N];   // (larger: earlier)
 #pragma unroll
   for (int j = 0; j < N; ++j) {
     const int i = 64 * j + lane;
     key[j] = i < n ? order_key(value[i]) : 0;
     id[j] = i < n ? ~(uint32_t)token[i] : 0;
   }
-  if (n <= best) return n;
-  const uint32_t least = wave_nth_key(key, best, 0);
-  int above = 0, ties = 0;
+  const uint32_t least = wave_nth_key(key, best);
+  int count = 0;
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    above += __popcll(__ballot(key[j] > least));
-    ties += __popcll(__ballot(key[j] == least));
-  }
-  uint32_t last = 0;   // of the ties the tokens up to this one (of ~token: from it on)
-  if (above + ties > best) {
+  for (int j = 0; j < N; ++j) count += __popcll(__ballot(key[j] >= least));
+  uint32_t last = 0;   // of the candidates at `least` those of this id and larger ones
+  if (count > best) {  // (then `least` is a key, and these are ties)
     uint32_t of_ties[N];
+    int above = 0;
 #pragma unroll
-    for (int j = 0; j < N; ++j) of_ties[j] = key[j] == least ? id[j] : 0;
-    last = wave_nth_key(of_ties, best - above, 0);
+    for (int j = 0; j < N; ++j) {
+      above += __popcll(__ballot(key[j] > least));
+      of_ties[j] = key[j] == least ? id[j] : 0;
+    }
+    last = wave_nth_key(of_ties, best - above);
   }
   int at = 0;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const bool keep = key[j] > least || (key[j] == least && id[j] >= last && id[j] != 0);
+    const bool keep = key[j] > least || (key[j] == least && id[j] >= last);
     const uint64_t mask = __ballot(keep);
     if (keep) {
-      const int to = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+      const int to = at + lanes_before(mask);
       value[to] = from_order_key(key[j]);
       token[to] = (int32_t)~id[j];
     }
@@ -124,39 +136,43 @@ __device__ __forceinline__ int prune(float* value, int32_t* token, int n, int be
   }
   return at;
 }
+__device__ __forceinline__ int prune(float* value, int32_t* token, int n, int best, int lane) {
+  wave_lds_fence();
+  if (n > best) {
+    if (n <= 64) n = prune_of<1>(value, token, n, best, lane);
+    else if (n <= 128) n = prune_of<2>(value, token, n, best, lane);
+    else n = prune_of<kListCap / 64>(value, token, n, best, lane);
+    wave_lds_fence();
+  }
+  return n;
+}
 
 // Elements x[0 .. 511] of a row, eight a lane, of which those from n on are -inf. Loads
 // are of 16 bytes at any alignment of the row, so that which lane adds what goes by
 // the token alone: two beams of the same logits have the same sum.
 template <typename T>
-__device__ __forceinline__ void load_tile(const T* x, int64_t n, int lane, float (&v)[8]) {
-  constexpr int E = 16 / (int)sizeof(T);
+struct Tile {
+  static constexpr int E = 16 / (int)sizeof(T);
+  T w[8];
+  __device__ __forceinline__ void load(const T* x, int64_t n, int lane) {
+    if (n >= kTile) {
 #pragma unroll
-  for (int u = 0; u < 8 / E; ++u) {
-    const int i = (u * 64 + lane) * E;
-    T w[E];
-    if (i + E <= n) {
-      __builtin_memcpy(w, x + i, 16);
+      for (int u = 0; u < 8 / E; ++u) __builtin_memcpy(w + u * E, x + (u * 64 + lane) * E, 16);
     } else {
 #pragma unroll
-      for (int j = 0; j < E; ++j) w[j] = i + j < n ? x[i + j] : (T)kMinusInf;
+      for (int k = 0; k < 8; ++k) w[k] = place(k, lane) < n ? x[place(k, lane)] : (T)kMinusInf;
     }
-#pragma unroll
-    for (int j = 0; j < E; ++j) v[u * E + j] = (float)w[j];
   }
-}
-// Place of element v[k] of a lane in its tile.
-template <typename T>
-__device__ __forceinline__ int place_in_tile(int k, int lane) {
-  constexpr int E = 16 / (int)sizeof(T);
-  return ((k / E) * 64 + lane) * E + k % E;
-}
+  // place of a lane's element k in the tile
+  static __device__ __forceinline__ int place(int k, int lane) { return ((k / E) * 64 + lane) * E + k % E; }
+};
 
 // A wave passes its part of a row once. A lane follows the largest of its logits and
 // the sum of their exponentials (fp32; the lanes' are joined in 64 bits). Candidates go to a
-// list in LDS: after the first tile those at or above the best-th largest lane maximum (as many
-// lanes have one), later those above the list's best-th, which is found anew when
-// the list has grown; ties with that are later tokens and no candidates.
+// list in LDS: those at or above the best-th largest lane maximum, since as many lanes have
+// seen one; it is found anew after 1, 2, 4, 8, ... tiles, so that of a part in any order about
+// `best` more are listed each time the part seen doubles. A full list is cut to the
+// first `best`; then only what is above the last of these counts (ties with it are later tokens).
 template <typename T>
 __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
   __shared__ float list_value[4][kListCap];
@@ -166,79 +182,77 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
   if (part >= a.num_parts) return;
   BeamPart* out = a.parts + (int64_t)row * a.num_parts + part;
   // (a beam that has ended or is dead: its logits are not looked at)
-  if ((a.ended && a.ended[row]) || !is_finite(a.scores[row])) {
-    if (lane == 0) *out = BeamPart{kLowest, 0.f, 0, 0};
-    return;
-  }
+  if ((a.ended && a.ended[row]) || !is_finite(a.scores[row])) return;
   const T* x = static_cast<const T*>(a.logits) + (int64_t)row * a.stride;
   const int64_t begin = (int64_t)part * a.per, end = min(begin + a.per, (int64_t)a.vocab);
   float* value = list_value[wave];
   int32_t* token = list_token[wave];
   float top = kLowest, sum = 0.f, bound = kMinusInf;
-  int n = 0;
+  int n = 0, seen = 0, renew = 1;
+  Tile<T> now, next, then;
+  if (begin < end) now.load(x + begin, end - begin, lane);
+  if (begin + kTile < end) next.load(x + begin + kTile, end - begin - kTile, lane);
   for (int64_t t = begin; t < end; t += kTile) {
+    if (t + 2 * kTile < end) then.load(x + t + 2 * kTile, end - t - 2 * kTile, lane);
     float v[8];
-    load_tile<T>(x + t, end - t, lane, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = (float)now.w[k];
     float most = v[0];
 #pragma unroll
     for (int k = 1; k < 8; ++k) most = fmaxf(most, v[k]);
-    const float now = fmaxf(top, most);
-    sum *= __builtin_amdgcn_exp2f((top - now) * 1.44269504088896340736f);
+    const float high = fmaxf(top, most);
+    sum *= __builtin_amdgcn_exp2f((top - high) * 1.44269504088896340736f);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f((v[k] - now) * 1.44269504088896340736f);
-    top = now;
-    if (t == begin) {
-      const uint32_t key[1] = {order_key(most)};
-      // just below the best-th largest lane maximum, not below -inf
-      uint32_t k = wave_nth_key(key, a.best, order_key(kMinusInf) + 1) - 1;
-      if (k == order_key(0.f) - 1) --k;   // (the key of -0)
-      bound = from_order_key(k);
-    }
-    if (!__any(most > bound)) continue;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const bool hit = v[k] > bound;
-      const uint64_t mask = __ballot(hit);
-      if (hit) {
-        const int to = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-        value[to] = v[k];
-        token[to] = (int32_t)t + place_in_tile<T>(k, lane);
-      }
-      n += __popcll(mask);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    if (n > kListCap - kTile || t == begin) {
-      n = prune(value, token, n, a.best, lane);
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      if (n >= a.best) {
-        // (n = best: the list's smallest)
-        float least = -kMinusInf;
-        for (int i = lane; i < n; i += 64) least = fminf(least, value[i]);
-#pragma unroll
-        for (int m = 32; m >= 1; m >>= 1) least = fminf(least, __shfl_xor(least, m));
-        bound = least;
-      } else {
-        bound = kMinusInf;
+    for (int k = 0; k < 8; ++k) sum += __builtin_amdgcn_exp2f((v[k] - high) * 1.44269504088896340736f);
+    top = high;
+    if (++seen == renew) {
+      renew *= 2;
+      // just below the best-th largest lane maximum, as long as that is no lane without a logit
+      const uint32_t key[1] = {order_key(top)};
+      uint32_t k = wave_nth_key<kBoundBit>(key, a.best);
+      if (k > order_key(kLowest)) {
+        if (--k == order_key(0.f) - 1) --k;   // (the key of -0)
+        bound = fmaxf(bound, from_order_key(k));
       }
     }
+    if (__any(most > bound)) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const bool hit = v[k] > bound;
+        const uint64_t mask = __ballot(hit);
+        if (mask) {
+          if (hit) {
+            const int to = n + lanes_before(mask);
+            value[to] = v[k];
+            token[to] = (int32_t)t + Tile<T>::place(k, lane);
+          }
+          n += __popcll(mask);
+        }
+      }
+      if (n > kListFull) {
+        n = prune(value, token, n, a.best, lane);
+        if (n >= a.best) {
+          float least = -kMinusInf;
+          for (int i = lane; i < n; i += 64) least = fminf(least, value[i]);
+#pragma unroll
+          for (int m = 32; m >= 1; m >>= 1) least = fminf(least, __shfl_xor(least, m));
+          bound = fmaxf(bound, least);
+        }
+      }
+    }
+    now = next;
+    next = then;
   }
   n = prune(value, token, n, a.best, lane);
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   Candidate* c = a.candidates + ((int64_t)row * a.num_parts + part) * a.best;
-  for (int i = lane; i < n; i += 64) c[i] = Candidate{value[i], token[i]};
+  for (int i = lane; i < a.best; i += 64) c[i] = i < n ? Candidate{value[i], token[i]} : Candidate{kMinusInf, -1};
   float most = top;
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
   double s = (double)sum * exp2((double)(top - most) * 1.44269504088896340736);
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
-  if (lane == 0) *out = BeamPart{most, (float)s, n, 0};
+  if (lane == 0) *out = BeamPart{most, (float)s};
 }
 
 // ---------------------------------------------------------------- the best of an item
@@ -251,25 +265,40 @@ __device__ __forceinline__ double from_order_key(uint64_t k) {
   return __longlong_as_double((long long)(k & 0x8000000000000000ull ? k & 0x7fffffffffffffffull : ~k));
 }
 
-// A workgroup for each item: ln sum exp of every beam from its parts, then `best`
-// rounds, each of which finds the first of the candidates behind the last round's.
+constexpr int kPickCap = 1024;   // candidates that are put in order together
+
+struct Ranked {
+  uint64_t key, id;   // larger keys first, then smaller ids
+};
+
+// A workgroup for each item. ln sum exp of every beam comes from its parts. Of the beams'
+// candidates those at or above a bound go to a list in LDS, and each one's place is how
+// many of the list come before it. The bound: of each wave's lane maxima the best-th largest
+// one (in the upper 32 bits), of the waves' the largest. A list that does
+// not hold them all (ties) is left, and `best` rounds find the first of the candidates
+// behind the last round's.
 __global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
   __shared__ double lse[kMaxBeams];
   __shared__ int32_t live[kMaxBeams];   // 0 dead, 1 live, 2 ended
-  __shared__ uint64_t best_key[4], best_id[4];
+  __shared__ __align__(16) Ranked list[kPickCap];
+  __shared__ uint32_t bounds[4];
+  __shared__ int32_t listed;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int item = (int)blockIdx.x, W = a.beams, P = a.num_parts;
+  if (tid == 0) listed = 0;
   for (int b = wave; b < W; b += 4) {
     const int row = item * W + b;
     const BeamPart* parts = a.parts + (int64_t)row * P;
     const bool open = is_finite(a.scores[row]);
     const bool ended = a.ended && a.ended[row];
+    const bool read = open && !ended;   // (its parts are written)
     float most = kLowest;
-    for (int p = lane; p < P; p += 64) most = fmaxf(most, parts[p].top);
+    for (int p = lane; p < P; p += 64) most = fmaxf(most, read ? parts[p].top : kLowest);
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
     double s = 0;
-    for (int p = lane; p < P; p += 64) s += (double)parts[p].sum * exp2((double)(parts[p].top - most) * 1.44269504088896340736);
+    for (int p = lane; p < P; p += 64)
+      s += read ? (double)parts[p].sum * exp2((double)(parts[p].top - most) * 1.44269504088896340736) : 0;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
     if (lane == 0) {
@@ -280,58 +309,102 @@ __global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
     }
   }
   __syncthreads();
-  uint64_t last_key = ~0ull, last_id = 0;   // candidates are in order of falling keys, rising ids
-  const int per_row = P * a.best;
-  for (int r = 0; r < a.best; ++r) {
-    uint64_t key = 0, id = ~0ull;
-    for (int i = tid; i < W * per_row; i += 256) {
-      const int b = i / per_row, j = i % per_row, p = j / a.best, c = j % a.best;
-      const int64_t at = ((int64_t)(item * W + b) * P + p);
-      double v;
-      int32_t tok;
-      if (live[b] == 1) {
-        if (c >= a.parts[at].count) continue;
-        const Candidate x = a.candidates[at * a.best + c];
-        v = ((double)x.value - lse[b]) + (double)a.scores[item * W + b];
-        tok = x.token;
-      } else if (live[b] == 2 && j == 0) {
-        v = (double)a.scores[item * W + b];
-        tok = a.end_token;
-      } else {
-        continue;
-      }
-      const uint64_t k = order_key(v), d = (uint64_t)b << 32 | (uint32_t)tok;
-      const bool behind = k < last_key || (k == last_key && d > last_id);
-      if (behind && (k > key || (k == key && d < id))) {
-        key = k;
-        id = d;
-      }
+  const int per_row = P * a.best, all = W * per_row;
+  // candidate i's key (larger: better; 0: none) and, of equal keys, its order
+  auto candidate = [&](int i, uint64_t& key, uint64_t& id) {
+    const int b = i / per_row, j = i - b * per_row;
+    const int row = item * W + b;
+    key = 0;
+    if (live[b] == 1) {
+      const Candidate x = a.candidates[(int64_t)row * per_row + j];
+      if (x.token < 0) return;
+      key = order_key(((double)x.value - lse[b]) + (double)a.scores[row]);
+      id = (uint64_t)b << 32 | (uint32_t)x.token;
+    } else if (live[b] == 2 && j == 0) {
+      key = order_key((double)a.scores[row]);
+      id = (uint64_t)b << 32 | (uint32_t)a.end_token;
     }
+  };
+  constexpr int R = 4;   // candidates a thread keeps; more are looked up again
+  uint64_t keys[R], ids[R];
+  uint32_t most[1] = {0};
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    keys[j] = 0;
+    if (tid + 256 * j < all) candidate(tid + 256 * j, keys[j], ids[j]);
+    most[0] = max(most[0], (uint32_t)(keys[j] >> 32));
+  }
+  for (int i = tid + 256 * R; i < all; i += 256) {
+    uint64_t key, id;
+    candidate(i, key, id);
+    most[0] = max(most[0], (uint32_t)(key >> 32));
+  }
+  const uint32_t mine = wave_nth_key(most, a.best);
+  if (lane == 0) bounds[wave] = mine;
+  __syncthreads();
+  const uint32_t bound = max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3]));
+  auto offer = [&](uint64_t key, uint64_t id) {
+    if (key != 0 && (uint32_t)(key >> 32) >= bound) {
+      const int at = atomicAdd(&listed, 1);
+      if (at < kPickCap) list[at] = Ranked{key, id};
+    }
+  };
+#pragma unroll
+  for (int j = 0; j < R; ++j) offer(keys[j], ids[j]);
+  for (int i = tid + 256 * R; i < all; i += 256) {
+    uint64_t key, id;
+    candidate(i, key, id);
+    offer(key, id);
+  }
+  __syncthreads();
+  const int n = listed;
+  auto write = [&](int place, uint64_t key, uint64_t id) {
+    const int64_t to = (int64_t)item * a.best + place;
+    a.out_scores[to] = key ? (float)from_order_key(key) : kMinusInf;
+    a.out_tokens[to] = key ? (int32_t)(uint32_t)id : -1;
+    a.out_parents[to] = key ? (int32_t)(id >> 32) : -1;
+  };
+  if (n <= kPickCap) {
+    for (int i = tid; i < n; i += 256) {
+      const Ranked me = list[i];
+      int place = 0;
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) {
+        const Ranked x = list[j];
+        place += (int)(x.key > me.key) | ((int)(x.key == me.key) & (int)(x.id < me.id));
+      }
+      if (place < a.best) write(place, me.key, me.id);
+    }
+    for (int i = n + tid; i < a.best; i += 256) write(i, 0, 0);
+    return;
+  }
+  uint64_t last_key = ~0ull, last_id = 0;   // candidates are in order of falling keys, rising ids
+  for (int r = 0; r < a.best; ++r) {
+    uint64_t best_key = 0, best_id = ~0ull;
     auto better = [&](uint64_t k, uint64_t d) {
-      if (k > key || (k == key && d < id)) {
-        key = k;
-        id = d;
+      if (k > best_key || (k == best_key && d < best_id)) {
+        best_key = k;
+        best_id = d;
       }
     };
+    for (int i = tid; i < all; i += 256) {
+      uint64_t key, id;
+      candidate(i, key, id);
+      if (key != 0 && (key < last_key || (key == last_key && id > last_id))) better(key, id);
+    }
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) better(__shfl_xor(key, m), __shfl_xor(id, m));
-    __syncthreads();
-    if (lane == 0) {
-      best_key[wave] = key;
-      best_id[wave] = id;
+    for (int m = 32; m >= 1; m >>= 1) {
+      const uint64_t k = __shfl_xor(best_key, m), d = __shfl_xor(best_id, m);
+      better(k, d);
     }
     __syncthreads();
+    if (lane == 0) list[wave] = Ranked{best_key, best_id};
+    __syncthreads();
 #pragma unroll
-    for (int w = 0; w < 4; ++w) better(best_key[w], best_id[w]);
-    if (tid == 0) {
-      const int64_t to = (int64_t)item * a.best + r;
-      const bool any = key != 0;
-      a.out_scores[to] = any ? (float)from_order_key(key) : kMinusInf;
-      a.out_tokens[to] = any ? (int32_t)(uint32_t)id : -1;
-      a.out_parents[to] = any ? (int32_t)(id >> 32) : -1;
-    }
-    last_key = key;
-    last_id = id;
+    for (int w = 0; w < 4; ++w) better(list[w].key, list[w].id);
+    if (tid == 0) write(r, best_key, best_id);
+    last_key = best_key;
+    last_id = best_id;
   }
 }
 
@@ -520,12 +593,12 @@ halo_status_t check_sizes(const halo_beam_sizes_t* s) {
   return HALO_OK;
 }
 
-// Elements of a wave's part of a row, and the parts of a row: about 8192 waves in
+// Elements of a wave's part of a row, and the parts of a row: about 4096 waves in
 // all, of at least four tiles each.
 void parts_of(const halo_beam_sizes_t* s, int32_t& per, int32_t& parts) {
   const int64_t rows = std::max<int64_t>((int64_t)s->num_items * s->num_beams, 1);
   const int64_t span = s->vocab;
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(8192 / rows, (span + 2047) / 2048));
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>(4096 / rows, (span + 2047) / 2048));
   per = (int32_t)((span + want * kTile - 1) / (want * kTile) * kTile);
   parts = (int32_t)((span + per - 1) / per);
 }
