@@ -234,6 +234,215 @@ __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- many rows
+
+// Fragments of 32 keys for 32x32x16 products: lane (c, hh) holds dims 16 s + 8 hh .. + 7 of
+// key c % 16 of page c / 16 (`tile`: that page's).
+template <bool KVQ, int D>
+__device__ __forceinline__ void load_keys32(const uint8_t* tile, int key, int hh, bf16x8_t (&k)[D / 16]) {
+  if constexpr (KVQ) {
+    // dims 16 s + 8 hh are in group 2 (s & 1) + hh
+    uint32_t codes[2][D / 32], scales;
+    const uint8_t* sc = tile + D * 8 + key * (D / 32);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const uint8_t* at = tile + ((2 * z + hh) * 16 + key) * (D / 8);
+      if constexpr (D == 128) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(at);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) codes[z][s] = x[s];
+      } else {
+        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(at);
+        codes[z][0] = x[0];
+        codes[z][1] = x[1];
+      }
+    }
+    if constexpr (D == 128) scales = *reinterpret_cast<const uint32_t*>(sc);
+    else scales = *reinterpret_cast<const uint16_t*>(sc);
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) k[s] = kvq_decode_bf16(codes[s & 1][s >> 1], kvq_scale_byte(scales, s >> 1));
+  } else {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      k[s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(tile + ((2 * s + hh) * 16 + key) * 16));
+  }
+}
+
+// A workgroup takes jobs of 16 slots of one head (which may span sequences), a wave four of the pages, 64 keys, as
+// fragments in registers. 32 rows at a time go to LDS, by direct loads, while the
+// ones before are worked on; rows are the A operand of 32x32x16 MFMAs, so a lane has 16
+// rows of a key. Bound by the VALU: a product's 64 results take a multiply-add, an
+// exponential (four times as long) and an addition.
+// LDS: 16-byte unit u of row r lies at place u ^ r (mod the units of a row; at d 64 r / 2), so that
+// the 32 rows' units of one fragment are in different banks.
+template <bool KVQ, int D>
+__device__ __forceinline__ void weights_wide(const WeightArgs& a) {
+  constexpr int NS = D / 16, U = D / 8, RB = 2 * D, kSlots = 16, NI = D / 64, kRowsPer = 64 / U;
+  constexpr int64_t kTile = KVQ ? kvq_k_tile<D>() : 32 * D;
+  __shared__ __align__(1024) uint8_t q_lds[2][32 * RB];
+  __shared__ __align__(16) float l_lds[2][32];
+  __shared__ __align__(16) int sees_lds[2][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hh = lane >> 5;
+  const int H = a.num_kv_heads, G = a.group;
+  const int step_e = 32 / G, step_g = 32 % G;   // 32 rows on
+  const int first = a.seq_page_indptr[0];
+  const int64_t slots = (int64_t)a.seq_page_indptr[a.num_seqs] - first;
+  const int64_t jobs = (slots + kSlots - 1) / kSlots * H;
+  for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+    const int h = (int)(job % H);
+    const int64_t chunk = job / H * kSlots, chunk_end = min(slots, chunk + kSlots), mine = chunk + 4 * wave;
+    bf16x8_t k[2][NS];
+    bool ok[2];   // this lane's pages
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int64_t at = mine + 2 * b + (c >> 4);
+      const int pid = at < chunk_end ? a.page_ids[first + at] : -1;
+      ok[b] = pid >= 0 && pid < a.num_pool_pages;
+      // (a page that is none is read as page 0 and not written)
+      if (a.num_pool_pages > 0)
+        load_keys32<KVQ, D>(static_cast<const uint8_t*>(a.k_pool) + ((int64_t)(ok[b] ? pid : 0) * H + h) * kTile, c & 15, hh, k[b]);
+    }
+    int seq = last_at_or_below(a.seq_page_indptr, a.num_seqs, first + chunk, lane);
+    int64_t slot = chunk;
+    while (slot < chunk_end) {
+      while (first + slot >= a.seq_page_indptr[seq + 1]) ++seq;   // (ends at num_seqs - 1: slot < slots)
+      const WeightSeq s(a, seq);
+      const int64_t from = slot, upto = min(chunk_end, (int64_t)s.next - first);
+      slot = upto;
+      if ((s.bad || s.bad_rows || a.num_pool_pages == 0) && threadIdx.x == 0 && a.error_flag) a.error_flag[0] = 1;
+      const int64_t place = first - (int64_t)s.base;   // of slot 0 in the sequence's list
+      if (s.bad || a.num_pool_pages == 0 || (place + from) * 16 >= s.end) continue;
+      // this wave's keys in the sequence
+      const int64_t k0 = max(from, mine), k1 = min(upto, mine + 4);
+      const int key_lo = k0 < k1 ? (int)min((place + k0) * 16, (int64_t)s.end) : s.end;
+      const int key_hi = k0 < k1 ? (int)min((place + k1) * 16, (int64_t)s.end) : s.end;
+      const bool whole = k1 - k0 == 4;
+      int t[2];   // this lane's tokens; past every row's end: none
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int64_t at = mine + 2 * b + (c >> 4);
+        const bool in = at >= k0 && at < k1;
+        t[b] = in ? (int)min((place + at) * 16 + (c & 15), (int64_t)INT32_MAX) : INT32_MAX;
+        if (in && !ok[b] && (place + at) * 16 < s.end && a.error_flag) a.error_flag[0] = 1;
+      }
+      float sum[2] = {0.f, 0.f};
+      const int64_t rows = (int64_t)(s.e1 - s.e0) * G;
+      // The rows of the tiles: of a wave's direct loads lane / U (+ kRowsPer j), of the lse and
+      // the limits the thread's own. e: its entry (one tile ahead of at, the row of q).
+      int e[NI + 1], g[NI + 1], row[NI + 1];
+      auto row_of = [&](int e) {   // of entry e: its row of q, or -1 (behind the last: none is looked up)
+        return e < s.e1 ? a.rows ? max(a.rows[e], -1) : e : -2;
+      };
+#pragma unroll
+      for (int j = 0; j <= NI; ++j) {
+        const int r = j < NI ? wave * 8 + j * kRowsPer + lane / U : threadIdx.x & 31;
+        e[j] = s.e0 + r / G;
+        g[j] = r % G;
+        row[j] = rows > 0 ? row_of(e[j]) : -2;
+      }
+      float l = 0.f;
+      int sees = 0;
+      // begins the loads of a tile's rows and finds the next tile's
+      auto issue = [&](int b) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const int r = wave * 8 + j * kRowsPer + lane / U;
+          const int at = row[j] >= 0 && row[j] < a.num_rows ? row[j] : 0;   // (one that is none: any row, unseen)
+          const int unit = (lane % U) ^ (D == 128 ? r & 15 : (r >> 1) & 7);
+          __builtin_amdgcn_global_load_lds(
+              static_cast<const uint8_t*>(a.q) + ((int64_t)at * H * G + (int64_t)h * G + g[j]) * RB + unit * 16,
+              &q_lds[b][(wave * 8 + j * kRowsPer) * RB], 16, 0, 0);
+        }
+        const int at = row[NI];
+        const bool fine = at >= 0 && at < a.num_rows;
+        l = fine ? a.lse[(int64_t)at * H * G + (int64_t)h * G + g[NI]] : kNegInf;
+        sees = fine ? a.row_end ? a.row_end[e[NI]] : s.end : 0;
+        if (!fine && at != -2 && a.error_flag) a.error_flag[0] = 1;
+#pragma unroll
+        for (int j = 0; j <= NI; ++j) {
+          e[j] += step_e;
+          g[j] += step_g;
+          if (g[j] >= G) {
+            g[j] -= G;
+            ++e[j];
+          }
+          row[j] = row_of(e[j]);
+        }
+      };
+      if (rows > 0) issue(0);
+      int b = 0;
+      for (int64_t r0 = 0; r0 < rows; r0 += 32, b ^= 1) {
+        if (threadIdx.x < 32) {
+          const bool none = l == kNegInf;   // (it saw no key)
+          l_lds[b][threadIdx.x] = none ? 0.f : -l * kLog2e;
+          sees_lds[b][threadIdx.x] = none ? 0 : min(sees, s.end);
+        }
+        wait_vmcnt<0>();
+        __syncthreads();   // (the tile is there, and the one before is done with)
+        if (r0 + 32 < rows) issue(b ^ 1);
+        const int limit = sees_lds[b][c];
+        if (!__any(limit > key_lo)) continue;
+        const bool full = whole && !__any(limit < key_hi);
+        bf16x8_t q[NS];
+#pragma unroll
+        for (int x = 0; x < NS; ++x)
+          q[x] = *reinterpret_cast<const bf16x8_t*>(&q_lds[b][c * RB + ((2 * x + hh) ^ (D == 128 ? c & 15 : (c >> 1) & 7)) * 16]);
+        float nl[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&l_lds[b][8 * j + 4 * hh]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) nl[4 * j + i] = x[i];
+        }
+        f32x16_t x[2] = {};
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+          for (int y = 0; y < NS; ++y) x[z] = mma32(q[y], k[z][y], x[z]);
+        if (full) {
+#pragma unroll
+          for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[z] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[z][i], a.scale_log2, nl[i]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int end = sees_lds[b][8 * j + 4 * hh + i];
+#pragma unroll
+              for (int z = 0; z < 2; ++z) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[z][4 * j + i], a.scale_log2, nl[4 * j + i]));
+                sum[z] += t[z] < end ? w : 0.f;
+              }
+            }
+        }
+      }
+      __syncthreads();   // (the next sequence's first tile goes to a buffer that may still be read)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const float w = halves_sum(sum[z]);
+        if (hh == 0 && ok[z] && t[z] < s.end) {
+          const int64_t at = ((int64_t)seq * H + h) * a.width + t[z];
+          const bool old = t[z] < s.start && a.decay != 0.f;
+          a.weights_out[at] = old ? __builtin_fmaf(a.decay, a.weights[at], w) : w;
+        }
+      }
+    }
+  }
+}
+
+// (the body in a function of its own: the host's pass does not know the direct loads)
+template <bool KVQ, int D>
+__global__ __launch_bounds__(256) void weights_wide_kernel(WeightArgs a) { weights_wide<KVQ, D>(a); }
+
+// Whether the wide kernel takes a call (of bf16 queries): where a sequence has 32 rows or more on
+// average.
+bool many_rows(const halo_weight_sizes_t& s, bool lists, int group) {
+  return (int64_t)(lists ? s.num_entries : s.num_seqs) * group >= 32 * (int64_t)s.num_seqs;
+}
+
 halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_t* params,
                            const halo_weight_sizes_t* sizes, const int32_t* page_ids, const int32_t* seq_page_indptr,
                            const int32_t* seq_start, const int32_t* seq_end, const int32_t* row_indptr,
@@ -273,12 +482,16 @@ halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_
                row_end, error_flag, params->num_pool_pages, sizes->num_seqs, sizes->num_rows, sizes->num_entries,
                sizes->width, H, params->num_q_heads / H, params->sm_scale * kLog2e, decay};
   (void)hipGetLastError();
+  const bool wide = params->kv_dtype == HALO_BF16 && many_rows(*sizes, row_indptr != nullptr, g.group);
   by_type_and_dim(params, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
     const dim3 grid(2048), block(256);
-    if (kvq) hipLaunchKernelGGL((weights_kernel<T, true, D>), grid, block, 0, static_cast<hipStream_t>(stream), g);
-    else hipLaunchKernelGGL((weights_kernel<T, false, D>), grid, block, 0, static_cast<hipStream_t>(stream), g);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (wide && kvq) hipLaunchKernelGGL((weights_wide_kernel<true, D>), grid, block, 0, s, g);
+    else if (wide) hipLaunchKernelGGL((weights_wide_kernel<false, D>), grid, block, 0, s, g);
+    else if (kvq) hipLaunchKernelGGL((weights_kernel<T, true, D>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((weights_kernel<T, false, D>), grid, block, 0, s, g);
   });
   return hip_check("attention weights launch");
 }
