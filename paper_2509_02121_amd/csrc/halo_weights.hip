@@ -269,26 +269,31 @@ __device__ __forceinline__ void load_keys32(const uint8_t* tile, int key, int hh
 }
 
 // A workgroup takes jobs of 16 slots of one head (which may span sequences), a wave four of the pages, 64 keys, as
-// fragments in registers. 32 rows at a time go to LDS, by direct loads, while the
-// ones before are worked on; rows are the A operand of 32x32x16 MFMAs, so a lane has 16
-// rows of a key. Bound by the VALU: a product's 64 results take a multiply-add, an
+// fragments in registers. Rows are the A operand of 32x32x16 MFMAs, 32 of them a tile, so a lane
+// has 16 rows of a key. Bound by the VALU: a product's 64 results take a multiply-add, an
 // exponential (four times as long) and an addition.
-// LDS: 16-byte unit u of row r lies at place u ^ r (mod the units of a row; at d 64 r / 2), so that
+// Rows go to LDS in batches of four tiles, by direct loads, a batch while the one before is worked on. What these need to
+// know of their rows, and the rows' lse and limits, lies in LDS too: a batch's lists are loaded three batches
+// ahead, and what they point to one batch later.
+// 16-byte unit u of row r of a tile lies at place u ^ r (mod the units of a row; at d 64 r / 2), so that
 // the 32 rows' units of one fragment are in different banks.
 template <bool KVQ, int D>
 __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
   constexpr int NS = D / 16, U = D / 8, RB = 2 * D, kSlots = 16, NI = D / 64, kRowsPer = 64 / U;
   constexpr int64_t kTile = KVQ ? kvq_k_tile<D>() : 32 * D;
-  __shared__ __align__(1024) uint8_t q_lds[2][32 * RB];
-  __shared__ __align__(16) float l_lds[2][32];
-  __shared__ __align__(16) int sees_lds[2][32];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // (two arrays, and nothing on its way where the loop begins: the compiler then knows that reads of one do not
+  // wait for loads to the other)
+  __shared__ __align__(1024) uint8_t q0[128 * RB], q1[128 * RB];
+  __shared__ int64_t row_lds[4][128];   // where the rows begin
+  __shared__ int sees_lds[4][128];
+  __shared__ __align__(16) float l_lds[4][128];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, hh = lane >> 5;
   const int H = a.num_kv_heads, G = a.group;
-  const int step_e = 32 / G, step_g = 32 % G;   // 32 rows on
   const int first = a.seq_page_indptr[0];
   const int64_t slots = (int64_t)a.seq_page_indptr[a.num_seqs] - first;
   const int64_t jobs = (slots + kSlots - 1) / kSlots * H;
+  const int64_t row_bytes = (int64_t)H * G * RB;
   for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
     const int h = (int)(job % H);
     const int64_t chunk = job / H * kSlots, chunk_end = min(slots, chunk + kSlots), mine = chunk + 4 * wave;
@@ -310,7 +315,7 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
       const WeightSeq s(a, seq);
       const int64_t from = slot, upto = min(chunk_end, (int64_t)s.next - first);
       slot = upto;
-      if ((s.bad || s.bad_rows || a.num_pool_pages == 0) && threadIdx.x == 0 && a.error_flag) a.error_flag[0] = 1;
+      if ((s.bad || s.bad_rows || a.num_pool_pages == 0) && tid == 0 && a.error_flag) a.error_flag[0] = 1;
       const int64_t place = first - (int64_t)s.base;   // of slot 0 in the sequence's list
       if (s.bad || a.num_pool_pages == 0 || (place + from) * 16 >= s.end) continue;
       // this wave's keys in the sequence
@@ -328,98 +333,170 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
       }
       float sum[2] = {0.f, 0.f};
       const int64_t rows = (int64_t)(s.e1 - s.e0) * G;
-      // The rows of the tiles: of a wave's direct loads lane / U (+ kRowsPer j), of the lse and
-      // the limits the thread's own. e: its entry (one tile ahead of at, the row of q).
-      int e[NI + 1], g[NI + 1], row[NI + 1];
-      auto row_of = [&](int e) {   // of entry e: its row of q, or -1 (behind the last: none is looked up)
-        return e < s.e1 ? a.rows ? max(a.rows[e], -1) : e : -2;
-      };
-#pragma unroll
-      for (int j = 0; j <= NI; ++j) {
-        const int r = j < NI ? wave * 8 + j * kRowsPer + lane / U : threadIdx.x & 31;
-        e[j] = s.e0 + r / G;
-        g[j] = r % G;
-        row[j] = rows > 0 ? row_of(e[j]) : -2;
-      }
-      float l = 0.f;
-      int sees = 0;
-      // begins the loads of a tile's rows and finds the next tile's
-      auto issue = [&](int b) {
-#pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          const int r = wave * 8 + j * kRowsPer + lane / U;
-          const int at = row[j] >= 0 && row[j] < a.num_rows ? row[j] : 0;   // (one that is none: any row, unseen)
-          const int unit = (lane % U) ^ (D == 128 ? r & 15 : (r >> 1) & 7);
-          __builtin_amdgcn_global_load_lds(
-              static_cast<const uint8_t*>(a.q) + ((int64_t)at * H * G + (int64_t)h * G + g[j]) * RB + unit * 16,
-              &q_lds[b][(wave * 8 + j * kRowsPer) * RB], 16, 0, 0);
-        }
-        const int at = row[NI];
-        const bool fine = at >= 0 && at < a.num_rows;
-        l = fine ? a.lse[(int64_t)at * H * G + (int64_t)h * G + g[NI]] : kNegInf;
-        sees = fine ? a.row_end ? a.row_end[e[NI]] : s.end : 0;
-        if (!fine && at != -2 && a.error_flag) a.error_flag[0] = 1;
-#pragma unroll
-        for (int j = 0; j <= NI; ++j) {
-          e[j] += step_e;
-          g[j] += step_g;
-          if (g[j] >= G) {
-            g[j] -= G;
-            ++e[j];
-          }
-          row[j] = row_of(e[j]);
-        }
-      };
-      if (rows > 0) issue(0);
-      int b = 0;
-      for (int64_t r0 = 0; r0 < rows; r0 += 32, b ^= 1) {
-        if (threadIdx.x < 32) {
+      if (rows > 0) {
+        // A batch's rows, one to each of 128 threads (the other half does the same): the entry, then its row of q,
+        // then that row's lse and limit. Rows behind the last one see nothing.
+        int e = 0, g = 0, row = 0, sees = 0;
+        float l = 0.f;
+        auto find = [&](int64_t batch) {
+          const int64_t r = min(batch * 128 + (tid & 127), rows);
+          e = s.e0 + (int)(r / G);
+          g = (int)(r % G);
+          const int in = min(e, s.e1 - 1);   // (there is one)
+          row = a.rows ? a.rows[in] : in;
+          if (r >= rows) e = -1;
+        };
+        auto look = [&] {
+          const bool fine = row >= 0 && row < a.num_rows;
+          if (!fine && e >= 0 && a.error_flag) a.error_flag[0] = 1;
+          if (!fine) row = 0;
+          l = a.num_rows > 0 ? a.lse[(int64_t)row * H * G + (int64_t)h * G + g] : kNegInf;
+          sees = a.row_end ? a.row_end[max(e, s.e0)] : s.end;
+          if (!fine || e < 0) sees = 0;
+        };
+        auto keep = [&](int64_t batch) {
           const bool none = l == kNegInf;   // (it saw no key)
-          l_lds[b][threadIdx.x] = none ? 0.f : -l * kLog2e;
-          sees_lds[b][threadIdx.x] = none ? 0 : min(sees, s.end);
-        }
-        wait_vmcnt<0>();
-        __syncthreads();   // (the tile is there, and the one before is done with)
-        if (r0 + 32 < rows) issue(b ^ 1);
-        const int limit = sees_lds[b][c];
-        if (!__any(limit > key_lo)) continue;
-        const bool full = whole && !__any(limit < key_hi);
-        bf16x8_t q[NS];
+          const int at = (int)(batch & 3), r = tid & 127;
+          row_lds[at][r] = row * row_bytes + (int64_t)(h * G + g) * RB;
+          l_lds[at][r] = none ? 0.f : -l * kLog2e;
+          sees_lds[at][r] = none ? 0 : min(sees, s.end);
+        };
+        const int64_t tiles = (rows + 31) / 32;
+        auto issue = [&](int64_t batch, uint8_t* q) {
+          if (a.num_rows == 0) return;
 #pragma unroll
-        for (int x = 0; x < NS; ++x)
-          q[x] = *reinterpret_cast<const bf16x8_t*>(&q_lds[b][c * RB + ((2 * x + hh) ^ (D == 128 ? c & 15 : (c >> 1) & 7)) * 16]);
-        float nl[16];
+          for (int i = 0; i < 4; ++i) {
+            if (batch * 4 + i >= tiles) break;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&l_lds[b][8 * j + 4 * hh]);
+            for (int j = 0; j < NI; ++j) {
+              const int r = wave * 8 + j * kRowsPer + lane / U;
+              const int unit = (lane % U) ^ (D == 128 ? r & 15 : (r >> 1) & 7);
+              __builtin_amdgcn_global_load_lds(static_cast<const uint8_t*>(a.q) + row_lds[batch & 3][32 * i + r] + unit * 16,
+                                               q + (32 * i + wave * 8 + j * kRowsPer) * RB, 16, 0, 0);
+            }
+          }
+        };
+        // A tile's scores go to x while the exponentials of the one before are taken from y: the matrix
+        // products of one wave run beside its own VALU instructions. A tile that no key of the wave is
+        // seen by is left out; one whose rows see all of them needs no limits.
+        uint64_t sees_any[2], sees_part[2];   // of a batch's rows: those that see a key of the wave, and not all of them
+        auto look_at = [&](int64_t batch) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) nl[4 * j + i] = x[i];
-        }
-        f32x16_t x[2] = {};
+          for (int j = 0; j < 2; ++j) {
+            const int limit = sees_lds[batch & 3][64 * j + lane];
+            sees_any[j] = __ballot(limit > key_lo);
+            sees_part[j] = __ballot(limit < key_hi);
+          }
+        };
+        auto read_q = [&](const uint8_t* q_lds, bf16x8_t (&q)[NS]) {
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
+          for (int x = 0; x < NS; ++x)
+            q[x] = *reinterpret_cast<const bf16x8_t*>(q_lds + c * RB + ((2 * x + hh) ^ (D == 128 ? c & 15 : (c >> 1) & 7)) * 16);
+        };
+        auto read_l = [&](int64_t tile, float (&nl)[16]) {
 #pragma unroll
-          for (int y = 0; y < NS; ++y) x[z] = mma32(q[y], k[z][y], x[z]);
-        if (full) {
+          for (int j = 0; j < 4; ++j) {
+            const f32x4_t l = *reinterpret_cast<const f32x4_t*>(&l_lds[(tile >> 2) & 3][(tile & 3) * 32 + 8 * j + 4 * hh]);
 #pragma unroll
-          for (int z = 0; z < 2; ++z)
+            for (int i = 0; i < 4; ++i) nl[4 * j + i] = l[i];
+          }
+        };
+        auto product = [&](int y, const bf16x8_t (&q)[NS], f32x16_t (&x)[2]) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[z] += __builtin_amdgcn_exp2f(__builtin_fmaf(x[z][i], a.scale_log2, nl[i]));
-        } else {
+          for (int z = 0; z < 2; ++z) x[z] = mma32(q[y], k[z][y], y == 0 ? f32x16_t{} : x[z]);
+        };
+        auto exponentials = [&](int i, const f32x16_t (&y)[2], const float (&nl)[16]) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
+          for (int z = 0; z < 2; ++z) sum[z] += __builtin_amdgcn_exp2f(__builtin_fmaf(y[z][i], a.scale_log2, nl[i]));
+        };
+        auto masked = [&](int64_t tile, const f32x16_t (&y)[2]) {
+          float nl[16];
+          read_l(tile, nl);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int end = sees_lds[b][8 * j + 4 * hh + i];
+          for (int i = 0; i < 16; ++i) {
+            const int end = sees_lds[(tile >> 2) & 3][(tile & 3) * 32 + 8 * (i >> 2) + 4 * hh + (i & 3)];
 #pragma unroll
-              for (int z = 0; z < 2; ++z) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[z][4 * j + i], a.scale_log2, nl[4 * j + i]));
-                sum[z] += t[z] < end ? w : 0.f;
+            for (int z = 0; z < 2; ++z) {
+              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(y[z][i], a.scale_log2, nl[i]));
+              sum[z] += t[z] < end ? w : 0.f;
+            }
+          }
+        };
+        bool held_any = false, held_full = false;   // of the tile whose scores are held
+        // tile 4 batch + i's scores to x, the exponentials of the one before, whose scores are in y
+        auto step = [&](int64_t batch, int i, const uint8_t* q_lds, f32x16_t (&x)[2], const f32x16_t (&y)[2]) {
+          const bool more = i < 4;
+          const bool any = more && (uint32_t)(sees_any[(i & 2) / 2] >> (32 * (i & 1))) != 0;
+          const bool full = any && whole && (uint32_t)(sees_part[(i & 2) / 2] >> (32 * (i & 1))) == 0;
+          const int64_t tile = batch * 4 + i;
+          if (any && held_full) {
+            bf16x8_t q[NS];
+            float nl[16];
+            read_l(tile - 1, nl);
+            read_q(q_lds, q);
+            // (in this order: the two chains of products in turn, each with its share of the rest)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+              product(s, q, x);
+#pragma unroll
+              for (int j = 0; j < 16 / NS; ++j) exponentials(16 / NS * s + j, y, nl);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          } else {
+            if (any) {
+              bf16x8_t q[NS];
+              read_q(q_lds, q);
+#pragma unroll
+              for (int s = 0; s < NS; ++s) {
+                product(s, q, x);
+                __builtin_amdgcn_sched_barrier(0);
               }
             }
+            if (held_full) {
+              float nl[16];
+              read_l(tile - 1, nl);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) exponentials(j, y, nl);
+            } else if (held_any) {
+              masked(tile - 1, y);
+            }
+          }
+          held_any = any;
+          held_full = full;
+        };
+        f32x16_t x[2], y[2];
+        // one batch: the next one's loads begin, and those of what the ones behind it need
+        auto work = [&](int64_t batch, const uint8_t* q, uint8_t* next) {
+          look_at(batch);
+          look();
+          issue(batch + 1, next);
+          step(batch, 0, q, x, y);
+          step(batch, 1, q + 32 * RB, y, x);
+          keep(batch + 2);
+          find(batch + 3);
+          step(batch, 2, q + 64 * RB, x, y);
+          step(batch, 3, q + 96 * RB, y, x);
+          wait_vmcnt<0>();
+          __syncthreads();
+        };
+        find(0);
+        look();
+        keep(0);
+        find(1);
+        look();
+        keep(1);
+        find(2);
+        __syncthreads();
+        issue(0, q0);
+        wait_vmcnt<0>();
+        __syncthreads();
+        for (int64_t batch = 0; batch * 4 < tiles; batch += 2) {
+          work(batch, q0, q1);
+          if ((batch + 1) * 4 < tiles) work(batch + 1, q1, q0);
         }
+        step((tiles - 1) / 4, 4, q0, x, y);   // (whole batches, so that the last scores are in y)
+        __syncthreads();   // (the next sequence's first batches go where the last tile's limits may still be read)
       }
-      __syncthreads();   // (the next sequence's first tile goes to a buffer that may still be read)
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
         const float w = halves_sum(sum[z]);
@@ -435,7 +512,7 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
 
 // (the body in a function of its own: the host's pass does not know the direct loads)
 template <bool KVQ, int D>
-__global__ __launch_bounds__(256) void weights_wide_kernel(WeightArgs a) { weights_wide<KVQ, D>(a); }
+__global__ __launch_bounds__(256, 2) void weights_wide_kernel(WeightArgs a) { weights_wide<KVQ, D>(a); }
 
 // Whether the wide kernel takes a call (of bf16 queries): where a sequence has 32 rows or more on
 // average.
