@@ -173,7 +173,12 @@ __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
         // (a page that is none is read as page 0 and not written)
         Fmt::load_keys(static_cast<const uint8_t*>(a.k_pool) + ((int64_t)(ok[p] ? pid : 0) * H + h) * Fmt::kTile, lane, k[p]);
       }
-      float sum[NP] = {};
+      float sum[NP] = {}, old[NP];
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int t = t0 + 16 * p + key;
+        old[p] = a.decay != 0.f && p < n && t < s.end && t < s.start ? a.weights[((int64_t)seq * H + h) * a.width + t] : 0.f;
+      }
       const int64_t rows = (int64_t)(s.e1 - s.e0) * G;
       for (int64_t r0 = 0; r0 < rows; r0 += 16) {
         if (rows > 16 || loaded != seq) {
@@ -225,9 +230,7 @@ __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
         const float w = rows_sum(sum[p]);
         const int t = t0 + 16 * p + key;
         if (ok[p] && p < n && t < s.end && grp == 0) {
-          const int64_t at = ((int64_t)seq * H + h) * a.width + t;
-          const bool old = t < s.start && a.decay != 0.f;
-          a.weights_out[at] = old ? __builtin_fmaf(a.decay, a.weights[at], w) : w;
+          a.weights_out[((int64_t)seq * H + h) * a.width + t] = __builtin_fmaf(a.decay, old[p], w);
         }
       }
     }
@@ -332,32 +335,35 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
         if (in && !ok[b] && (place + at) * 16 < s.end && a.error_flag) a.error_flag[0] = 1;
       }
       float sum[2] = {0.f, 0.f};
-      const int64_t rows = (int64_t)(s.e1 - s.e0) * G;
+      const int64_t rows = (int64_t)(s.e1 - s.e0) * G;   // (below INT32_MAX - 1024)
       if (rows > 0) {
-        // A batch's rows, one to each of 128 threads (the other half does the same): the entry, then its row of q,
-        // then that row's lse and limit. Rows behind the last one see nothing.
+        // A batch's rows, one to each of 128 threads (the other half does the same, and at the start the second
+        // batch): the entry, then its row of q, then that row's lse and limit. Rows behind the last one see nothing.
         int e = 0, g = 0, row = 0, sees = 0;
+        bool fine = false;
         float l = 0.f;
-        auto find = [&](int64_t batch) {
-          const int64_t r = min(batch * 128 + (tid & 127), rows);
-          e = s.e0 + (int)(r / G);
-          g = (int)(r % G);
+        auto find = [&](int64_t first_row) {
+          const int r = (int)min(first_row, rows);
+          e = (int)((uint32_t)r / (uint32_t)G);
+          g = r - e * G;
+          e += s.e0;
           const int in = min(e, s.e1 - 1);   // (there is one)
           row = a.rows ? a.rows[in] : in;
           if (r >= rows) e = -1;
         };
-        auto look = [&] {
-          const bool fine = row >= 0 && row < a.num_rows;
+        auto place_row = [&](int at, int r) {
+          fine = row >= 0 && row < a.num_rows;
           if (!fine && e >= 0 && a.error_flag) a.error_flag[0] = 1;
           if (!fine) row = 0;
+          row_lds[at][r] = row * row_bytes + (int64_t)(h * G + g) * RB;
+        };
+        auto look = [&] {
           l = a.num_rows > 0 ? a.lse[(int64_t)row * H * G + (int64_t)h * G + g] : kNegInf;
           sees = a.row_end ? a.row_end[max(e, s.e0)] : s.end;
           if (!fine || e < 0) sees = 0;
         };
-        auto keep = [&](int64_t batch) {
+        auto keep = [&](int at, int r) {
           const bool none = l == kNegInf;   // (it saw no key)
-          const int at = (int)(batch & 3), r = tid & 127;
-          row_lds[at][r] = row * row_bytes + (int64_t)(h * G + g) * RB;
           l_lds[at][r] = none ? 0.f : -l * kLog2e;
           sees_lds[at][r] = none ? 0 : min(sees, s.end);
         };
@@ -468,26 +474,30 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
         // one batch: the next one's loads begin, and those of what the ones behind it need
         auto work = [&](int64_t batch, const uint8_t* q, uint8_t* next) {
           look_at(batch);
-          look();
+          const bool behind = (batch + 2) * 4 < tiles;
+          if (behind) {
+            place_row((int)(batch + 2) & 3, tid & 127);
+            look();
+          }
           issue(batch + 1, next);
           step(batch, 0, q, x, y);
           step(batch, 1, q + 32 * RB, y, x);
-          keep(batch + 2);
-          find(batch + 3);
+          if (behind) {
+            keep((int)(batch + 2) & 3, tid & 127);
+            find((batch + 3) * 128 + (tid & 127));
+          }
           step(batch, 2, q + 64 * RB, x, y);
           step(batch, 3, q + 96 * RB, y, x);
           wait_vmcnt<0>();
           __syncthreads();
         };
-        find(0);
-        look();
-        keep(0);
-        find(1);
-        look();
-        keep(1);
-        find(2);
+        find(tid);
+        place_row(tid >> 7, tid & 127);
         __syncthreads();
         issue(0, q0);
+        look();
+        keep(tid >> 7, tid & 127);
+        if (tiles > 8) find(256 + (tid & 127));
         wait_vmcnt<0>();
         __syncthreads();
         for (int64_t batch = 0; batch * 4 < tiles; batch += 2) {
@@ -545,6 +555,8 @@ halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_
   if (!row_indptr && (rows || row_end) && sizes->num_entries < sizes->num_seqs)
     return fail(HALO_ERR_INVALID_ARGUMENT, "without row_indptr, rows and row_end have an element for each sequence");
   if (!aligned16(k_pool) || !aligned16(q)) return fail(HALO_ERR_INVALID_ARGUMENT, "k_pool and q must be 16-byte aligned");
+  if ((int64_t)sizes->num_entries * (params->num_q_heads / H) > INT32_MAX - 1024)
+    return fail(HALO_ERR_UNSUPPORTED, "num_entries * num_q_heads / num_kv_heads must be less than 2^31 - 1024");
   const int64_t n = sizes->num_seqs, cells = n * H * sizes->width * 4, elt = params->kv_dtype == HALO_BF16 ? 2 : 4;
   const int64_t rows_h = (int64_t)sizes->num_rows * params->num_q_heads, entries = 4 * (int64_t)sizes->num_entries;
   const int64_t tile = kvq ? params->head_dim * 8 + params->head_dim / 2 : 16 * params->head_dim * elt;
