@@ -237,6 +237,151 @@ __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- a row for each sequence
+
+// What a lane loads of a page's 16 keys: fragments, or the codes and scales that make them.
+template <typename T, bool KVQ, int D>
+struct PageKeys {
+  using Fmt = KeyFormat<T, KVQ, D>;
+  using F = typename Fmt::F;
+  F k[D / 32];
+  __device__ __forceinline__ void load(const uint8_t* tile, int lane) { Fmt::load_keys(tile, lane, k); }
+  __device__ __forceinline__ F fragment(int s) const { return k[s]; }
+};
+template <typename T, int D>
+struct PageKeys<T, true, D> {
+  uint32_t codes[D / 32], scales;
+  __device__ __forceinline__ void load(const uint8_t* tile, int lane) {
+    const uint8_t* at = tile + lane * (D / 8);
+    const uint8_t* sc = tile + D * 8 + (lane & 15) * (D / 32);   // (lane 16 grp + key is unit (grp, key))
+    if constexpr (D == 128) {
+      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(at);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) codes[s] = x[s];
+      scales = *reinterpret_cast<const uint32_t*>(sc);
+    } else {
+      const u32x2_t x = *reinterpret_cast<const u32x2_t*>(at);
+      codes[0] = x[0];
+      codes[1] = x[1];
+      scales = *reinterpret_cast<const uint16_t*>(sc);
+    }
+  }
+  __device__ __forceinline__ bf16x8_t fragment(int s) const { return kvq_decode_bf16(codes[s], kvq_scale_byte(scales, s)); }
+};
+// Pages on their way, and waves a SIMD whose registers hold as many.
+template <typename T, bool KVQ, int D>
+constexpr int step_ring() { return KVQ ? 6 : sizeof(T) == 4 && D == 128 ? 2 : 4; }
+// (fp32 rows, and their parts, take more)
+template <typename T> constexpr int step_waves() { return sizeof(T) == 2 ? 4 : 2; }
+
+// A decode step: one entry a sequence and at most 16 q heads of a kv head, so one tile of
+// rows, which stays in registers while the sequence's pages pass by. A wave has one run of slots of one
+// head, as long as keeps the chip full once; pages are loaded a ring ahead of their use, and a
+// page's old weights are waited for when its place in the ring comes round. Bound by HBM: each
+// key is read once.
+template <typename T, bool KVQ, int D>
+__global__ __launch_bounds__(256, step_waves<T>()) void weights_step_kernel(WeightArgs a) {
+  using Fmt = KeyFormat<T, KVQ, D>;
+  using F = typename Fmt::F;
+  constexpr int NS = D / 32, R = step_ring<T, KVQ, D>(), PARTS = Fmt::kParts;
+  const int lane = threadIdx.x & 63, key = lane & 15, grp = lane >> 4;
+  const int H = a.num_kv_heads, G = a.group;
+  const int first = a.seq_page_indptr[0];
+  const int64_t slots = (int64_t)a.seq_page_indptr[a.num_seqs] - first;
+  const int64_t waves = (int64_t)gridDim.x * 4, wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int run = (int)min((int64_t)64, max((int64_t)1, (slots * H + waves - 1) / waves));
+  const int64_t jobs = (slots + run - 1) / run * H;
+  for (int64_t job = wave; job < jobs; job += waves) {
+    const int h = (int)(job % H);
+    const int64_t chunk = job / H * run;
+    const int n = (int)min((int64_t)run, slots - chunk);
+    const int from = first + (int)chunk;
+    const int ids = a.page_ids[from + min(lane, n - 1)];
+    int seq = last_at_or_below(a.seq_page_indptr, a.num_seqs, from, lane);
+    const uint8_t* pool = static_cast<const uint8_t*>(a.k_pool) + h * Fmt::kTile;
+    PageKeys<T, KVQ, D> keys[R];
+    float w[R], old[R];
+    int64_t to[R];   // of the ring's pages: where their weights go, and how many (the same in every lane)
+    int count[R];
+    auto load = [&](int i, int r) {   // (behind the last page: that one again)
+      const int pid = __builtin_amdgcn_readlane(ids, min(i, n - 1));
+      keys[r].load(pool + (int64_t)(pid >= 0 && pid < a.num_pool_pages ? pid : 0) * H * Fmt::kTile, lane);
+    };
+    auto finish = [&](int r) {
+      if (lane < count[r]) a.weights_out[to[r] + lane] = __builtin_fmaf(a.decay, old[r], w[r]);
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      to[r] = count[r] = 0;
+      w[r] = old[r] = 0.f;
+      load(r, r);
+    }
+    int next = from;   // the first slot of another sequence than the one in q
+    int base = 0, end = 0, start = 0, sees = 0;
+    bool bad = false;
+    F q[PARTS][NS];
+    float l2[4];
+    for (int i0 = 0; i0 < n; i0 += R) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int i = i0 + r, slot = from + min(i, n - 1);
+        finish(r);
+        count[r] = 0;
+        if (i < n) {
+          if (slot >= next) {   // another sequence: its row
+            while (slot >= a.seq_page_indptr[seq + 1]) ++seq;   // (ends at num_seqs - 1)
+            const WeightSeq s(a, seq);
+            next = s.next;
+            base = s.base;
+            end = s.end;
+            start = a.decay != 0.f ? s.start : 0;
+            bad = s.bad;
+            const int at = a.rows ? a.rows[seq] : seq;
+            const bool fine = at >= 0 && at < a.num_rows;
+            sees = fine ? a.row_end ? min(a.row_end[seq], end) : end : 0;
+            if ((bad || !fine) && lane == 0 && a.error_flag) a.error_flag[0] = 1;
+            const int64_t row = (int64_t)(fine ? at : 0) * H * G + (int64_t)h * G;
+            if (fine && key < G) Fmt::load_query(static_cast<const T*>(a.q) + (row + key) * D, grp, q);
+            else
+#pragma unroll
+              for (int x = 0; x < PARTS; ++x)
+#pragma unroll
+                for (int y = 0; y < NS; ++y) q[x][y] = zero_frag<F>();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) l2[j] = fine && 4 * grp + j < G ? a.lse[row + 4 * grp + j] * kLog2e : kNegInf;
+          }
+          const int t0 = (slot - base) * 16, pid = __builtin_amdgcn_readlane(ids, i);
+          const bool ok = pid >= 0 && pid < a.num_pool_pages, here = !bad && t0 < end;
+          if (here && !ok && lane == 0 && a.error_flag) a.error_flag[0] = 1;
+          if (here && ok) {
+            f32x4_t x = {};
+#pragma unroll
+            for (int y = 0; y < NS; ++y) {
+              const F k = keys[r].fragment(y);
+#pragma unroll
+              for (int m = 0; m < PARTS; ++m) x = mma(q[PARTS - 1 - m][y], k, x);
+            }
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], a.scale_log2, -l2[j]));
+              sum += l2[j] == kNegInf ? 0.f : p;   // (no such row, or it saw no key)
+            }
+            sum = rows_sum(sum);
+            w[r] = t0 + key < sees ? sum : 0.f;
+            to[r] = ((int64_t)seq * H + h) * a.width + t0;
+            count[r] = min(16, end - t0);
+            old[r] = lane < min(min(start, end) - t0, 16) ? a.weights[to[r] + lane] : 0.f;
+          }
+        }
+        load(i + R, r);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) finish(r);
+  }
+}
+
 // ---------------------------------------------------------------- many rows
 
 // Fragments of 32 keys for 32x32x16 products: lane (c, hh) holds dims 16 s + 8 hh .. + 7 of
@@ -571,13 +716,16 @@ halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_
                row_end, error_flag, params->num_pool_pages, sizes->num_seqs, sizes->num_rows, sizes->num_entries,
                sizes->width, H, params->num_q_heads / H, params->sm_scale * kLog2e, decay};
   (void)hipGetLastError();
+  const bool step = !row_indptr && g.group <= 16 && params->num_pool_pages > 0;
   const bool wide = params->kv_dtype == HALO_BF16 && many_rows(*sizes, row_indptr != nullptr, g.group);
   by_type_and_dim(params, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
     const dim3 grid(2048), block(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (wide && kvq) hipLaunchKernelGGL((weights_wide_kernel<true, D>), grid, block, 0, s, g);
+    if (step && kvq) hipLaunchKernelGGL((weights_step_kernel<T, true, D>), dim3(kNumCUs * step_waves<T>()), block, 0, s, g);
+    else if (step) hipLaunchKernelGGL((weights_step_kernel<T, false, D>), dim3(kNumCUs * step_waves<T>()), block, 0, s, g);
+    else if (wide && kvq) hipLaunchKernelGGL((weights_wide_kernel<true, D>), grid, block, 0, s, g);
     else if (wide) hipLaunchKernelGGL((weights_wide_kernel<false, D>), grid, block, 0, s, g);
     else if (kvq) hipLaunchKernelGGL((weights_kernel<T, true, D>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((weights_kernel<T, false, D>), grid, block, 0, s, g);
