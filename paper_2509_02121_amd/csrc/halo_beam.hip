@@ -432,63 +432,93 @@ struct BeamTableArgs {
 // child. One that is malformed is its own parents' item, with no pages in a row whose
 // length does not fit.
 struct ItemBeams {
-  int32_t parent[kMaxBeams], len[kMaxBeams], pages[kMaxBeams], copied[kMaxBeams], mother[kMaxBeams], bad;
-  __device__ __forceinline__ void load(const BeamTableArgs& a, int item, bool as_it_is) {
-    const int tid = threadIdx.x, W = a.s.num_beams;
-    if (tid == 0) bad = 0;
-    __syncthreads();
-    if (tid < W) {
-      const int p = a.parents[(int64_t)item * a.s.parents_stride + tid], n = a.seq_len[(int64_t)item * W + tid];
-      const bool fits = n >= 0 && (int64_t)n <= (int64_t)a.s.table_width * 16;
-      parent[tid] = p;
-      len[tid] = n;
-      pages[tid] = fits ? (int)(((int64_t)n + 15) >> 4) : 0;
-      mother[tid] = 0;
-      if (p < -1 || p >= W || !fits) bad = 1;
+  int32_t parent[kMaxBeams], len[kMaxBeams], pages[kMaxBeams], copied[kMaxBeams];
+  uint64_t mothers;   // beams with children
+  int32_t bad;
+  // A beam's parent and length, by the lane of the same number.
+  static __device__ __forceinline__ void read(const BeamTableArgs& a, int item, int lane, int& p, int& n) {
+    const int W = a.s.num_beams;
+    p = lane < W ? a.parents[(int64_t)item * a.s.parents_stride + lane] : -1;
+    n = lane < W ? a.seq_len[(int64_t)item * W + lane] : 0;
+  }
+  // Takes them, by one wave; to be read after a barrier. as_it_is: as if the item were malformed.
+  __device__ __forceinline__ void take(const BeamTableArgs& a, int p, int n, bool as_it_is, int lane) {
+    const int W = a.s.num_beams;
+    const bool fits = n >= 0 && (int64_t)n <= (int64_t)a.s.table_width * 16;
+    const bool wrong = __any(p < -1 || p >= W || !fits);
+    if ((wrong || as_it_is) && lane < W) p = lane;
+    uint64_t children = 0;
+    bool later = false;
+    for (int k = 0; k < W; ++k) {
+      const int of = __builtin_amdgcn_readlane(p, k);
+      if (of >= 0) children |= 1ull << of;
+      later |= k < lane && of == p;
     }
-    __syncthreads();
-    if (tid < W) {
-      if (bad || as_it_is) parent[tid] = tid;
+    const int of_parent = __shfl(n, max(p, 0));
+    if (lane < W) {
+      parent[lane] = p;
+      len[lane] = n;
+      pages[lane] = fits ? (int)(((int64_t)n + 15) >> 4) : 0;
+      copied[lane] = p >= 0 && later && (of_parent & 15) != 0;
     }
-    __syncthreads();
-    if (tid < W) {
-      const int p = parent[tid];
-      bool later = false;
-      for (int k = 0; k < tid; ++k) later |= parent[k] == p;
-      copied[tid] = p >= 0 && later && (len[p] & 15) != 0;
-      if (p >= 0) mother[p] = 1;   // (the same value from every child)
+    if (lane == 0) {
+      mothers = children;
+      bad = wrong;
     }
-    __syncthreads();
   }
 };
+
+// Beams whose places in a column a thread holds at a time.
+constexpr int kHeld = 8;
 
 // A workgroup for each item: how many pages it takes, and which ones it frees. Beams
 // of an item share pages only in the same place of their rows, so a page of a
 // beam without children is free if no beam with children has it there, nor an
 // earlier beam without: each place of the rows is looked at by itself, W x W
-// comparisons, without counts of references.
+// comparisons, without counts of references. A thread has a place, and the pages of all
+// beams there (of more than kHeld beams: of kHeld at a time, against the others).
 __global__ __launch_bounds__(256) void beam_freed_kernel(BeamTableArgs a) {
   __shared__ ItemBeams m;
   __shared__ int sums[4];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, item = (int)blockIdx.x, W = a.s.num_beams;
-  m.load(a, item, false);
+  if (wave == 0) {
+    int p, n;
+    ItemBeams::read(a, item, lane, p, n);
+    m.take(a, p, n, false, lane);
+  }
+  __syncthreads();
   const int32_t* table = a.block_table + (int64_t)item * W * a.s.table_width;
   int32_t* list = a.freed + (int64_t)item * W * a.s.table_width;
-  int most = 0;
-  for (int b = 0; b < W; ++b) most = max(most, m.mother[b] ? 0 : m.pages[b]);
+  const uint64_t mothers = m.mothers;
+  int most = 0;   // places that hold a page which may be free
+  for (int b = 0; b < W; ++b) most = max(most, mothers >> b & 1 ? 0 : m.pages[b]);
   int done = 0;
   for (int c0 = 0; c0 < most; c0 += 256) {
     const int c = c0 + tid;
     uint64_t gone = 0;
-    for (int b = 0; b < W; ++b) {
-      if (m.mother[b] || c >= m.pages[b]) continue;
-      const int page = table[(int64_t)b * a.s.table_width + c];
-      bool held = false;
-      for (int k = 0; k < W; ++k)
-        if ((m.mother[k] || k < b) && c < m.pages[k]) held |= table[(int64_t)k * a.s.table_width + c] == page;
-      gone |= held ? 0ull : 1ull << b;
+    int mine = 0;
+    int32_t page[kHeld];
+    for (int b0 = 0; b0 < W; b0 += kHeld) {
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j)
+        page[j] = b0 + j < W && c < m.pages[b0 + j] ? table[(int64_t)(b0 + j) * a.s.table_width + c] : 0;
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        const int b = b0 + j;
+        if (b >= W || (mothers >> b & 1)) continue;
+        bool held = c >= m.pages[b];
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+          if (b0 + k < W && (k < j || (mothers >> (b0 + k) & 1))) held |= c < m.pages[b0 + k] && page[k] == page[j];
+        if (W > kHeld && !held)
+          for (int k = 0; k < W; ++k)
+            if (k < b0 || (k >= b0 + kHeld && (mothers >> k & 1)))
+              held |= c < m.pages[k] && table[(int64_t)k * a.s.table_width + c] == page[j];
+        gone |= held ? 0ull : 1ull << b;
+      }
     }
-    const int mine = __popcll(gone), upto = wave_inclusive_sum(mine);
+    mine = __popcll(gone);
+    const int upto = wave_inclusive_sum(mine);
     __syncthreads();
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
@@ -497,16 +527,21 @@ __global__ __launch_bounds__(256) void beam_freed_kernel(BeamTableArgs a) {
       at += w < wave ? sums[w] : 0;
       done += sums[w];
     }
-    while (gone) {
-      const int b = __builtin_ctzll(gone);
-      gone &= gone - 1;
-      list[at++] = table[(int64_t)b * a.s.table_width + c];
+    if (W <= kHeld) {
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j)
+        if (gone >> j & 1) list[at++] = page[j];
+    } else {
+      while (gone) {
+        const int b = __builtin_ctzll(gone);
+        gone &= gone - 1;
+        list[at++] = table[(int64_t)b * a.s.table_width + c];
+      }
     }
   }
-  if (tid == 0) {
-    int taken = 0;
-    for (int k = 0; k < W; ++k) taken += m.copied[k];
-    a.counts[item] = ItemCount{taken, done, m.bad, 0};
+  if (tid < 64) {
+    const int taken = __popcll(__ballot(tid < W && m.copied[tid]));
+    if (tid == 0) a.counts[item] = ItemCount{taken, done, m.bad, 0};
   }
 }
 
@@ -514,10 +549,15 @@ __global__ __launch_bounds__(256) void beam_freed_kernel(BeamTableArgs a) {
 // each one, which every workgroup makes itself.
 __global__ __launch_bounds__(256) void beam_rows_kernel(BeamTableArgs a) {
   __shared__ ItemBeams m;
-  __shared__ int64_t sums[4][5];
+  __shared__ int32_t sums[4][5];   // (a table has less than 2^31 pages)
+  __shared__ int32_t fresh[kMaxBeams];   // the pages that the copies take
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, W = a.s.num_beams;
   const int item = (int)(blockIdx.x / a.splits), split = (int)(blockIdx.x % a.splits);
-  int64_t s[5] = {0, 0, 0, 0, 0};   // taken and freed before the item, of all; malformed items
+  const bool any = item < a.s.num_items;
+  const int first = a.free_next[0];
+  int p = -1, n = 0;   // (loaded beside the counts)
+  if (any && wave == 0) ItemBeams::read(a, item, lane, p, n);
+  int32_t s[5] = {0, 0, 0, 0, 0};   // taken and freed before the item, of all; malformed items
   for (int i = tid; i < a.s.num_items; i += 256) {
     const ItemCount c = a.counts[i];
     s[2] += c.taken;
@@ -530,17 +570,22 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamTableArgs a) {
   }
 #pragma unroll
   for (int k = 0; k < 5; ++k) {
-#pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) s[k] += __shfl_xor(s[k], x);
-    if (lane == 0) sums[wave][k] = s[k];
+    s[k] = wave_inclusive_sum(s[k]);
+    if (lane == 63) sums[wave][k] = s[k];
   }
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < 5; ++k) s[k] = sums[0][k] + sums[1][k] + sums[2][k] + sums[3][k];
-  const int first = a.free_next[0];
   const bool in = first >= 0 && first <= a.s.num_free;
-  const bool fits = in && s[2] <= a.s.num_free - first && first + s[2] - s[3] >= 0;
+  const bool fits = in && s[2] <= a.s.num_free - first && first + s[2] >= s[3];
   const int64_t rest = fits ? first + s[2] : first;   // from here on the free list stays
+  if (any && wave == 0) {
+    m.take(a, p, n, !fits, lane);
+    const bool copy = lane < W && m.copied[lane];
+    const uint64_t mask = __ballot(copy);
+    const int before = lanes_before(mask);
+    if (lane < W) fresh[lane] = copy ? a.free_pages[first + s[0] + before] : -1;
+  }
   if (blockIdx.x == 0 && tid == 0) {
     a.out.free_next[0] = (int)(fits ? rest - s[3] : first);
     if ((s[4] || !fits) && a.error_flag) a.error_flag[0] = 1;
@@ -548,32 +593,41 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamTableArgs a) {
   if (in)
     for (int64_t j = rest + (int64_t)blockIdx.x * 256 + tid; j < a.s.num_free; j += (int64_t)gridDim.x * 256)
       a.out.free_pages[j] = a.free_pages[j];
-  if (item >= a.s.num_items) return;
-  m.load(a, item, !fits);
+  if (!any) return;
+  __syncthreads();
   if (fits) {
     const int32_t* list = a.freed + (int64_t)item * W * a.s.table_width;
-    const int n = a.counts[item].freed;
-    for (int64_t j = (int64_t)split * 256 + tid; j < n; j += (int64_t)a.splits * 256)
+    const int freed = a.counts[item].freed;
+    for (int64_t j = (int64_t)split * 256 + tid; j < freed; j += (int64_t)a.splits * 256)
       a.out.free_pages[rest - s[3] + s[1] + j] = list[j];
   }
-  int64_t next = first + s[0];   // the page that the item's next copy takes
-  for (int k = 0; k < W; ++k) {
-    const int p = m.parent[k];
-    const int64_t row = (int64_t)item * W + k;
-    const int pages = p < 0 ? 0 : m.pages[p];
-    const bool copied = m.copied[k] && fits;
-    const int32_t* from = a.block_table + ((int64_t)item * W + max(p, 0)) * a.s.table_width;
-    int32_t* to = a.out.block_table + row * a.s.table_width;
-    const int32_t fresh = copied ? a.free_pages[next] : -1;
-    for (int64_t c = (int64_t)split * 256 + tid; c < pages; c += (int64_t)a.splits * 256)
-      to[c] = copied && c == pages - 1 ? fresh : from[c];
-    if (split == 0 && tid == 0) {
-      a.out.seq_len[row] = p < 0 ? 0 : m.len[p];
-      a.out.copy_src[row] = copied ? from[pages - 1] : -1;
-      a.out.copy_dst[row] = fresh;
-    }
-    next += copied;
+  const int32_t* table = a.block_table + (int64_t)item * W * a.s.table_width;
+  int32_t* out = a.out.block_table + (int64_t)item * W * a.s.table_width;
+  if (split == 0 && tid < W) {
+    const int p = m.parent[tid];
+    const int64_t row = (int64_t)item * W + tid;
+    const bool copy = m.copied[tid] && m.pages[p] > 0;
+    a.out.seq_len[row] = p < 0 ? 0 : m.len[p];
+    a.out.copy_src[row] = copy ? table[(int64_t)p * a.s.table_width + m.pages[p] - 1] : -1;
+    a.out.copy_dst[row] = fresh[tid];
   }
+  int most = 0;
+  for (int k = 0; k < W; ++k) most = max(most, m.parent[k] < 0 ? 0 : m.pages[m.parent[k]]);
+  for (int64_t c = (int64_t)split * 256 + tid; c < most; c += (int64_t)a.splits * 256)
+    for (int k0 = 0; k0 < W; k0 += kHeld) {
+      int32_t page[kHeld];
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        const int p = k0 + j < W ? m.parent[k0 + j] : -1;
+        page[j] = p >= 0 && c < m.pages[p] ? table[(int64_t)p * a.s.table_width + c] : 0;
+      }
+#pragma unroll
+      for (int j = 0; j < kHeld; ++j) {
+        const int k = k0 + j, p = k < W ? m.parent[k] : -1;
+        if (p >= 0 && c < m.pages[p])
+          out[(int64_t)k * a.s.table_width + c] = m.copied[k] && c == m.pages[p] - 1 ? fresh[k] : page[j];
+      }
+    }
 }
 
 // ---------------------------------------------------------------- host side
