@@ -543,7 +543,7 @@ halo_status_t halo_rope_qk(const halo_rope_params_t* rope, float amplitude, cons
 typedef struct {
   int32_t num_seqs;
   int32_t num_rows;      /* tokens of q and lse */
-  int32_t num_entries;   /* elements of rows and row_end */
+  int32_t num_entries;   /* elements of rows and row_end; times num_q_heads / num_kv_heads < 2^31 - 1024 */
   int32_t width;         /* tokens of a row of the weights */
 } halo_weight_sizes_t;
 
@@ -620,8 +620,9 @@ halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, const float*
  * of the page list src, j < new_len[i]; any other sequence is copied whole (in
  * place: left alone). kept is [num_seqs][num_kv_heads][kept_width], ascending in a
  * row, bits are copied unchanged. dst_page_ids == page_ids with dst_page_indptr ==
- * seq_page_indptr moves in place; otherwise no page of dst may be a page of src or
- * listed twice (beams that share pages are evicted to pages of their own). A page
+ * seq_page_indptr moves in place, and no page may then be listed twice; otherwise no
+ * page of dst may be a page of src or listed twice (beams that share pages are
+ * evicted to pages of their own). A page
  * list holds at least the pages of its tokens; slots past new_len[i] keep what
  * they hold. All pointers but params are DEVICE pointers, pools 16-byte aligned.
  * A sequence whose lengths do not fit its pages or each other (new_len[i] > kept_width where

@@ -711,7 +711,7 @@ halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_
   if (!row_indptr && (rows || row_end) && sizes->num_entries < sizes->num_seqs)
     return fail(HALO_ERR_INVALID_ARGUMENT, "without row_indptr, rows and row_end have an element for each sequence");
   if (!aligned16(k_pool) || !aligned16(q)) return fail(HALO_ERR_INVALID_ARGUMENT, "k_pool and q must be 16-byte aligned");
-  if ((int64_t)sizes->num_entries * (params->num_q_heads / H) > INT32_MAX - 1024)
+  if ((int64_t)sizes->num_entries * (params->num_q_heads / H) >= INT32_MAX - 1023)
     return fail(HALO_ERR_UNSUPPORTED, "num_entries * num_q_heads / num_kv_heads must be less than 2^31 - 1024");
   const int64_t n = sizes->num_seqs, cells = n * H * sizes->width * 4, elt = params->kv_dtype == HALO_BF16 ? 2 : 4;
   const int64_t rows_h = (int64_t)sizes->num_rows * params->num_q_heads, entries = 4 * (int64_t)sizes->num_entries;

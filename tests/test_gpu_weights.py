@@ -158,6 +158,42 @@ def test_decode_step(gpu_lib, dtype, kvq):
     case.check(_call(case, row_indptr=None, rows=None, row_end=None, seq_start=None), start=10 ** 6)
 
 
+@pytest.mark.parametrize("dtype,kvq", FORMATS)
+@pytest.mark.parametrize("heads", [(1, 1), (32, 2), (34, 2), (64, 1)])
+def test_decode_step_with_rows_and_ends(gpu_lib, heads, dtype, kvq):
+    """An entry for each sequence, with its row and end from lists; q heads of a kv head that fill a tile, and more."""
+    rng = np.random.default_rng(23)
+    lengths = [0, 1, 16, *rng.integers(0, 200, 20), 1000]
+    case = Case(lengths, [1] * len(lengths), heads, 64, dtype, kvq, seed=23)
+    case.check(_call(case, row_indptr=None))
+    ends = np.array([len(k) for k in case.keys])
+    case.check(_call(case, row_indptr=None, row_end=None), row_end=ends)
+
+
+@pytest.mark.parametrize("dtype,kvq,dim", [(BF16, False, 128), (F32, False, 64), (F32, False, 128), (BF16, True, 128)])
+def test_decode_step_of_many_pages(gpu_lib, dtype, kvq, dim):
+    """More pages than waves, several sequences to a run of them; keys of more than 64 MiB (those of 2 bytes and 4)."""
+    rng = np.random.default_rng(24)
+    lengths = [*rng.integers(1, 40, 60), *rng.integers(500, 1500, 34)]
+    rng.shuffle(lengths)
+    case = Case(lengths, [1] * len(lengths), (8, 8), dim, dtype, kvq, seed=24)
+    assert sum(len(x) for x in case.lists) * 8 > 4 * 4096
+    case.check(_call(case, row_indptr=None))
+
+
+@pytest.mark.parametrize("kvq", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_more_rows_than_are_held(gpu_lib, dim, kvq):
+    """Rows in many batches, some of them one row longer; rows that see none, some or all of the keys in turn."""
+    case = Case([300, 40, 700], [1100, 129, 343], (3, 1), dim, BF16, kvq, seed=25)
+    case.check(_call(case))
+    case = Case([513, 64], [1025, 128], (2, 2), dim, BF16, kvq, seed=26, causal=False)
+    case.row_end[::3] = 0
+    case.row_end[200:500] = 100
+    # (lse over all of the keys: a row that sees fewer of them has smaller weights)
+    case.check(_call(case))
+
+
 def test_lists_that_are_left_out(gpu_lib):
     case = Case([50, 20, 90], [3, 0, 20], seed=6, causal=False)
     case.check(_call(case, row_end=None))

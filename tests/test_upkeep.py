@@ -142,6 +142,7 @@ def test_weights_refusals(lib, kvq):
         assert call(sizes=sizes) == BAD
     for decay in (-0.5, math.nan, math.inf):
         assert call(decay=decay) == BAD
+    assert call(sizes=(2, 3, (2 ** 31 - 1024) // 2, 40)) == UNSUPPORTED  # (entries times q heads of a kv head)
     assert call(sizes=(2, 3, 1, 40), none=("row_indptr",)) == BAD        # an entry for each sequence
     assert call(k_pool=8) == BAD and call(q=2) == BAD
     for written in ("out", "flag"):
