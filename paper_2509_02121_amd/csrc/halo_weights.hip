@@ -398,45 +398,53 @@ __global__ __launch_bounds__(256, step_waves<T>()) void weights_step_kernel(Weig
 // Fragments of 32 keys for 32x32x16 products: lane (c, hh) holds dims 16 s + 8 hh .. + 7 of
 // key c % 16 of page c / 16 (`tile`: that page's).
 template <bool KVQ, int D>
-__device__ __forceinline__ void load_keys32(const uint8_t* tile, int key, int hh, bf16x8_t (&k)[D / 16]) {
-  if constexpr (KVQ) {
-    // dims 16 s + 8 hh are in group 2 (s & 1) + hh
-    uint32_t codes[2][D / 32], scales;
-    const uint8_t* sc = tile + D * 8 + key * (D / 32);
+struct Keys32 {
+  u32x4_t x[D / 16];
+  __device__ __forceinline__ void load(const uint8_t* tile, int key, int hh) {
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const uint8_t* at = tile + ((2 * z + hh) * 16 + key) * (D / 8);
-      if constexpr (D == 128) {
-        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(at);
+    for (int s = 0; s < D / 16; ++s) x[s] = *reinterpret_cast<const u32x4_t*>(tile + ((2 * s + hh) * 16 + key) * 16);
+  }
+  __device__ __forceinline__ void fragments(bf16x8_t (&k)[D / 16]) const {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) codes[z][s] = x[s];
-      } else {
-        const u32x2_t x = *reinterpret_cast<const u32x2_t*>(at);
-        codes[z][0] = x[0];
-        codes[z][1] = x[1];
-      }
-    }
-    if constexpr (D == 128) scales = *reinterpret_cast<const uint32_t*>(sc);
-    else scales = *reinterpret_cast<const uint16_t*>(sc);
+    for (int s = 0; s < D / 16; ++s) k[s] = __builtin_bit_cast(bf16x8_t, x[s]);
+  }
+};
+template <int D>
+struct Keys32<true, D> {
+  // dims 16 s + 8 hh are in group 2 (s & 1) + hh
+  using Codes = typename std::conditional<D == 128, u32x4_t, u32x2_t>::type;
+  using Scales = typename std::conditional<D == 128, uint32_t, uint16_t>::type;
+  Codes codes[2];
+  Scales scales;
+  __device__ __forceinline__ void load(const uint8_t* tile, int key, int hh) {
+#pragma unroll
+    for (int z = 0; z < 2; ++z) codes[z] = *reinterpret_cast<const Codes*>(tile + ((2 * z + hh) * 16 + key) * (D / 8));
+    scales = *reinterpret_cast<const Scales*>(tile + D * 8 + key * (D / 32));
+  }
+  __device__ __forceinline__ void fragments(bf16x8_t (&k)[D / 16]) const {
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) k[s] = kvq_decode_bf16(codes[s & 1][s >> 1], kvq_scale_byte(scales, s >> 1));
-  } else {
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s)
-      k[s] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(tile + ((2 * s + hh) * 16 + key) * 16));
   }
-}
+};
 
-// A workgroup takes jobs of 16 slots of one head (which may span sequences), a wave four of the pages, 64 keys, as
-// fragments in registers. Rows are the A operand of 32x32x16 MFMAs, 32 of them a tile, so a lane
+// A workgroup takes jobs of one head, groups of 16 slots (which may span sequences), a wave four of a group's pages, 64
+// keys, as fragments in registers. Rows are the A operand of 32x32x16 MFMAs, 32 of them a tile, so a lane
 // has 16 rows of a key. Bound by the VALU: a product's 64 results take a multiply-add, an
 // exponential (four times as long) and an addition.
-// Rows go to LDS in batches of four tiles, by direct loads, a batch while the one before is worked on. What these need to
-// know of their rows, and the rows' lse and limits, lies in LDS too: a batch's lists are loaded three batches
-// ahead, and what they point to one batch later.
+// Rows go to LDS by direct loads, in batches of four tiles, with their lse and limits. What a batch's loads need
+// to know are two lists, one of which is read from the other.
+// HELD: a sequence's rows are passed by its pages 256 at a time, and stay where they are for all of a job's
+// groups, so the waves work without a barrier; the next group's keys are on their way while the last
+// tile's exponentials are taken. A job is as long as fills the chip once: 32 sequences of 1000-8000 tokens with
+// 32 tokens' queries (32 + 8 heads), 4 bits, 95.5 -> 61 us; that is 4500 groups of 4 tiles a wave, whose lists and rows
+// had taken twice as long to arrive as the products take.
+// Otherwise, for more rows, a job is one group, and a batch is loaded while the one before is worked on: its lists are loaded
+// three batches ahead, and what they point to one batch later (8 sequences of 4608 tokens, 512 tokens each:
+// 183 us, 0.8 PFLOP/s).
 // 16-byte unit u of row r of a tile lies at place u ^ r (mod the units of a row; at d 64 r / 2), so that
 // the 32 rows' units of one fragment are in different banks.
-template <bool KVQ, int D>
+constexpr int kHeldRows = 256;
+template <bool KVQ, int D, bool HELD>
 __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
   constexpr int NS = D / 16, U = D / 8, RB = 2 * D, kSlots = 16, NI = D / 64, kRowsPer = 64 / U;
   constexpr int64_t kTile = KVQ ? kvq_k_tile<D>() : 32 * D;
@@ -451,21 +459,49 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
   const int H = a.num_kv_heads, G = a.group;
   const int first = a.seq_page_indptr[0];
   const int64_t slots = (int64_t)a.seq_page_indptr[a.num_seqs] - first;
-  const int64_t jobs = (slots + kSlots - 1) / kSlots * H;
+  int64_t run = kSlots;
+  if constexpr (HELD) run *= max((int64_t)1, ((slots + kSlots - 1) / kSlots * H + gridDim.x - 1) / gridDim.x);
+  const int64_t jobs = (slots + run - 1) / run * H;
   const int64_t row_bytes = (int64_t)H * G * RB;
   for (int64_t job = blockIdx.x; job < jobs; job += gridDim.x) {
     const int h = (int)(job % H);
-    const int64_t chunk = job / H * kSlots, chunk_end = min(slots, chunk + kSlots), mine = chunk + 4 * wave;
-    bf16x8_t k[2][NS];
-    bool ok[2];   // this lane's pages
+    const int64_t chunk = job / H * run, chunk_end = min(slots, chunk + run);
+    int64_t mine = chunk + 4 * wave;   // the wave's first slot
+    Keys32<KVQ, D> keys[2];
+    int pid[2];   // this lane's pages
+    bool ok[2];
+    auto load_ids = [&](int64_t from) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int64_t at = mine + 2 * b + (c >> 4);
-      const int pid = at < chunk_end ? a.page_ids[first + at] : -1;
-      ok[b] = pid >= 0 && pid < a.num_pool_pages;
-      // (a page that is none is read as page 0 and not written)
-      if (a.num_pool_pages > 0)
-        load_keys32<KVQ, D>(static_cast<const uint8_t*>(a.k_pool) + ((int64_t)(ok[b] ? pid : 0) * H + h) * kTile, c & 15, hh, k[b]);
+      for (int b = 0; b < 2; ++b) {
+        const int64_t at = from + 2 * b + (c >> 4);
+        pid[b] = at < chunk_end ? a.page_ids[first + at] : -1;
+      }
+    };
+    auto in_pool = [&](int id) { return id >= 0 && id < a.num_pool_pages; };
+    auto load_page = [&](int b) {   // (a page that is none is read as page 0 and not written)
+      keys[b].load(static_cast<const uint8_t*>(a.k_pool) + ((int64_t)(in_pool(pid[b]) ? pid[b] : 0) * H + h) * kTile, c & 15, hh);
+    };
+    auto load_keys = [&] {
+      load_page(0);
+      load_page(1);
+    };
+    bf16x8_t k[2][NS];
+    auto take_keys = [&] {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        ok[b] = in_pool(pid[b]);
+        keys[b].fragments(k[b]);
+      }
+    };
+    if constexpr (!HELD) {
+      load_ids(mine);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        ok[b] = in_pool(pid[b]);
+        if (a.num_pool_pages == 0) continue;
+        load_page(b);
+        keys[b].fragments(k[b]);
+      }
     }
     int seq = last_at_or_below(a.seq_page_indptr, a.num_seqs, first + chunk, lane);
     int64_t slot = chunk;
@@ -477,213 +513,257 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
       if ((s.bad || s.bad_rows || a.num_pool_pages == 0) && tid == 0 && a.error_flag) a.error_flag[0] = 1;
       const int64_t place = first - (int64_t)s.base;   // of slot 0 in the sequence's list
       if (s.bad || a.num_pool_pages == 0 || (place + from) * 16 >= s.end) continue;
-      // this wave's keys in the sequence
-      const int64_t k0 = max(from, mine), k1 = min(upto, mine + 4);
-      const int key_lo = k0 < k1 ? (int)min((place + k0) * 16, (int64_t)s.end) : s.end;
-      const int key_hi = k0 < k1 ? (int)min((place + k1) * 16, (int64_t)s.end) : s.end;
-      const bool whole = k1 - k0 == 4;
-      int t[2];   // this lane's tokens; past every row's end: none
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int64_t at = mine + 2 * b + (c >> 4);
-        const bool in = at >= k0 && at < k1;
-        t[b] = in ? (int)min((place + at) * 16 + (c & 15), (int64_t)INT32_MAX) : INT32_MAX;
-        if (in && !ok[b] && (place + at) * 16 < s.end && a.error_flag) a.error_flag[0] = 1;
-      }
-      float sum[2] = {0.f, 0.f};
       const int64_t rows = (int64_t)(s.e1 - s.e0) * G;   // (below INT32_MAX - 1024)
-      if (rows > 0) {
-        // A batch's rows, one to each of 128 threads (the other half does the same, and at the start the second
-        // batch): the entry, then its row of q, then that row's lse and limit. Rows behind the last one see nothing.
-        int e = 0, g = 0, row = 0, sees = 0;
-        bool fine = false;
-        float l = 0.f;
-        auto find = [&](int64_t first_row) {
-          const int r = (int)min(first_row, rows);
-          e = (int)((uint32_t)r / (uint32_t)G);
-          g = r - e * G;
-          e += s.e0;
-          const int in = min(e, s.e1 - 1);   // (there is one)
-          row = a.rows ? a.rows[in] : in;
-          if (r >= rows) e = -1;
-        };
-        auto place_row = [&](int at, int r) {
-          fine = row >= 0 && row < a.num_rows;
-          if (!fine && e >= 0 && a.error_flag) a.error_flag[0] = 1;
-          if (!fine) row = 0;
-          row_lds[at][r] = row * row_bytes + (int64_t)(h * G + g) * RB;
-        };
-        auto look = [&] {
-          l = a.num_rows > 0 ? a.lse[(int64_t)row * H * G + (int64_t)h * G + g] : kNegInf;
-          sees = a.row_end ? a.row_end[max(e, s.e0)] : s.end;
-          if (!fine || e < 0) sees = 0;
-        };
-        auto keep = [&](int at, int r) {
-          const bool none = l == kNegInf;   // (it saw no key)
-          l_lds[at][r] = none ? 0.f : -l * kLog2e;
-          sees_lds[at][r] = none ? 0 : min(sees, s.end);
-        };
-        const int64_t tiles = (rows + 31) / 32;
-        auto issue = [&](int64_t batch, uint8_t* q) {
-          if (a.num_rows == 0) return;
+      const int64_t keys_end = min(upto, ((int64_t)s.end + 15) / 16 - place);
+      int64_t row0 = 0, group = from;
+      if constexpr (HELD) {
+        load_ids(from + 4 * wave);
+        load_keys();
+      }
+      do {
+        if constexpr (HELD) {
+          take_keys();
+          mine = group + 4 * wave;
+          load_ids((group + kSlots < keys_end ? group + kSlots : from) + 4 * wave);   // (behind the last one: the next rows')
+        }
+        // this wave's keys in the sequence
+        const int64_t k0 = max(from, mine), k1 = min(upto, mine + 4);
+        const int key_lo = k0 < k1 ? (int)min((place + k0) * 16, (int64_t)s.end) : s.end;
+        const int key_hi = k0 < k1 ? (int)min((place + k1) * 16, (int64_t)s.end) : s.end;
+        const bool whole = k1 - k0 == 4;
+        int t[2];   // this lane's tokens; past every row's end: none
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (batch * 4 + i >= tiles) break;
+        for (int b = 0; b < 2; ++b) {
+          const int64_t at = mine + 2 * b + (c >> 4);
+          const bool in = at >= k0 && at < k1;
+          t[b] = in ? (int)min((place + at) * 16 + (c & 15), (int64_t)INT32_MAX) : INT32_MAX;
+          if (in && !ok[b] && (place + at) * 16 < s.end && a.error_flag) a.error_flag[0] = 1;
+        }
+        float sum[2] = {0.f, 0.f}, old[2] = {0.f, 0.f};
+        const int64_t to = ((int64_t)seq * H + h) * a.width;
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-              const int r = wave * 8 + j * kRowsPer + lane / U;
-              const int unit = (lane % U) ^ (D == 128 ? r & 15 : (r >> 1) & 7);
-              __builtin_amdgcn_global_load_lds(static_cast<const uint8_t*>(a.q) + row_lds[batch & 3][32 * i + r] + unit * 16,
-                                               q + (32 * i + wave * 8 + j * kRowsPer) * RB, 16, 0, 0);
+        for (int z = 0; z < 2; ++z)
+          if (HELD && hh == 0 && ok[z] && t[z] < min(s.start, s.end) && a.decay != 0.f && row0 == 0) old[z] = a.weights[to + t[z]];
+        if (rows > 0) {
+          // A batch's rows, one to each of 128 threads (the other half does the same, and at the start the second
+          // batch): the entry, then its row of q, then that row's lse and limit. Rows behind the last one see nothing.
+          int e = 0, g = 0, row = 0, sees = 0;
+          bool fine = false;
+          float l = 0.f;
+          auto find = [&](int64_t first_row) {
+            const int r = (int)min(first_row, rows);
+            e = (int)((uint32_t)r / (uint32_t)G);
+            g = r - e * G;
+            e += s.e0;
+            const int in = min(e, s.e1 - 1);   // (there is one)
+            row = a.rows ? a.rows[in] : in;
+            if (r >= rows) e = -1;
+          };
+          auto place_row = [&](int at, int r) {
+            fine = row >= 0 && row < a.num_rows;
+            if (!fine && e >= 0 && a.error_flag) a.error_flag[0] = 1;
+            if (!fine) row = 0;
+            row_lds[at][r] = row * row_bytes + (int64_t)(h * G + g) * RB;
+          };
+          auto look = [&] {
+            l = a.num_rows > 0 ? a.lse[(int64_t)row * H * G + (int64_t)h * G + g] : kNegInf;
+            sees = a.row_end ? a.row_end[max(e, s.e0)] : s.end;
+            if (!fine || e < 0) sees = 0;
+          };
+          auto keep = [&](int at, int r) {
+            const bool none = l == kNegInf;   // (it saw no key)
+            l_lds[at][r] = none ? 0.f : -l * kLog2e;
+            sees_lds[at][r] = none ? 0 : min(sees, s.end);
+          };
+          const int64_t tiles = ((HELD ? min(rows - row0, (int64_t)kHeldRows) : rows) + 31) / 32;
+          auto issue = [&](int64_t batch, uint8_t* q) {
+            if (a.num_rows == 0) return;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (batch * 4 + i >= tiles) break;
+#pragma unroll
+              for (int j = 0; j < NI; ++j) {
+                const int r = wave * 8 + j * kRowsPer + lane / U;
+                const int unit = (lane % U) ^ (D == 128 ? r & 15 : (r >> 1) & 7);
+                __builtin_amdgcn_global_load_lds(static_cast<const uint8_t*>(a.q) + row_lds[batch & 3][32 * i + r] + unit * 16,
+                                                 q + (32 * i + wave * 8 + j * kRowsPer) * RB, 16, 0, 0);
+              }
             }
-          }
-        };
-        // A tile's scores go to x while the exponentials of the one before are taken from y: the matrix
-        // products of one wave run beside its own VALU instructions. A tile that no key of the wave is
-        // seen by is left out; one whose rows see all of them needs no limits.
-        uint64_t sees_any[2], sees_part[2];   // of a batch's rows: those that see a key of the wave, and not all of them
-        auto look_at = [&](int64_t batch) {
+          };
+          // A tile's scores go to x while the exponentials of the one before are taken from y: the matrix
+          // products of one wave run beside its own VALU instructions. A tile that no key of the wave is
+          // seen by is left out; one whose rows see all of them needs no limits.
+          uint64_t sees_any[2], sees_part[2];   // of a batch's rows: those that see a key of the wave, and not all of them
+          auto look_at = [&](int64_t batch) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int limit = sees_lds[batch & 3][64 * j + lane];
-            sees_any[j] = __ballot(limit > key_lo);
-            sees_part[j] = __ballot(limit < key_hi);
-          }
-        };
-        auto read_q = [&](const uint8_t* q_lds, bf16x8_t (&q)[NS]) {
-#pragma unroll
-          for (int x = 0; x < NS; ++x)
-            q[x] = *reinterpret_cast<const bf16x8_t*>(q_lds + c * RB + ((2 * x + hh) ^ (D == 128 ? c & 15 : (c >> 1) & 7)) * 16);
-        };
-        auto read_l = [&](int64_t tile, float (&nl)[16]) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const f32x4_t l = *reinterpret_cast<const f32x4_t*>(&l_lds[(tile >> 2) & 3][(tile & 3) * 32 + 8 * j + 4 * hh]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) nl[4 * j + i] = l[i];
-          }
-        };
-        auto product = [&](int y, const bf16x8_t (&q)[NS], f32x16_t (&x)[2]) {
-#pragma unroll
-          for (int z = 0; z < 2; ++z) x[z] = mma32(q[y], k[z][y], y == 0 ? f32x16_t{} : x[z]);
-        };
-        auto exponentials = [&](int i, const f32x16_t (&y)[2], const float (&nl)[16]) {
-#pragma unroll
-          for (int z = 0; z < 2; ++z) sum[z] += __builtin_amdgcn_exp2f(__builtin_fmaf(y[z][i], a.scale_log2, nl[i]));
-        };
-        auto masked = [&](int64_t tile, const f32x16_t (&y)[2]) {
-          float nl[16];
-          read_l(tile, nl);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int end = sees_lds[(tile >> 2) & 3][(tile & 3) * 32 + 8 * (i >> 2) + 4 * hh + (i & 3)];
-#pragma unroll
-            for (int z = 0; z < 2; ++z) {
-              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(y[z][i], a.scale_log2, nl[i]));
-              sum[z] += t[z] < end ? w : 0.f;
+            for (int j = 0; j < 2; ++j) {
+              const int limit = sees_lds[batch & 3][64 * j + lane];
+              sees_any[j] = __ballot(limit > key_lo);
+              sees_part[j] = __ballot(limit < key_hi);
             }
-          }
-        };
-        bool held_any = false, held_full = false;   // of the tile whose scores are held
-        // tile 4 batch + i's scores to x, the exponentials of the one before, whose scores are in y
-        auto step = [&](int64_t batch, int i, const uint8_t* q_lds, f32x16_t (&x)[2], const f32x16_t (&y)[2]) {
-          const bool more = i < 4;
-          const bool any = more && (uint32_t)(sees_any[(i & 2) / 2] >> (32 * (i & 1))) != 0;
-          const bool full = any && whole && (uint32_t)(sees_part[(i & 2) / 2] >> (32 * (i & 1))) == 0;
-          const int64_t tile = batch * 4 + i;
-          if (any && held_full) {
-            bf16x8_t q[NS];
+          };
+          auto read_q = [&](const uint8_t* q_lds, bf16x8_t (&q)[NS]) {
+#pragma unroll
+            for (int x = 0; x < NS; ++x)
+              q[x] = *reinterpret_cast<const bf16x8_t*>(q_lds + c * RB + ((2 * x + hh) ^ (D == 128 ? c & 15 : (c >> 1) & 7)) * 16);
+          };
+          auto read_l = [&](int64_t tile, float (&nl)[16]) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const f32x4_t l = *reinterpret_cast<const f32x4_t*>(&l_lds[(tile >> 2) & 3][(tile & 3) * 32 + 8 * j + 4 * hh]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) nl[4 * j + i] = l[i];
+            }
+          };
+          auto product = [&](int y, const bf16x8_t (&q)[NS], f32x16_t (&x)[2]) {
+#pragma unroll
+            for (int z = 0; z < 2; ++z) x[z] = mma32(q[y], k[z][y], y == 0 ? f32x16_t{} : x[z]);
+          };
+          auto exponentials = [&](int i, const f32x16_t (&y)[2], const float (&nl)[16]) {
+#pragma unroll
+            for (int z = 0; z < 2; ++z) sum[z] += __builtin_amdgcn_exp2f(__builtin_fmaf(y[z][i], a.scale_log2, nl[i]));
+          };
+          auto masked = [&](int64_t tile, const f32x16_t (&y)[2]) {
             float nl[16];
-            read_l(tile - 1, nl);
-            read_q(q_lds, q);
-            // (in this order: the two chains of products in turn, each with its share of the rest)
+            read_l(tile, nl);
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-              product(s, q, x);
+            for (int i = 0; i < 16; ++i) {
+              const int end = sees_lds[(tile >> 2) & 3][(tile & 3) * 32 + 8 * (i >> 2) + 4 * hh + (i & 3)];
 #pragma unroll
-              for (int j = 0; j < 16 / NS; ++j) exponentials(16 / NS * s + j, y, nl);
-              __builtin_amdgcn_sched_barrier(0);
+              for (int z = 0; z < 2; ++z) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(y[z][i], a.scale_log2, nl[i]));
+                sum[z] += t[z] < end ? w : 0.f;
+              }
             }
-          } else {
-            if (any) {
+          };
+          bool held_any = false, held_full = false;   // of the tile whose scores are held
+          // tile 4 batch + i's scores to x, the exponentials of the one before, whose scores are in y
+          auto step = [&](int64_t batch, int i, const uint8_t* q_lds, f32x16_t (&x)[2], const f32x16_t (&y)[2]) {
+            const bool more = i < 4;
+            const bool any = more && (uint32_t)(sees_any[(i & 2) / 2] >> (32 * (i & 1))) != 0;
+            const bool full = any && whole && (uint32_t)(sees_part[(i & 2) / 2] >> (32 * (i & 1))) == 0;
+            const int64_t tile = batch * 4 + i;
+            if (any && held_full) {
               bf16x8_t q[NS];
+              float nl[16];
+              read_l(tile - 1, nl);
               read_q(q_lds, q);
+              // (in this order: the two chains of products in turn, each with its share of the rest)
 #pragma unroll
               for (int s = 0; s < NS; ++s) {
                 product(s, q, x);
+#pragma unroll
+                for (int j = 0; j < 16 / NS; ++j) exponentials(16 / NS * s + j, y, nl);
                 __builtin_amdgcn_sched_barrier(0);
               }
-            }
-            if (held_full) {
-              float nl[16];
-              read_l(tile - 1, nl);
+            } else {
+              if (any) {
+                bf16x8_t q[NS];
+                read_q(q_lds, q);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) exponentials(j, y, nl);
-            } else if (held_any) {
-              masked(tile - 1, y);
+                for (int s = 0; s < NS; ++s) {
+                  product(s, q, x);
+                  __builtin_amdgcn_sched_barrier(0);
+                }
+              }
+              if (held_full) {
+                float nl[16];
+                read_l(tile - 1, nl);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) exponentials(j, y, nl);
+              } else if (held_any) {
+                masked(tile - 1, y);
+              }
             }
-          }
-          held_any = any;
-          held_full = full;
-        };
-        f32x16_t x[2], y[2];
-        // one batch: the next one's loads begin, and those of what the ones behind it need
-        auto work = [&](int64_t batch, const uint8_t* q, uint8_t* next) {
-          look_at(batch);
-          const bool behind = (batch + 2) * 4 < tiles;
-          if (behind) {
-            place_row((int)(batch + 2) & 3, tid & 127);
+            held_any = any;
+            held_full = full;
+          };
+          f32x16_t x[2], y[2];
+          // one batch: the next one's loads begin, and those of what the ones behind it need
+          auto work = [&](int64_t batch, const uint8_t* q, uint8_t* next) {
+            look_at(batch);
+            const bool behind = (batch + 2) * 4 < tiles;
+            if (behind) {
+              place_row((int)(batch + 2) & 3, tid & 127);
+              look();
+            }
+            issue(batch + 1, next);
+            step(batch, 0, q, x, y);
+            step(batch, 1, q + 32 * RB, y, x);
+            if (behind) {
+              keep((int)(batch + 2) & 3, tid & 127);
+              find((batch + 3) * 128 + (tid & 127));
+            }
+            step(batch, 2, q + 64 * RB, x, y);
+            step(batch, 3, q + 96 * RB, y, x);
+            wait_vmcnt<0>();
+            __syncthreads();
+          };
+          if (!HELD || group == from) {
+            find(row0 + tid);
+            place_row(tid >> 7, tid & 127);
+            __syncthreads();
+            issue(0, q0);
+            if constexpr (HELD) issue(1, q1);
             look();
+            keep(tid >> 7, tid & 127);
+            if (!HELD && tiles > 8) find(256 + (tid & 127));
+            wait_vmcnt<0>();
+            __syncthreads();
           }
-          issue(batch + 1, next);
-          step(batch, 0, q, x, y);
-          step(batch, 1, q + 32 * RB, y, x);
-          if (behind) {
-            keep((int)(batch + 2) & 3, tid & 127);
-            find((batch + 3) * 128 + (tid & 127));
+          if constexpr (HELD) {
+            for (int64_t batch = 0; batch * 4 < tiles; ++batch) {
+              const uint8_t* q = batch ? q1 : q0;
+              look_at(batch);
+              step(batch, 0, q, x, y);
+              step(batch, 1, q + 32 * RB, y, x);
+              step(batch, 2, q + 64 * RB, x, y);
+              step(batch, 3, q + 96 * RB, y, x);
+            }
+          } else {
+            for (int64_t batch = 0; batch * 4 < tiles; batch += 2) {
+              work(batch, q0, q1);
+              if ((batch + 1) * 4 < tiles) work(batch + 1, q1, q0);
+            }
           }
-          step(batch, 2, q + 64 * RB, x, y);
-          step(batch, 3, q + 96 * RB, y, x);
-          wait_vmcnt<0>();
-          __syncthreads();
-        };
-        find(tid);
-        place_row(tid >> 7, tid & 127);
-        __syncthreads();
-        issue(0, q0);
-        look();
-        keep(tid >> 7, tid & 127);
-        if (tiles > 8) find(256 + (tid & 127));
-        wait_vmcnt<0>();
-        __syncthreads();
-        for (int64_t batch = 0; batch * 4 < tiles; batch += 2) {
-          work(batch, q0, q1);
-          if ((batch + 1) * 4 < tiles) work(batch + 1, q1, q0);
+          if constexpr (HELD) load_keys();   // (the next group's: nothing needs this one's any more)
+          step((tiles - 1) / 4, 4, q0, x, y);   // (whole batches, so that the last scores are in y)
+          // (the next first batches go where the last rows and limits may still be read)
+          if (!HELD || group + kSlots >= keys_end) __syncthreads();
         }
-        step((tiles - 1) / 4, 4, q0, x, y);   // (whole batches, so that the last scores are in y)
-        __syncthreads();   // (the next sequence's first batches go where the last tile's limits may still be read)
-      }
+        if constexpr (!HELD) {
 #pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const float w = halves_sum(sum[z]);
-        if (hh == 0 && ok[z] && t[z] < s.end) {
-          const int64_t at = ((int64_t)seq * H + h) * a.width + t[z];
-          const bool old = t[z] < s.start && a.decay != 0.f;
-          a.weights_out[at] = old ? __builtin_fmaf(a.decay, a.weights[at], w) : w;
+          for (int z = 0; z < 2; ++z)
+            if (hh == 0 && ok[z] && t[z] < min(s.start, s.end) && a.decay != 0.f) old[z] = a.weights[to + t[z]];
         }
-      }
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          const float w = halves_sum(sum[z]);
+          if (hh == 0 && ok[z] && t[z] < s.end) {
+            if (row0 > 0) a.weights_out[to + t[z]] += w;
+            else a.weights_out[to + t[z]] = __builtin_fmaf(a.decay, old[z], w);   // (without an old weight: decay * 0)
+          }
+        }
+        group += kSlots;
+        if (HELD && group >= keys_end) {
+          group = from;
+          row0 += kHeldRows;
+        }
+      } while (HELD && (group > from || row0 < rows));
     }
   }
 }
 
 // (the body in a function of its own: the host's pass does not know the direct loads)
-template <bool KVQ, int D>
-__global__ __launch_bounds__(256, 2) void weights_wide_kernel(WeightArgs a) { weights_wide<KVQ, D>(a); }
+template <bool KVQ, int D, bool HELD>
+__global__ __launch_bounds__(256, 2) void weights_wide_kernel(WeightArgs a) { weights_wide<KVQ, D, HELD>(a); }
 
-// Whether the wide kernel takes a call (of bf16 queries): where a sequence has 32 rows or more on
-// average.
-bool many_rows(const halo_weight_sizes_t& s, bool lists, int group) {
-  return (int64_t)(lists ? s.num_entries : s.num_seqs) * group >= 32 * (int64_t)s.num_seqs;
+// Whether a sequence has `rows` rows or more on average. The wide kernel takes bf16 queries from 17 on, where
+// the general one passes a second tile (window of 8 tokens, G 4, sequences of 1000-8000 tokens: 113 us general, 73 wide;
+// of 4 tokens: 93 and 83; 512 sequences of 50-200 tokens: 85 and 81, of 4 tokens 55 and 89). It holds them up to 512: 128
+// tokens, 224 us a batch at a time, 205 held; 256 tokens, 397 and 427.
+bool many_rows(const halo_weight_sizes_t& s, bool lists, int group, int rows) {
+  return (int64_t)(lists ? s.num_entries : s.num_seqs) * group >= rows * (int64_t)s.num_seqs;
 }
 
 halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_t* params,
@@ -728,7 +808,8 @@ halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_
                sizes->width, H, params->num_q_heads / H, params->sm_scale * kLog2e, decay};
   (void)hipGetLastError();
   const bool step = !row_indptr && g.group <= 16 && params->num_pool_pages > 0;
-  const bool wide = params->kv_dtype == HALO_BF16 && many_rows(*sizes, row_indptr != nullptr, g.group);
+  const bool wide = params->kv_dtype == HALO_BF16 && many_rows(*sizes, row_indptr != nullptr, g.group, 17);
+  const bool held = !many_rows(*sizes, row_indptr != nullptr, g.group, 2 * kHeldRows + 1);
   by_type_and_dim(params, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
@@ -736,8 +817,10 @@ halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (step && kvq) hipLaunchKernelGGL((weights_step_kernel<T, true, D>), dim3(kNumCUs * step_waves<T>()), block, 0, s, g);
     else if (step) hipLaunchKernelGGL((weights_step_kernel<T, false, D>), dim3(kNumCUs * step_waves<T>()), block, 0, s, g);
-    else if (wide && kvq) hipLaunchKernelGGL((weights_wide_kernel<true, D>), grid, block, 0, s, g);
-    else if (wide) hipLaunchKernelGGL((weights_wide_kernel<false, D>), grid, block, 0, s, g);
+    else if (wide && held && kvq) hipLaunchKernelGGL((weights_wide_kernel<true, D, true>), dim3(2 * kNumCUs), block, 0, s, g);
+    else if (wide && held) hipLaunchKernelGGL((weights_wide_kernel<false, D, true>), dim3(2 * kNumCUs), block, 0, s, g);
+    else if (wide && kvq) hipLaunchKernelGGL((weights_wide_kernel<true, D, false>), grid, block, 0, s, g);
+    else if (wide) hipLaunchKernelGGL((weights_wide_kernel<false, D, false>), grid, block, 0, s, g);
     else if (kvq) hipLaunchKernelGGL((weights_kernel<T, true, D>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((weights_kernel<T, false, D>), grid, block, 0, s, g);
   });

@@ -194,6 +194,21 @@ def test_more_rows_than_are_held(gpu_lib, dim, kvq):
     case.check(_call(case))
 
 
+@pytest.mark.parametrize("kvq", [False, True])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_window_of_rows(gpu_lib, dim, kvq):
+    """Some rows for many pages: several groups of pages with the same rows, sequences that begin and end inside of
+    them, and one with more rows than are held at once."""
+    rng = np.random.default_rng(27)
+    lengths = [*rng.integers(0, 3000, 12), 17000, 1, 256, 4096]
+    rows = [*rng.integers(0, 60, 12), 64, 3, 300, 128]
+    case = Case(lengths, rows, (4, 2), dim, BF16, kvq, seed=27)
+    case.check(_call(case))
+    once = case.old.clone()
+    _call(case, weights=once, weights_out=once)
+    case.check(torch.where(torch.arange(case.width, device="cuda") < cuda(lengths)[:, None, None], once, -7.0))
+
+
 def test_lists_that_are_left_out(gpu_lib):
     case = Case([50, 20, 90], [3, 0, 20], seed=6, causal=False)
     case.check(_call(case, row_end=None))
