@@ -82,9 +82,6 @@ __device__ __forceinline__ uint32_t wave_nth_key(const uint32_t (&key)[N], int n
   return t;
 }
 
-__device__ __forceinline__ int lanes_before(uint64_t mask) {
-  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-}
 // LDS that a wave alone writes and reads: what was written can be read by its other lanes.
 __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -94,8 +91,10 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 constexpr int kBoundBit = 14;    // of a bound on logits the bits from here on
 constexpr int kTile = 512;       // elements a wave looks at together
-constexpr int kListCap = 640;    // candidates a wave holds
-constexpr int kListFull = kListCap - kTile;
+// Candidates a wave holds. (Of rows in any order 64 best need about 800 places until the part ends, 16 best 230: 64 of
+// 16 x 16 rows of 128256 bf16 logits take 97 us with 640 places, 78 with 1024; 32 of them 44 and 50, as more registers and
+// LDS leave fewer waves; 64 of 8 x 64 rows of 32000 fp32 logits, parts of 8 tiles, 37 and 47.)
+constexpr int kListCap = 640, kLongListCap = 1024, kLongListFrom = 33, kLongPart = 16 * kTile;
 
 // Keeps the `best` first of the list's n candidates (by value, then token), N a lane.
 template <int N>
@@ -128,7 +127,7 @@ __device__ __forceinline__ int prune_of(float* value, int32_t* token, int n, int
     const bool keep = key[j] > least || (key[j] == least && id[j] >= last);
     const uint64_t mask = __ballot(keep);
     if (keep) {
-      const int to = at + lanes_before(mask);
+      const int to = lanes_before(mask, at);
       value[to] = from_order_key(key[j]);
       token[to] = (int32_t)~id[j];
     }
@@ -136,12 +135,13 @@ __device__ __forceinline__ int prune_of(float* value, int32_t* token, int n, int
   }
   return at;
 }
+template <int CAP>
 __device__ __forceinline__ int prune(float* value, int32_t* token, int n, int best, int lane) {
   wave_lds_fence();
   if (n > best) {
     if (n <= 64) n = prune_of<1>(value, token, n, best, lane);
     else if (n <= 128) n = prune_of<2>(value, token, n, best, lane);
-    else n = prune_of<kListCap / 64>(value, token, n, best, lane);
+    else n = prune_of<CAP / 64>(value, token, n, best, lane);
     wave_lds_fence();
   }
   return n;
@@ -173,10 +173,10 @@ struct Tile {
 // seen one; it is found anew after 1, 2, 4, 8, ... tiles, so that of a part in any order about
 // `best` more are listed each time the part seen doubles. A full list is cut to the
 // first `best`; then only what is above the last of these counts (ties with it are later tokens).
-template <typename T>
+template <typename T, int CAP>
 __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
-  __shared__ float list_value[4][kListCap];
-  __shared__ int32_t list_token[4][kListCap];
+  __shared__ float list_value[4][CAP];
+  __shared__ int32_t list_token[4][CAP];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int row = (int)blockIdx.y, part = (int)blockIdx.x * 4 + wave;
   if (part >= a.num_parts) return;
@@ -222,15 +222,15 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
         const uint64_t mask = __ballot(hit);
         if (mask) {
           if (hit) {
-            const int to = n + lanes_before(mask);
+            const int to = lanes_before(mask, n);
             value[to] = v[k];
             token[to] = (int32_t)t + Tile<T>::place(k, lane);
           }
           n += __popcll(mask);
         }
       }
-      if (n > kListFull) {
-        n = prune(value, token, n, a.best, lane);
+      if (n > CAP - kTile) {
+        n = prune<CAP>(value, token, n, a.best, lane);
         if (n >= a.best) {
           float least = -kMinusInf;
           for (int i = lane; i < n; i += 64) least = fminf(least, value[i]);
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
     now = next;
     next = then;
   }
-  n = prune(value, token, n, a.best, lane);
+  n = prune<CAP>(value, token, n, a.best, lane);
   Candidate* c = a.candidates + ((int64_t)row * a.num_parts + part) * a.best;
   for (int i = lane; i < a.best; i += 64) c[i] = i < n ? Candidate{value[i], token[i]} : Candidate{kMinusInf, -1};
   float most = top;
@@ -265,28 +265,36 @@ __device__ __forceinline__ double from_order_key(uint64_t k) {
   return __longlong_as_double((long long)(k & 0x8000000000000000ull ? k & 0x7fffffffffffffffull : ~k));
 }
 
-constexpr int kPickCap = 1024;   // candidates that are put in order together
+constexpr int kPickCap = 512;    // candidates that are put in order together
+// Candidates of an item that workgroups of 16 waves are taken from on (16 beams of 16 parts with 16 best, 4096: 24.5 us
+// by 4 waves, 12 by 16).
+constexpr int kManyCandidates = 2048;
+constexpr uint64_t kLastId = (1ull << 38) - 1;   // ids: beam, token
 
 struct Ranked {
   uint64_t key, id;   // larger keys first, then smaller ids
 };
 
-// A workgroup for each item. ln sum exp of every beam comes from its parts. Of the beams'
+// A workgroup of NW waves for each item. ln sum exp of every beam comes from its parts. Of the beams'
 // candidates those at or above a bound go to a list in LDS, and each one's place is how
 // many of the list come before it. The bound: of each wave's lane maxima the best-th largest
-// one (in the upper 32 bits), of the waves' the largest. A list that does
-// not hold them all (ties) is left, and `best` rounds find the first of the candidates
-// behind the last round's.
-__global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
+// one (in the upper 32 bits), of the waves' the largest. Where the list does not hold them all, the candidates
+// from the bound up are counted in 2048 equal parts of their range, then those of the part that holds the last one
+// of the best, and so on, of equal keys by their ids, until what is left fits.
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void beam_pick_kernel(BeamArgs a) {
+  constexpr int T = 64 * NW;
   __shared__ double lse[kMaxBeams];
   __shared__ int32_t live[kMaxBeams];   // 0 dead, 1 live, 2 ended
   __shared__ __align__(16) Ranked list[kPickCap];
-  __shared__ uint32_t bounds[4];
+  __shared__ int count[kBins];
+  __shared__ int sums[NW], found[2];
+  __shared__ uint32_t bounds[NW], tops[NW];
   __shared__ int32_t listed;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int item = (int)blockIdx.x, W = a.beams, P = a.num_parts;
   if (tid == 0) listed = 0;
-  for (int b = wave; b < W; b += 4) {
+  for (int b = wave; b < W; b += NW) {
     const int row = item * W + b;
     const BeamPart* parts = a.parts + (int64_t)row * P;
     const bool open = is_finite(a.scores[row]);
@@ -310,102 +318,114 @@ __global__ __launch_bounds__(256) void beam_pick_kernel(BeamArgs a) {
   }
   __syncthreads();
   const int per_row = P * a.best, all = W * per_row;
-  // candidate i's key (larger: better; 0: none) and, of equal keys, its order
+  // A candidate's key (larger: better; 0: none) and, of equal keys, its order.
   auto candidate = [&](int i, uint64_t& key, uint64_t& id) {
+    const bool in = i < all;
+    i = in ? i : 0;
     const int b = i / per_row, j = i - b * per_row;
-    const int row = item * W + b;
-    key = 0;
-    if (live[b] == 1) {
-      const Candidate x = a.candidates[(int64_t)row * per_row + j];
-      if (x.token < 0) return;
-      key = order_key(((double)x.value - lse[b]) + (double)a.scores[row]);
-      id = (uint64_t)b << 32 | (uint32_t)x.token;
-    } else if (live[b] == 2 && j == 0) {
-      key = order_key((double)a.scores[row]);
-      id = (uint64_t)b << 32 | (uint32_t)a.end_token;
-    }
+    const int row = item * W + b, how = live[b];
+    const Candidate x = a.candidates[(int64_t)row * per_row + j];   // (of a beam that is not live: anything)
+    const double score = (double)a.scores[row];
+    const bool of_live = in && how == 1 && x.token >= 0, of_ended = in && how == 2 && j == 0;
+    key = order_key(of_ended ? score : ((double)x.value - lse[b]) + score);
+    if (!of_live && !of_ended) key = 0;
+    id = (uint64_t)b << 32 | (uint32_t)(of_ended ? a.end_token : x.token);
   };
-  constexpr int R = 4;   // candidates a thread keeps; more are looked up again
+  // each(key, id) of this thread's candidates, R of which it keeps; more are looked up again, several at once
+  constexpr int R = 4;
   uint64_t keys[R], ids[R];
-  uint32_t most[1] = {0};
 #pragma unroll
-  for (int j = 0; j < R; ++j) {
-    keys[j] = 0;
-    if (tid + 256 * j < all) candidate(tid + 256 * j, keys[j], ids[j]);
-    most[0] = max(most[0], (uint32_t)(keys[j] >> 32));
-  }
-  for (int i = tid + 256 * R; i < all; i += 256) {
-    uint64_t key, id;
-    candidate(i, key, id);
-    most[0] = max(most[0], (uint32_t)(key >> 32));
-  }
-  const uint32_t mine = wave_nth_key(most, a.best);
-  if (lane == 0) bounds[wave] = mine;
-  __syncthreads();
-  const uint32_t bound = max(max(bounds[0], bounds[1]), max(bounds[2], bounds[3]));
-  auto offer = [&](uint64_t key, uint64_t id) {
-    if (key != 0 && (uint32_t)(key >> 32) >= bound) {
-      const int at = atomicAdd(&listed, 1);
-      if (at < kPickCap) list[at] = Ranked{key, id};
+  for (int j = 0; j < R; ++j) candidate(tid + T * j, keys[j], ids[j]);
+  auto pass = [&](auto each) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) each(keys[j], ids[j]);
+    for (int i = tid + T * R; i < all; i += T * R) {
+      uint64_t k[R], d[R];
+#pragma unroll
+      for (int j = 0; j < R; ++j) candidate(i + T * j, k[j], d[j]);
+#pragma unroll
+      for (int j = 0; j < R; ++j) each(k[j], d[j]);
     }
   };
+  uint32_t most[1] = {0};
+  pass([&](uint64_t key, uint64_t) { most[0] = max(most[0], (uint32_t)(key >> 32)); });
+  const uint32_t mine = wave_nth_key(most, a.best);
+  uint32_t top = most[0];
 #pragma unroll
-  for (int j = 0; j < R; ++j) offer(keys[j], ids[j]);
-  for (int i = tid + 256 * R; i < all; i += 256) {
-    uint64_t key, id;
-    candidate(i, key, id);
-    offer(key, id);
+  for (int m = 32; m >= 1; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+  if (lane == 0) {
+    bounds[wave] = mine;
+    tops[wave] = top;
   }
   __syncthreads();
-  const int n = listed;
+  uint32_t bound = 0;
+#pragma unroll
+  for (int v = 0; v < NW; ++v) {
+    bound = max(bound, bounds[v]);
+    top = max(top, tops[v]);
+  }
+  auto offer = [&](uint64_t key, uint64_t id) {
+    const int at = atomicAdd(&listed, 1);
+    if (at < kPickCap) list[at] = Ranked{key, id};
+  };
+  pass([&](uint64_t key, uint64_t id) {
+    if (key != 0 && (uint32_t)(key >> 32) >= bound) offer(key, id);
+  });
+  __syncthreads();
+  int n = listed;
+  if (n > kPickCap) {
+    // The best are those above a range and `left` of the ones in it: first of keys, then of the ids (counted from
+    // the last one) of those with one key. (There are more than a.best from the bound on.)
+    uint64_t lo = bound ? (uint64_t)bound << 32 : 1, hi = (uint64_t)top << 32 | 0xffffffffu, tie = 0;
+    bool of_tie = false;
+    int left = a.best;
+    for (int step = 0; step < 10; ++step) {   // (64 bits of a key and 38 of an id, 11 at a time)
+      const int shift = max(0, 53 - (int)__clzll((hi - lo) | 1));   // (to 11 bits)
+      for (int i = tid; i < kBins; i += T) count[i] = 0;
+      __syncthreads();
+      pass([&](uint64_t key, uint64_t id) {
+        const uint64_t x = of_tie ? kLastId - id : key;
+        if ((!of_tie || key == tie) && x >= lo && x <= hi) atomicAdd(&count[(x - lo) >> shift], 1);
+      });
+      __syncthreads();
+      int bin;
+      find_bin<NW>(count, sums, found, left, bin);
+      const int in_bin = count[bin];
+      lo += (uint64_t)bin << shift;
+      hi = min(hi, lo + (((uint64_t)1 << shift) - 1));
+      if (tid == 0) listed = 0;
+      __syncthreads();   // (the counts have been read)
+      if (a.best - left + in_bin <= kPickCap) break;
+      if (lo == hi) {   // (no two candidates have one key and one id)
+        tie = lo;
+        of_tie = true;
+        lo = 0;
+        hi = kLastId;
+      }
+    }
+    pass([&](uint64_t key, uint64_t id) {
+      if (of_tie ? key > tie || (key == tie && kLastId - id >= lo) : key >= lo) offer(key, id);
+    });
+    __syncthreads();
+    n = listed;
+  }
   auto write = [&](int place, uint64_t key, uint64_t id) {
     const int64_t to = (int64_t)item * a.best + place;
     a.out_scores[to] = key ? (float)from_order_key(key) : kMinusInf;
     a.out_tokens[to] = key ? (int32_t)(uint32_t)id : -1;
     a.out_parents[to] = key ? (int32_t)(id >> 32) : -1;
   };
-  if (n <= kPickCap) {
-    for (int i = tid; i < n; i += 256) {
-      const Ranked me = list[i];
-      int place = 0;
+  for (int i = tid; i < n; i += T) {
+    const Ranked me = list[i];
+    int place = 0;
 #pragma unroll 8
-      for (int j = 0; j < n; ++j) {
-        const Ranked x = list[j];
-        place += (int)(x.key > me.key) | ((int)(x.key == me.key) & (int)(x.id < me.id));
-      }
-      if (place < a.best) write(place, me.key, me.id);
+    for (int j = 0; j < n; ++j) {
+      const Ranked x = list[j];
+      place += (int)(x.key > me.key) | ((int)(x.key == me.key) & (int)(x.id < me.id));
     }
-    for (int i = n + tid; i < a.best; i += 256) write(i, 0, 0);
-    return;
+    if (place < a.best) write(place, me.key, me.id);
   }
-  uint64_t last_key = ~0ull, last_id = 0;   // candidates are in order of falling keys, rising ids
-  for (int r = 0; r < a.best; ++r) {
-    uint64_t best_key = 0, best_id = ~0ull;
-    auto better = [&](uint64_t k, uint64_t d) {
-      if (k > best_key || (k == best_key && d < best_id)) {
-        best_key = k;
-        best_id = d;
-      }
-    };
-    for (int i = tid; i < all; i += 256) {
-      uint64_t key, id;
-      candidate(i, key, id);
-      if (key != 0 && (key < last_key || (key == last_key && id > last_id))) better(key, id);
-    }
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-      const uint64_t k = __shfl_xor(best_key, m), d = __shfl_xor(best_id, m);
-      better(k, d);
-    }
-    __syncthreads();
-    if (lane == 0) list[wave] = Ranked{best_key, best_id};
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 4; ++w) better(list[w].key, list[w].id);
-    if (tid == 0) write(r, best_key, best_id);
-    last_key = best_key;
-    last_id = best_id;
-  }
+  for (int i = n + tid; i < a.best; i += T) write(i, 0, 0);
 }
 
 // ---------------------------------------------------------------- the tables
@@ -583,7 +603,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamTableArgs a) {
     m.take(a, p, n, !fits, lane);
     const bool copy = lane < W && m.copied[lane];
     const uint64_t mask = __ballot(copy);
-    const int before = lanes_before(mask);
+    const int before = lanes_before(mask, 0);
     if (lane < W) fresh[lane] = copy ? a.free_pages[first + s[0] + before] : -1;
   }
   if (blockIdx.x == 0 && tid == 0) {
@@ -736,9 +756,15 @@ extern "C" halo_status_t halo_beam_select(const halo_beam_sizes_t* sizes, const 
   hipStream_t s = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   const dim3 grid((unsigned)((g.num_parts + 3) / 4), (unsigned)rows);
-  if (sizes->dtype == HALO_BF16) hipLaunchKernelGGL(beam_scan_kernel<__bf16>, grid, dim3(256), 0, s, g);
-  else hipLaunchKernelGGL(beam_scan_kernel<float>, grid, dim3(256), 0, s, g);
-  hipLaunchKernelGGL(beam_pick_kernel, dim3(sizes->num_items), dim3(256), 0, s, g);
+  const bool bf16 = sizes->dtype == HALO_BF16, many = sizes->num_best >= kLongListFrom && g.per >= kLongPart;
+  if (bf16 && many) hipLaunchKernelGGL((beam_scan_kernel<__bf16, kLongListCap>), grid, dim3(256), 0, s, g);
+  else if (bf16) hipLaunchKernelGGL((beam_scan_kernel<__bf16, kListCap>), grid, dim3(256), 0, s, g);
+  else if (many) hipLaunchKernelGGL((beam_scan_kernel<float, kLongListCap>), grid, dim3(256), 0, s, g);
+  else hipLaunchKernelGGL((beam_scan_kernel<float, kListCap>), grid, dim3(256), 0, s, g);
+  if ((int64_t)sizes->num_beams * g.num_parts * sizes->num_best > kManyCandidates)
+    hipLaunchKernelGGL(beam_pick_kernel<16>, dim3(sizes->num_items), dim3(1024), 0, s, g);
+  else
+    hipLaunchKernelGGL(beam_pick_kernel<4>, dim3(sizes->num_items), dim3(256), 0, s, g);
   return hip_check("beam selection launch");
 }
 

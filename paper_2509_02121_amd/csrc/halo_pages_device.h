@@ -63,6 +63,45 @@ __device__ __forceinline__ int wave_inclusive_sum(int x) {
   return x;
 }
 
+// How many lanes before this one the mask has, and `more`.
+__device__ __forceinline__ int lanes_before(uint64_t mask, int more) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, more));
+}
+
+constexpr int kBins = 2048;      // 11 bits
+
+// The largest of the kBins counts' places with `left` or more at or above it, and how
+// many of `left` fall into it, by the whole workgroup.
+template <int W>
+__device__ __forceinline__ void find_bin(const int (&count)[kBins], int (&sums)[W], int (&found)[2], int& left, int& bin) {
+  constexpr int N = kBins / (64 * W);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  int c[N], mine = 0;
+#pragma unroll
+  for (int j = 0; j < N; ++j) mine += c[j] = count[kBins - 1 - (N * tid + j)];
+  const int upto = wave_inclusive_sum(mine);
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int above = upto - mine;
+#pragma unroll
+  for (int v = 0; v < W; ++v) above += v < wave ? sums[v] : 0;
+  if (above < left && above + mine >= left) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (above < left && above + c[j] >= left) {
+        found[0] = kBins - 1 - (N * tid + j);
+        found[1] = left - above;
+        above = INT32_MAX / 2;
+      } else {
+        above += c[j];
+      }
+    }
+  }
+  __syncthreads();
+  bin = found[0];
+  left = found[1];
+}
+
 // The range of one sequence, and its whole-page tiles (none where the range
 // does not fit its page list: its own workgroup flags that).
 struct SeqRange {

@@ -87,6 +87,24 @@ def test_select_ties_and_orders(gpu_lib, kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["random", "equal", "few", "close"])
+@pytest.mark.parametrize("n,w,vocab,best", [(1, 16, 20011, 64), (2, 64, 3001, 64), (2, 3, 40009, 33), (1, 1, 70001, 64)])
+def test_select_many_candidates(gpu_lib, n, w, vocab, best, kind, dtype):
+    """More candidates than are put in order together: all apart, all the same, of few values, and of nearly one."""
+    logits, scores = _random(n, w, vocab, dtype, 31)
+    if kind == "equal":
+        logits.fill_(0.5)
+    elif kind == "few":
+        logits = logits.round().clamp(-1, 2)
+    elif kind == "close":
+        logits = (4 + torch.arange(w, device="cuda")[None, :, None] * 2.0 ** -6 + 0 * logits.float()).to(dtype)
+        logits[:, :, ::7] += 2.0 ** -5
+    if kind != "random":
+        scores[:] = -6.25
+    check_select(logits, scores, best)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_select_masked_logits(gpu_lib, dtype):
     logits, scores = _random(4, 3, 3001, dtype, 7)
     low = torch.finfo(dtype).min
