@@ -571,7 +571,8 @@ typedef struct {
  * negative, past width or past its pages is skipped whole, a page whose id is
  * outside [0, num_pool_pages) and an entry whose row is outside [0, num_rows) by
  * itself, and one whose entries are no range of [0, num_entries) has none; 1 is then
- * written to error_flag (may be NULL; 0 never is). */
+ * written to error_flag (may be NULL; 0 never is). Entries that see no token need not be
+ * looked at. */
 halo_status_t halo_kv_page_weights(const void* k_pool, const halo_attn_params_t* params,
                                    const halo_weight_sizes_t* sizes,
                                    const int32_t* page_ids, const int32_t* seq_page_indptr,

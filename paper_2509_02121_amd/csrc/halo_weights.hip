@@ -127,6 +127,14 @@ struct WeightSeq {
   }
 };
 
+// Flags sequences without pages that are to have tokens, which no job comes by: 64 a wave, from the last wave on, as
+// small calls leave it without a job.
+__device__ __forceinline__ void flag_without_pages(const WeightArgs& a) {
+  if (!a.error_flag) return;
+  for (uint32_t i = (gridDim.x - blockIdx.x) * 256 - 1 - threadIdx.x; i < (uint32_t)a.num_seqs; i += gridDim.x * 256)
+    if (a.seq_page_indptr[i + 1] == a.seq_page_indptr[i] && a.seq_end[i] != 0) a.error_flag[0] = 1;
+}
+
 // The (page slot, head) tiles are dealt to the waves in jobs of `run` slots of one
 // head, which may span sequences; of a job a wave takes up to NP pages of one
 // sequence at a time, and passes all its rows by them. Rows are the A operand and keys the B
@@ -137,6 +145,7 @@ __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
   using Fmt = KeyFormat<T, KVQ, D>;
   using F = typename Fmt::F;
   constexpr int NS = D / 32, NP = weight_pages<T, KVQ, D>(), PARTS = Fmt::kParts;
+  flag_without_pages(a);
   const int lane = threadIdx.x & 63, key = lane & 15, grp = lane >> 4;
   const int H = a.num_kv_heads, G = a.group;
   const int first = a.seq_page_indptr[0];
@@ -168,9 +177,10 @@ __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
       bool ok[NP];
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        const int pid = p < n && t0 + 16 * p < s.end ? a.page_ids[s.base + from + p] : -2;
+        const bool asked = p < n && t0 + 16 * p < s.end;
+        const int pid = asked ? a.page_ids[s.base + from + p] : -1;
         ok[p] = pid >= 0 && pid < a.num_pool_pages;
-        if (!ok[p] && pid != -2 && lane == 0 && a.error_flag) a.error_flag[0] = 1;
+        if (asked && !ok[p] && lane == 0 && a.error_flag) a.error_flag[0] = 1;
         // (a page that is none is read as page 0 and not written)
         Fmt::load_keys(static_cast<const uint8_t*>(a.k_pool) + ((int64_t)(ok[p] ? pid : 0) * H + h) * Fmt::kTile, lane, k[p]);
       }
@@ -388,6 +398,7 @@ __device__ __forceinline__ void weights_step(const WeightArgs& a) {
 }
 template <typename T, bool KVQ, int D>
 __global__ __launch_bounds__(256, step_waves<T>()) void weights_step_kernel(WeightArgs a) {
+  flag_without_pages(a);
   const int64_t slots = (int64_t)a.seq_page_indptr[a.num_seqs] - a.seq_page_indptr[0];
   if (!KVQ && slots * a.num_kv_heads * KeyFormat<T, KVQ, D>::kTile > kStepCached) weights_step<T, KVQ, D, !KVQ>(a);
   else weights_step<T, KVQ, D, false>(a);
@@ -756,7 +767,10 @@ __device__ __forceinline__ void weights_wide(const WeightArgs& a) {
 
 // (the body in a function of its own: the host's pass does not know the direct loads)
 template <bool KVQ, int D, bool HELD>
-__global__ __launch_bounds__(256, 2) void weights_wide_kernel(WeightArgs a) { weights_wide<KVQ, D, HELD>(a); }
+__global__ __launch_bounds__(256, 2) void weights_wide_kernel(WeightArgs a) {
+  flag_without_pages(a);
+  weights_wide<KVQ, D, HELD>(a);
+}
 
 // Whether a sequence has `rows` rows or more on average. The wide kernel takes bf16 queries from 17 on, where
 // the general one passes a second tile (window of 8 tokens, G 4, sequences of 1000-8000 tokens: 113 us general, 73 wide;

@@ -343,6 +343,41 @@ def test_what_does_not_fit_is_flagged(gpu_lib, kvq):
     assert (out == -7.0).all()
 
 
+@pytest.mark.parametrize("rows", [1, 3, 40, 700])
+def test_tokens_without_pages_are_flagged(gpu_lib, rows):
+    """A sequence of no pages at all whose end says that it has tokens: skipped and flagged; without any it is not."""
+    for at in (0, 1, 2):
+        lengths = [30, 20]
+        lengths.insert(at, 0)
+        case = Case(lengths, [rows] * 3, (2, 1), 64, BF16, seed=28)
+        ends = list(lengths)
+        for end, want in ((0, 0), (5, 1), (-1, 1)):
+            ends[at] = end
+            flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+            lists = dict(row_indptr=None) if rows == 1 else {}
+            case.check(_call(case, seq_end=cuda(ends), error_flag=flag, **lists))
+            assert int(flag) == want, (at, end)
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    none = Case([0, 0], [rows] * 2, (2, 1), 64, BF16, seed=29)
+    none.check(_call(none, page_ids=cuda([0]), seq_end=cuda([0, 3]), error_flag=flag))
+    assert int(flag) == 1
+
+
+@pytest.mark.parametrize("dtype,rows", [(F32, 1), (F32, 3), (BF16, 1), (BF16, 3), (BF16, 40), (BF16, 700)])
+@pytest.mark.parametrize("bad", [-1, -2, -2 ** 31, 5, 2 ** 31 - 1])
+def test_any_bad_page_is_flagged(gpu_lib, bad, dtype, rows):
+    case = Case([30, 20], [rows] * 2, (2, 1), 64, dtype, seed=30, extra_pages=1)
+    assert len(case.pool) == 5
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ids = case.ids.clone()
+    ids[3] = bad                                          # the second page of the second sequence
+    out = _call(case, page_ids=ids, error_flag=flag, **(dict(row_indptr=None) if rows == 1 else {}))
+    assert int(flag) == 1 and (out[1, :, 16:] == -7.0).all()
+    want, bound = case.expected(1)
+    assert (np.abs(out[1, :, :16].double().cpu().numpy() - want[:, :16]) <= bound[:, :16]).all()
+    case.check(out, which=[(0, 30)])
+
+
 def test_no_lists_and_too_few_rows(gpu_lib):
     case = Case([40, 50], [1, 1], seed=14)
     flag = torch.zeros(1, dtype=torch.int32, device="cuda")
