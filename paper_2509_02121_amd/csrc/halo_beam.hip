@@ -173,6 +173,8 @@ struct Tile {
 // seen one; it is found anew after 1, 2, 4, 8, ... tiles, so that of a part in any order about
 // `best` more are listed each time the part seen doubles. A full list is cut to the
 // first `best`; then only what is above the last of these counts (ties with it are later tokens).
+// Bound by HBM: 1024 rows of 200019 fp32 logits, 819 MB, 16 best, 138 us (5.9 TB/s); with fewer tiles a wave by its start
+// and end: 256 rows of 128256 bf16 logits, 66 MB, 8 best, 23 us.
 template <typename T, int CAP>
 __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
   __shared__ float list_value[4][CAP];
@@ -280,7 +282,8 @@ struct Ranked {
 // many of the list come before it. The bound: of each wave's lane maxima the best-th largest
 // one (in the upper 32 bits), of the waves' the largest. Where the list does not hold them all, the candidates
 // from the bound up are counted in 2048 equal parts of their range, then those of the part that holds the last one
-// of the best, and so on, of equal keys by their ids, until what is left fits.
+// of the best, and so on, of equal keys by their ids, until what is left fits. Bound by latency: 4 beams of 16 parts with
+// 8 best 6.9 us; 16 beams of 16 parts with 64 best, 16384 candidates, 54 us (a round for each of the best: 2100).
 template <int NW>
 __global__ __launch_bounds__(64 * NW) void beam_pick_kernel(BeamArgs a) {
   constexpr int T = 64 * NW;
@@ -496,7 +499,8 @@ constexpr int kHeld = 8;
 // beam without children is free if no beam with children has it there, nor an
 // earlier beam without: each place of the rows is looked at by itself, W x W
 // comparisons, without counts of references. A thread has a place, and the pages of all
-// beams there (of more than kHeld beams: of kHeld at a time, against the others).
+// beams there (of more than kHeld beams: of kHeld at a time, against the others). Bound by latency: 4 items of 4 beams
+// 3.8 us, 256 items of 8 beams of up to 256 pages 7.4.
 __global__ __launch_bounds__(256) void beam_freed_kernel(BeamTableArgs a) {
   __shared__ ItemBeams m;
   __shared__ int sums[4];
@@ -566,7 +570,8 @@ __global__ __launch_bounds__(256) void beam_freed_kernel(BeamTableArgs a) {
 }
 
 // The items' rows, copies and freed pages at their places: sums over the items before
-// each one, which every workgroup makes itself.
+// each one, which every workgroup makes itself (in a launch of its own, as it needs all counts). Bound by latency: 4
+// items of 4 beams 5.5 us, 256 items of 8 beams of up to 256 pages 7.5.
 __global__ __launch_bounds__(256) void beam_rows_kernel(BeamTableArgs a) {
   __shared__ ItemBeams m;
   __shared__ int32_t sums[4][5];   // (a table has less than 2^31 pages)
