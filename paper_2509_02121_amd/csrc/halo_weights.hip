@@ -777,7 +777,11 @@ __global__ __launch_bounds__(256, 2) void weights_wide_kernel(WeightArgs a) {
 // Whether a sequence has `rows` rows or more on average. The wide kernel takes bf16 queries from 17 on, where
 // the general one passes a second tile (window of 8 tokens, G 4, sequences of 1000-8000 tokens: 113 us general, 73 wide;
 // of 4 tokens: 93 and 83; 512 sequences of 50-200 tokens: 85 and 81, of 4 tokens 55 and 89). It holds them up to 512: 128
-// tokens, 224 us a batch at a time, 205 held; 256 tokens, 397 and 427.
+// tokens, 224 us a batch at a time, 205 held; 256 tokens, 397 and 427. Short sequences do not pay for what a
+// workgroup waits for at their beginning: 2048 of 30-64 tokens with windows of 8, 16 and 32 take 135, 201 and 351 us by
+// the general kernel, 179, 217 and 293 a batch at a time, 249, 281 and 336 held; 512 of 200-300 tokens 130, 193 and 324,
+// 106, 121 and 152, 106, 115 and 134. How many tokens there are is known here by the weights' width alone.
+constexpr int kShortWidth = 80, kHeldWidth = 129;   // five pages; more than eight
 bool many_rows(const halo_weight_sizes_t& s, bool lists, int group, int rows) {
   return (int64_t)(lists ? s.num_entries : s.num_seqs) * group >= rows * (int64_t)s.num_seqs;
 }
@@ -824,8 +828,8 @@ halo_status_t page_weights(bool kvq, const void* k_pool, const halo_attn_params_
                sizes->width, H, params->num_q_heads / H, params->sm_scale * kLog2e, decay};
   (void)hipGetLastError();
   const bool step = !row_indptr && g.group <= 16 && params->num_pool_pages > 0;
-  const bool wide = params->kv_dtype == HALO_BF16 && many_rows(*sizes, row_indptr != nullptr, g.group, 17);
-  const bool held = !many_rows(*sizes, row_indptr != nullptr, g.group, 2 * kHeldRows + 1);
+  const bool wide = params->kv_dtype == HALO_BF16 && many_rows(*sizes, row_indptr != nullptr, g.group, sizes->width <= kShortWidth ? 65 : 17);
+  const bool held = sizes->width >= kHeldWidth && !many_rows(*sizes, row_indptr != nullptr, g.group, 2 * kHeldRows + 1);
   by_type_and_dim(params, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;

@@ -209,6 +209,17 @@ def test_a_window_of_rows(gpu_lib, dim, kvq):
     case.check(torch.where(torch.arange(case.width, device="cuda") < cuda(lengths)[:, None, None], once, -7.0))
 
 
+@pytest.mark.parametrize("kvq", [False, True])
+@pytest.mark.parametrize("longest", [50, 100, 200])
+@pytest.mark.parametrize("rows", [10, 30, 90])
+def test_short_sequences(gpu_lib, rows, longest, kvq):
+    """Many sequences to a job, some empty, with rows for each of the kernels that weights of this width may go to."""
+    rng = np.random.default_rng(32)
+    lengths = [*rng.integers(0, longest, 60), longest]
+    case = Case(lengths, rng.integers(rows // 2, rows, 61), (4, 2), 64, BF16, kvq, seed=32)
+    case.check(_call(case))
+
+
 def test_lists_that_are_left_out(gpu_lib):
     case = Case([50, 20, 90], [3, 0, 20], seed=6, causal=False)
     case.check(_call(case, row_end=None))
