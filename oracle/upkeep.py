@@ -91,7 +91,9 @@ def select(logits, scores, ended, end_token, best):
             continue
         if np.isnan(row).any() or (row == np.inf).any() or (row == -np.inf).all():
             continue
-        value = (row - log_sum_exp(row)) + float(scores[b])
+        # (from the largest logit, in whose size ln sum exp may be lost)
+        top = np.max(row)
+        value = ((row - top) - log_sum_exp(row - top)) + float(scores[b])
         live = np.flatnonzero(row > -np.inf)
         # (a beam's candidates past its own best `best` are none of the item's)
         order = live[np.lexsort((live, -row[live]))][:best]

@@ -287,7 +287,9 @@ struct Ranked {
 template <int NW>
 __global__ __launch_bounds__(64 * NW) void beam_pick_kernel(BeamArgs a) {
   constexpr int T = 64 * NW;
-  __shared__ double lse[kMaxBeams];
+  // ln sum exp of a beam's logits is top + ln_sum, not added: of logits of 1e20 the sum would be top
+  __shared__ double ln_sum[kMaxBeams];
+  __shared__ float top_of[kMaxBeams];
   __shared__ int32_t live[kMaxBeams];   // 0 dead, 1 live, 2 ended
   __shared__ __align__(16) Ranked list[kPickCap];
   __shared__ int count[kBins];
@@ -315,7 +317,8 @@ __global__ __launch_bounds__(64 * NW) void beam_pick_kernel(BeamArgs a) {
     if (lane == 0) {
       // (a NaN or +inf among the logits makes the sum no number)
       const bool sound = is_finite(s) && s > 0 && is_finite(most);
-      lse[b] = sound ? (double)most + log(s) : 0;
+      top_of[b] = most;
+      ln_sum[b] = sound ? log(s) : 0;
       live[b] = !open ? 0 : ended ? 2 : sound ? 1 : 0;
     }
   }
@@ -330,7 +333,7 @@ __global__ __launch_bounds__(64 * NW) void beam_pick_kernel(BeamArgs a) {
     const Candidate x = a.candidates[(int64_t)row * per_row + j];   // (of a beam that is not live: anything)
     const double score = (double)a.scores[row];
     const bool of_live = in && how == 1 && x.token >= 0, of_ended = in && how == 2 && j == 0;
-    key = order_key(of_ended ? score : ((double)x.value - lse[b]) + score);
+    key = order_key(of_ended ? score : (((double)x.value - (double)top_of[b]) - ln_sum[b]) + score);
     if (!of_live && !of_ended) key = 0;
     id = (uint64_t)b << 32 | (uint32_t)(of_ended ? a.end_token : x.token);
   };

@@ -184,6 +184,25 @@ def test_select_extreme_logits(gpu_lib):
     check_select(logits, scores, 2)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", [2, 700, 5000])
+@pytest.mark.parametrize("high", [False, True])
+def test_select_a_beam_whose_tokens_are_all_masked_alike(gpu_lib, high, vocab, dtype):
+    """Every logit the type's lowest (or largest) number: ln sum exp is that number in 64 bits too, and each token has
+    1 / vocab of the beam."""
+    logits, _ = _random(1, 2, vocab, dtype, vocab)
+    logits[0, 0] = torch.finfo(dtype).max if high else torch.finfo(dtype).min
+    logits[0, 1] = 0.0
+    logits[0, 1, 1] = 1.0                      # (the largest of the other beam, and better than any of the masked one)
+    out = check_select(logits, [[-1.0, -1.0]], 2 * vocab if vocab == 2 else 3)
+    own = 1.0 - np.log(vocab - 1 + np.e)
+    want = sorted([(-1 + own, 1, 1)] + [(-1 - np.log(vocab), 0, t) for t in range(2)] +
+                  [(-1 - np.log(vocab - 1 + np.e), 1, 0)], key=lambda x: (-x[0], x[1], x[2]))[:out.num_best]
+    assert out.parents[0].tolist() == [x[1] for x in want] and out.tokens[0].tolist() == [x[2] for x in want]
+    # (a fp32 rounding of a number below 16, an exponential and a sum)
+    assert np.allclose(out.scores[0].double().cpu().numpy(), [x[0] for x in want], rtol=0, atol=(16 + vocab / 64 + 40) * U)
+
+
 # ------------------------------------------------------------------ the tables
 
 class Beams:

@@ -76,6 +76,14 @@ def test_select_by_hand():
     assert upkeep.select(logits, [-np.inf] * 3, None, 0, 2) == ([-np.inf] * 2, [-1, -1], [-1, -1])
 
 
+def test_select_of_logits_that_are_all_the_lowest_number():
+    """Each of n tokens has 1 / n of the beam, also where ln n is nothing beside the logits."""
+    low = float(np.finfo(np.float32).min)
+    s, t, p = upkeep.select([[low] * 4, [0.0] * 3 + [-np.inf]], [-1.0, -1.0], None, 0, 4)
+    assert t == [0, 1, 2, 0] and p == [1, 1, 1, 0]
+    assert np.allclose(s, [-1 - math.log(3)] * 3 + [-1 - math.log(4)], rtol=1e-15)
+
+
 def test_beam_tables_by_hand():
     # beams 0 and 1 share page 3; both go on from beam 1, whose page 5 is partly filled
     new = upkeep.beam_tables(1, 2, [[1, 1]], [20, 20], [[3, 4, -1], [3, 5, -1]], [8, 6, 7], 1)
