@@ -686,7 +686,8 @@ int64_t halo_beam_workspace_bytes(const halo_beam_sizes_t* sizes);
  * no candidate, nor is any of a beam whose score is not finite or whose logits
  * hold a NaN or +inf. A beam with ended[w] != 0 (ended may be NULL) offers its
  * end_token at its own score and nothing else. Where there are fewer candidates, the rest is -inf, -1, -1.
- * Candidates are compared in 64 bits (the exponentials are in fp32, their sums joined in 64). DEVICE
+ * Candidates are compared in 64 bits; the exponentials, and their sums along each of the 64 or more
+ * lanes that share a row, are in fp32, and the lanes' sums are joined in 64 bits. DEVICE
  * pointers; logits need only their elements' alignment; no output and no part of the
  * workspace (256-byte aligned, its contents on entry do not matter) may overlap another array. */
 halo_status_t halo_beam_select(const halo_beam_sizes_t* sizes, const void* logits, const float* scores,

@@ -28,8 +28,8 @@ constexpr float kMinusInf = -__builtin_huge_valf();
 
 // What a wave found in its part of a row.
 struct BeamPart {
-  float top;   // the largest logit, or the lowest finite number
-  float sum;   // of exp(logit - top)
+  float top;    // the largest logit, or the lowest finite number
+  double sum;   // of exp(logit - top)
 };
 struct Candidate {
   float value;
@@ -251,10 +251,10 @@ __global__ __launch_bounds__(256) void beam_scan_kernel(BeamArgs a) {
   float most = top;
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
-  double s = (double)sum * exp2((double)(top - most) * 1.44269504088896340736);
+  double s = (double)sum * exp2(((double)top - (double)most) * 1.44269504088896340736);
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
-  if (lane == 0) *out = BeamPart{most, (float)s};
+  if (lane == 0) *out = BeamPart{most, s};
 }
 
 // ---------------------------------------------------------------- the best of an item
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(64 * NW) void beam_pick_kernel(BeamArgs a) {
     for (int m = 32; m >= 1; m >>= 1) most = fmaxf(most, __shfl_xor(most, m));
     double s = 0;
     for (int p = lane; p < P; p += 64)
-      s += read ? (double)parts[p].sum * exp2((double)(parts[p].top - most) * 1.44269504088896340736) : 0;
+      s += read ? parts[p].sum * exp2(((double)parts[p].top - (double)most) * 1.44269504088896340736) : 0;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
     if (lane == 0) {

@@ -203,6 +203,22 @@ def test_select_a_beam_whose_tokens_are_all_masked_alike(gpu_lib, high, vocab, d
     assert np.allclose(out.scores[0].double().cpu().numpy(), [x[0] for x in want], rtol=0, atol=(16 + vocab / 64 + 40) * U)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_select_sums_are_joined_in_64_bits(gpu_lib, dtype):
+    """Two beams whose sums of exponentials, 504 and 8 times e^-20 or e^-21, are one number in 32 bits: the candidates
+    of the one with the smaller sum come first. (The 8 tokens of small logits are one lane's: in its fp32 sum they
+    have nothing larger beside them.)"""
+    logits = torch.zeros((1, 2, 512), dtype=dtype, device="cuda")
+    per = 16 // dtype.itemsize
+    tokens = [(u * 64 + 5) * per + i for u in range(8 // per) for i in range(per)]
+    assert np.float32(504 + 8 * np.exp(-20.0)) == np.float32(504 + 8 * np.exp(-21.0))
+    for small in ((-20.0, -21.0), (-21.0, -20.0)):
+        for b in range(2):
+            logits[0, b, tokens] = small[b]
+        out = check_select(logits, [[-1.0, -1.0]], 4)
+        assert out.parents[0].tolist() == [int(small[1] < small[0])] * 4 and out.tokens[0].tolist() == [0, 1, 2, 3]
+
+
 # ------------------------------------------------------------------ the tables
 
 class Beams:
