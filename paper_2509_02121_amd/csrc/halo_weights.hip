@@ -173,8 +173,8 @@ __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
       slot += n;
       if ((s.bad || s.bad_rows || a.num_pool_pages == 0) && lane == 0 && a.error_flag) a.error_flag[0] = 1;
       if (s.bad || a.num_pool_pages == 0) continue;
+      if ((int64_t)from * 16 >= s.end) continue;   // (a list may have more pages than 32-bit tokens)
       const int t0 = from * 16;
-      if (t0 >= s.end) continue;
       F k[NP][NS];
       bool ok[NP];
 #pragma unroll
@@ -367,8 +367,9 @@ __device__ __forceinline__ void weights_step(const WeightArgs& a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) l2[j] = fine && 4 * grp + j < G ? a.lse[row + 4 * grp + j] * kLog2e : kNegInf;
           }
-          const int t0 = (slot - base) * 16, pid = __builtin_amdgcn_readlane(ids, i);
-          const bool ok = pid >= 0 && pid < a.num_pool_pages, here = !bad && t0 < end;
+          const int64_t token = (int64_t)(slot - base) * 16;   // (a list may have more pages than 32-bit tokens)
+          const int t0 = (int)token, pid = __builtin_amdgcn_readlane(ids, i);
+          const bool ok = pid >= 0 && pid < a.num_pool_pages, here = !bad && token < end;
           if (here && !ok && lane == 0 && a.error_flag) a.error_flag[0] = 1;
           if (here && ok) {
             f32x4_t x = {};

@@ -409,6 +409,20 @@ def test_rows_of_weights_past_32_bits(gpu_lib):
     case.check(out[:, :, :340], decay=0.0)
 
 
+@pytest.mark.parametrize("rows,lists,kvq", [(1, False, True), (2, True, False), (40, True, True), (700, True, False)])
+def test_page_lists_past_32_bits(gpu_lib, rows, lists, kvq):
+    """A list of more pages than a sequence has, whose last ones would begin past token 2^31: they are not looked at."""
+    case = Case([100, 40], [rows] * 2, (2, 1), 64, BF16, kvq, seed=33, width=200)
+    much = (1 << 27) + 50
+    ids = torch.full((much + 3,), -1, dtype=torch.int32, device="cuda")
+    ids[:7], ids[much:] = cuda(case.lists[0]), cuda(case.lists[1])
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = _call(case, page_ids=ids, seq_page_indptr=cuda([0, much, much + 3]), error_flag=flag,
+                **({} if lists else dict(row_indptr=None)))
+    assert int(flag) == 0
+    case.check(out)
+
+
 def test_pools_past_32_bits(gpu_lib):
     """Pages behind 2^32 bytes of a pool."""
     case = Case([300, 64], [4, 2], (8, 8), 128, BF16, seed=16)
