@@ -127,12 +127,15 @@ struct WeightSeq {
   }
 };
 
-// Flags sequences without pages that are to have tokens, which no job comes by: 64 a wave, from the last wave on, as
-// small calls leave it without a job.
+// Flags sequences without pages, which no job comes by, that are to have tokens or whose entries are no range: 64 a
+// wave, from the last wave on, as small calls leave it without a job.
 __device__ __forceinline__ void flag_without_pages(const WeightArgs& a) {
   if (!a.error_flag) return;
-  for (uint32_t i = (gridDim.x - blockIdx.x) * 256 - 1 - threadIdx.x; i < (uint32_t)a.num_seqs; i += gridDim.x * 256)
-    if (a.seq_page_indptr[i + 1] == a.seq_page_indptr[i] && a.seq_end[i] != 0) a.error_flag[0] = 1;
+  for (uint32_t i = (gridDim.x - blockIdx.x) * 256 - 1 - threadIdx.x; i < (uint32_t)a.num_seqs; i += gridDim.x * 256) {
+    if (a.seq_page_indptr[i + 1] != a.seq_page_indptr[i]) continue;
+    const WeightSeq s(a, (int)i);
+    if (s.end != 0 || s.bad_rows) a.error_flag[0] = 1;
+  }
 }
 
 // The (page slot, head) tiles are dealt to the waves in jobs of `run` slots of one

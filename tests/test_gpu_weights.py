@@ -374,6 +374,18 @@ def test_tokens_without_pages_are_flagged(gpu_lib, rows):
     assert int(flag) == 1
 
 
+@pytest.mark.parametrize("dtype,rows", [(F32, 3), (BF16, 3), (BF16, 40), (BF16, 700)])
+def test_entries_of_a_sequence_without_tokens_are_checked(gpu_lib, rows, dtype):
+    """The last sequence has no pages, no tokens and entries that are no range of the list."""
+    case = Case([30, 20, 0], [rows] * 3, (2, 1), 64, dtype, seed=34)
+    for end, want in ((3 * rows, 0), (2 * rows, 0), (2 * rows - 1, 1), (3 * rows + 1, 1), (-3, 1), (2 ** 31 - 1, 1)):
+        indptr = case.row_indptr.copy()
+        indptr[3] = end
+        flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+        case.check(_call(case, row_indptr=cuda(indptr), error_flag=flag))
+        assert int(flag) == want, end
+
+
 @pytest.mark.parametrize("dtype,rows", [(F32, 1), (F32, 3), (BF16, 1), (BF16, 3), (BF16, 40), (BF16, 700)])
 @pytest.mark.parametrize("bad", [-1, -2, -2 ** 31, 5, 2 ** 31 - 1])
 def test_any_bad_page_is_flagged(gpu_lib, bad, dtype, rows):
