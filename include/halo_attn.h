@@ -611,7 +611,8 @@ typedef struct {
  * arrays, weights, weights_out [num_seqs][num_kv_heads][width], kept
  * [num_seqs][num_kv_heads][budget]. weights_out may be weights; no other output
  * may overlap an array. A sequence with a negative length or one past width is
- * left alone (new_len[i] = seq_len[i]) and 1 written to error_flag (may be NULL). */
+ * left alone (new_len[i] = seq_len[i]) and 1 written to error_flag (may be NULL).
+ * num_seqs * num_kv_heads must be less than 2^24, where width > 4096 less than 2^22. */
 halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, const float* weights, const int32_t* seq_len,
                                    int32_t* kept, float* weights_out, int32_t* new_len, int32_t* error_flag,
                                    void* stream);
@@ -629,7 +630,8 @@ halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, const float*
  * A sequence whose lengths do not fit its pages or each other (new_len[i] > kept_width where
  * it is less than seq_len[i]) is skipped whole, a token whose kept index is outside [0,
  * seq_len[i]) or a page of which is outside [0, num_pool_pages) by itself; 1 is then
- * written to error_flag (may be NULL). */
+ * written to error_flag (may be NULL).
+ * num_seqs * num_kv_heads must be at most 2^23, in place less than 2^21. */
 halo_status_t halo_kv_page_keep_kv(void* k_pool, void* v_pool, const halo_attn_params_t* params,
                                    const int32_t* page_ids, const int32_t* seq_page_indptr,
                                    const int32_t* seq_len, const int32_t* new_len,

@@ -651,6 +651,9 @@ halo_status_t page_keep(bool kvq, void* k_pool, void* v_pool, const halo_attn_pa
     return fail(HALO_ERR_INVALID_ARGUMENT, "in place, both dst_page_ids and dst_page_indptr are those of the sequences");
   const int64_t blocks = (int64_t)num_seqs * params->num_kv_heads * 2;
   if (blocks > 1 << 24) return fail(HALO_ERR_UNSUPPORTED, "num_seqs * num_kv_heads must be at most 2^23");
+  const bool in_place = dst_page_ids == page_ids;
+  if (in_place && blocks * 64 * kInPlaceWaves > UINT32_MAX)   // (threads of a launch)
+    return fail(HALO_ERR_UNSUPPORTED, "in place, num_seqs * num_kv_heads must be less than 2^21");
   KeepArgs g{static_cast<uint8_t*>(k_pool), static_cast<uint8_t*>(v_pool), page_ids, seq_page_indptr, seq_len, new_len,
              kept, dst_page_ids, dst_page_indptr, error_flag, params->num_pool_pages, num_seqs, params->num_kv_heads,
              kept_width};
@@ -663,7 +666,7 @@ halo_status_t page_keep(bool kvq, void* k_pool, void* v_pool, const halo_attn_pa
     auto launch = [&](auto t, auto kvq) {
       using U = decltype(t);
       constexpr bool Q = decltype(kvq)::value;
-      if (dst_page_ids == page_ids)
+      if (in_place)
         hipLaunchKernelGGL((keep_in_place_kernel<U, Q, D>), dim3((unsigned)blocks), dim3(64 * kInPlaceWaves), 0, s, g);
       else
         hipLaunchKernelGGL((keep_kernel<U, Q, D>), dim3(4096), dim3(256), 0, s, g);
@@ -688,7 +691,9 @@ extern "C" halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, c
   if ((int64_t)sizes->sinks + sizes->recent > sizes->budget || sizes->trigger < sizes->budget)
     return fail(HALO_ERR_INVALID_ARGUMENT, "sinks + recent must be <= budget, and trigger >= budget");
   const int64_t n = sizes->num_seqs, rows = n * sizes->num_kv_heads;
-  if (rows > 1 << 24) return fail(HALO_ERR_UNSUPPORTED, "num_seqs * num_kv_heads must be at most 2^24");
+  const bool long_rows = sizes->width > 4096;
+  if (rows * (long_rows ? 1024 : 256) > UINT32_MAX)   // (threads of a launch)
+    return fail(HALO_ERR_UNSUPPORTED, "num_seqs * num_kv_heads must be less than 2^24, of rows of more than 4096 tokens 2^22");
   if (n == 0) return HALO_OK;
   if (!seq_len || !kept || !new_len || (sizes->width > 0 && (!weights || !weights_out)))
     return fail(HALO_ERR_INVALID_ARGUMENT, "weights, seq_len, kept, weights_out, new_len must not be NULL");
@@ -705,7 +710,7 @@ extern "C" halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, c
     hipLaunchKernelGGL((evict_kernel<W, R>), dim3((unsigned)rows), dim3(64 * W), 0, static_cast<hipStream_t>(stream), g);
   };
   if (sizes->width <= 1024) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
-  else if (sizes->width <= 4096) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
+  else if (!long_rows) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{});
   else launch(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{});
   return hip_check("evict launch");
 }

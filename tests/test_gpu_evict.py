@@ -118,6 +118,16 @@ def test_evict_repeats_in_a_graph(gpu_lib):
             assert torch.equal(a, b) and torch.equal(a, c)
 
 
+def test_evict_as_many_rows_as_a_launch_holds(gpu_lib):
+    n, h = 2 ** 16 - 1, 2 ** 8
+    w = torch.rand((n, h, 2), device="cuda").round(decimals=1)
+    kept = torch.full((n, h, 1), -1, dtype=torch.int32, device="cuda")
+    new_len, out = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros_like(w)
+    halo.kv_evict_select(w, torch.full_like(new_len, 2), kept, new_len, weights_out=out)
+    assert torch.equal(kept[..., 0], (w[..., 1] > w[..., 0]).int()) and bool((new_len == 1).all())
+    assert torch.equal(out[..., 0], w.amax(2)) and not bool(out[..., 1].any())
+
+
 # ------------------------------------------------------------------ moving them
 
 class Keep:
@@ -278,6 +288,24 @@ def test_keep_what_does_not_fit_is_flagged(gpu_lib, kvq):
     case.call(error_flag=flag, params=params(2, 2, 128, BF16, 0))
     case.check(want)
     assert int(flag) == 1
+
+
+def test_keep_in_place_of_as_many_rows_as_a_launch_holds(gpu_lib):
+    """2^21 - 256 (sequence, head) pairs, of which the last sequence's keep their second token."""
+    n, h = 2 ** 13 - 1, 2 ** 8
+    pool = torch.randn((1, h, 16 * 64), device="cuda").to(BF16)
+    want = pool.clone()
+    k = want.view(h, 8, 16, 8)
+    k[:, :, 0] = k[:, :, 1]
+    got = pool.clone()
+    v = torch.zeros_like(pool)
+    lengths, new = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    lengths[-1], new[-1] = 2, 1
+    indptr = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    indptr[-1] = 1
+    kept = torch.ones((n, h, 1), dtype=torch.int32, device="cuda")
+    halo.kv_page_keep_kv(got, v, params(h, h, 64, BF16, 1), cuda([0]), indptr, lengths, new, kept)
+    assert torch.equal(got, want)
 
 
 def test_keep_pools_past_32_bits(gpu_lib):

@@ -190,6 +190,14 @@ def test_evict_refusals(lib):
     assert lib.halo_kv_evict_select(*[None] * 8) == BAD
 
 
+def test_evict_refuses_more_rows_than_a_launch_holds(lib):
+    """A launch has less than 2^32 threads: 256 a row, 1024 where rows have more than 4096 tokens."""
+    for sizes in ((2 ** 14, 2 ** 8, 4097, 8, 8, 1, 2), (2 ** 16, 2 ** 8, 4096, 8, 8, 1, 2), (2 ** 16, 2 ** 8, 0, 8, 8, 1, 2)):
+        assert _evict_call(lib, sizes) == UNSUPPORTED, sizes
+        assert b"num_seqs * num_kv_heads" in lib.halo_last_error_message()
+    assert _evict_call(lib, (2 ** 14, 2 ** 8, 4096, 8, 8, 1, 2)) == BAD     # (looked at further: arrays that overlap)
+
+
 def _keep_call(lib, params=None, width=8, seqs=2, kvq=False, none=(), same=None, **offset):
     a = Buffers("k", "v", "ids", "indptr", "len", "new_len", "kept", "dst_ids", "dst_indptr", "flag").take(none, same,
                                                                                                           **offset)
@@ -216,6 +224,14 @@ def test_keep_refusals(lib, kvq):
     assert call(seqs=0) == halo.HALO_OK
     fn = lib.halo_kvq_page_keep_kv if kvq else lib.halo_kv_page_keep_kv
     assert fn(*[None] * 8, 0, None, None, 1, None, None) == BAD
+
+
+@pytest.mark.parametrize("kvq", [False, True])
+def test_keep_in_place_refuses_more_rows_than_a_launch_holds(lib, kvq):
+    """Two workgroups of 1024 threads a (sequence, head), and a launch has less than 2^32."""
+    same = {"dst_ids": "ids", "dst_indptr": "indptr"}
+    assert _keep_call(lib, {"num_kv_heads": 4}, seqs=2 ** 19, kvq=kvq, same=same) == UNSUPPORTED
+    assert b"in place" in lib.halo_last_error_message()
 
 
 def _release_call(lib, sizes=(2, 16, 4, 8, 0, 0), none=(), same=None, **offset):
