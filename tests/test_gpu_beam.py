@@ -301,6 +301,20 @@ def test_tables_of_many_beams_and_long_rows(gpu_lib):
     case.check(*case.call())
 
 
+@pytest.mark.parametrize("items", [0, 1, 2, 40, 257])
+def test_tables_with_long_free_lists_and_rows(gpu_lib, items):
+    """More of the free list, and of a row, than an item's workgroup passes at once, in calls that fit and that do not."""
+    case = Beams(items, 3, 300 if items else 0, seed=15 + items, spare=150001)
+    case.check(*case.call())
+    if items:
+        case.next = 3
+        case.parents[:] = -1
+        case.check(*case.call(), flagged=True)
+    if 0 < items <= 2:
+        case = Beams(items, 5, 30000, seed=16, width=3000, spare=70000, gone=0.0)
+        case.check(*case.call())
+
+
 def test_tables_more_parents_than_beams(gpu_lib):
     """The first of an item's candidates, as a selection of twice as many gives them."""
     case = Beams(6, 4, 300, seed=4)
