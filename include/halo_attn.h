@@ -440,10 +440,11 @@ halo_status_t halo_prefix_attn_prefill_kvq(const halo_plan_t* plan, const void* 
  *   seq_start, seq_count, seq_end [num_seqs]: seq_len, seq_new and their sum;
  *   in_token_offset [num_seqs] int64: tokens of the sequences before;
  *   positions [max_tokens] int32, slots [max_tokens] int64: of each new token,
- *     its place in its sequence (in the pages of its own row: behind a shared
- *     prefix the caller adds the prefix's length for halo_rope_qk), and page * page_size + place in the page (-1
- *     for a negative page id); behind the last token 0 and -1, as for the
- *     padding of a captured step. Either may be NULL;
+ *     its place in its sequence (in the pages of its own row: for halo_rope_qk the
+ *     caller adds, behind a shared prefix, the prefix's length, and, where tokens of
+ *     the sequence were evicted, how many: see halo_kv_page_keep_kv), and page *
+ *     page_size + place in the page (-1 for a negative page id); behind the last
+ *     token 0 and -1, as for the padding of a captured step. Either may be NULL;
  *   free_next [1]: the first page that is still free.
  * A sequence whose lengths are negative or add up to more than table_width *
  * page_size (or 2^31 - 16) takes part with no pages and no tokens, its seq_end
@@ -626,7 +627,11 @@ halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, const float*
  * page of dst may be a page of src or listed twice (beams that share pages are
  * evicted to pages of their own). A page
  * list holds at least the pages of its tokens; slots past new_len[i] keep what
- * they hold. All pointers but params are DEVICE pointers, pools 16-byte aligned.
+ * they hold. Kept keys stay turned by the positions that they came with, while the
+ * places in the cache are counted anew: a token that comes later has its place
+ * (halo_kv_step_tables' position) plus the tokens that its sequence has lost so far,
+ * the sum of seq_len[i] - new_len[i], as its position for halo_rope_qk.
+ * All pointers but params are DEVICE pointers, pools 16-byte aligned.
  * A sequence whose lengths do not fit its pages or each other (new_len[i] > kept_width where
  * it is less than seq_len[i]) is skipped whole, a token whose kept index is outside [0,
  * seq_len[i]) or a page of which is outside [0, num_pool_pages) by itself; 1 is then

@@ -931,8 +931,8 @@ kv4_page_copy, bind_kv4_page_copy = kvq_page_copy, bind_kvq_page_copy
 class StepTables:
     """The outputs of kv_step_tables (torch tensors on one GPU): the page
     lists, ranges and offsets that kv_page_scatter_kv and kv_page_gather take,
-    positions (in the sequence's own pages: behind a shared prefix its length
-    is to be added for rope_qk) and slots of up to max_tokens new tokens, page
+    positions (in the sequence's own pages: behind a shared prefix its length,
+    and of a sequence that lost tokens how many, is to be added for rope_qk) and slots of up to max_tokens new tokens, page
     lists of up to max_pages pages. seq_end is the next step's seq_len and free_next its
     free_next (copy them there: a call's outputs must not be its inputs)."""
 
@@ -1276,7 +1276,8 @@ def kv_page_keep_kv(k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len, 
                     dst_page_indptr=None, error_flag=None, stream=None):
     """halo_kv_page_keep_kv on torch tensors: the tokens kept [sequences, kv
     heads, budget] of each page list into another one (None: to the front of
-    their own)."""
+    their own). Later tokens' positions for rope_qk are the step tables' plus
+    the tokens that their sequence has lost, seq_len - new_len of every call."""
     load_library()
     _check(_LIB.halo_kv_page_keep_kv(*_keep_args(False, k_pool, v_pool, params, page_ids, seq_page_indptr, seq_len,
                                                  new_len, kept, dst_page_ids, dst_page_indptr, error_flag, stream)))

@@ -12,6 +12,8 @@ import oracle
 from gpu_helpers import assert_parity
 from oracle import upkeep
 from paper_2509_02121_amd import halo
+from test_gpu_step import _rope_reference
+from test_step import rope_frequencies
 from upkeep_helpers import BF16, F32, cuda, params, to_numpy, values
 
 pytestmark = pytest.mark.gpu
@@ -144,6 +146,67 @@ def test_decode_loop_that_evicts(gpu_lib):
         for x, y in zip(c.tokens(lists, now), (keys, vals)):
             assert all(np.array_equal(a, b) for a, b in zip(x, y))
     assert evicted > n
+
+
+def test_decode_loop_that_evicts_with_rotary_positions(gpu_lib):
+    """Kept keys stay turned by the positions that they came with, so a new token's position is its place in the cache,
+    which the step tables give, and the tokens that its sequence has lost; counted on the GPU."""
+    prompts = [70, 12, 48, 33, 1]
+    n, budget, trigger, sinks, recent = len(prompts), 40, 44, 2, 8
+    c = Cache(n, 6, 64, 24)
+    rope, (w, _) = halo.Rope(D), rope_frequencies(D, 10000.0, "none", 1.0, 8192, 32, 1)
+    keys, vals = [[np.zeros((0, H, D))] * n for _ in range(2)]
+    lengths, lost = cuda([0] * n), cuda([0] * n)
+    weights = torch.zeros((n, H, c.table.shape[1] * PAGE), device="cuda")
+    kept = torch.full((n, H, budget), -1, dtype=torch.int32, device="cuda")
+    new_len = cuda([0] * n)
+    came = [0] * n                    # tokens that each sequence has had
+    apart = 0
+    for step in range(14):
+        counts = [1] * n if step else prompts
+        q, k, v = (c.random(sum(counts), heads, D).cuda() for heads in (HQ, H, H))
+        start = lengths
+        steps = c.append(lengths, cuda(counts))
+        lengths = steps.seq_end.clone()
+        positions = steps.positions[:sum(counts)] + torch.repeat_interleave(lost, cuda(counts), output_size=sum(counts))
+        true = torch.tensor([t for i in range(n) for t in range(came[i], came[i] + counts[i])], dtype=torch.int32)
+        assert torch.equal(positions.cpu(), true)
+        apart += int((steps.positions[:sum(counts)].cpu() != true).sum())
+        wanted = [_rope_reference(x, true, w, 1.0, False) for x in (q, k)]
+        halo.rope_qk(q, k, positions, rope)
+        for x, (want, tol) in zip((q, k), wanted):
+            assert ((x.double().cpu() - want).abs() <= tol).all()
+        halo.kv_page_scatter_kv(c.k, c.v, c.params, steps.page_ids, steps.seq_page_indptr, steps.seq_start,
+                                steps.seq_count, steps.in_token_offset, k, v, c.flag)
+        first = np.cumsum([0] + counts)
+        for x, y in zip((keys, vals), (k, v)):
+            for i in range(n):
+                x[i] = np.concatenate([x[i], y[first[i]:first[i + 1]].double().cpu().numpy()])
+        came = [a + b for a, b in zip(came, counts)]
+        host = lengths.tolist()
+        q = q[first[1:] - 1].contiguous()             # each sequence's last query
+        o, lse = c.attend(q, c.lists(c.table, host), host)
+        c.check_attention(o, lse, q, keys, vals, f"step {step}")
+        halo.kv_page_weights(weights, c.k, c.params, steps.page_ids, steps.seq_page_indptr, start, lengths, q, lse,
+                             decay=0.9, error_flag=c.flag)
+        before = weights.double().cpu().numpy()
+        halo.kv_evict_select(weights, lengths, kept, new_len, trigger, sinks, recent, error_flag=c.flag)
+        halo.kv_page_keep_kv(c.k, c.v, c.params, steps.page_ids, steps.seq_page_indptr, lengths, new_len, kept,
+                             error_flag=c.flag)
+        free, free_next = torch.empty_like(c.free), torch.empty_like(c.free_next)
+        halo.kv_release_pages(c.table, lengths, new_len, c.free, c.free_next, free, free_next, c.flag)
+        lost += lengths - new_len
+        c.free, c.free_next, lengths = free, free_next, new_len.clone()
+        for i in range(n):
+            for h in range(H):
+                stay = upkeep.evict(before[i, h], host[i], budget, trigger, sinks, recent)
+                if stay is not None:
+                    for x in (keys, vals):
+                        x[i][:budget, h] = x[i][stay, h]
+            if host[i] > trigger:
+                keys[i], vals[i] = keys[i][:budget], vals[i][:budget]
+        c.pages_are_whole(c.lists(c.table, lengths.tolist()))
+    assert apart > n and [a - b for a, b in zip(came, lengths.tolist())] == lost.tolist()
 
 
 def test_beam_search_that_shares_pages(gpu_lib):
