@@ -301,6 +301,49 @@ def test_special_values(gpu_lib):
     assert np.isnan(out[1, 0, :30]).all() and np.isfinite(out[1, 0, 30:48]).all()
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype,kvq,rows,width", [(BF16, False, 1, 210), (BF16, True, 1, 210), (F32, False, 1, 210),
+                                                  (BF16, False, 40, 210), (BF16, True, 40, 210), (BF16, False, 300, 210),
+                                                  (BF16, True, 300, 210), (BF16, False, 700, 210), (BF16, True, 700, 210),
+                                                  (F32, False, 40, 210), (F32, True, 40, 210)])
+def test_special_values_stay_where_they_are(gpu_lib, rows, width, causal, dtype, kvq):
+    """In each of the kernels a key that is no number spoils its own token and a row that is none the tokens that it
+    sees, whether rows see all keys of a wave or not; a row with lse -inf adds nothing."""
+    case = Case([200, 130, 70], [rows] * 3, (2, 1), 64, dtype, kvq, seed=35, width=width, causal=causal)
+    lists = dict(row_indptr=None) if rows == 1 else {}
+    keys = case.pool.clone()
+    page = int(case.lists[0][4])                       # token 70
+    if kvq:
+        keys[page, :, 64 * 8:].view(1, 16, 2)[:, 6] = 255
+    else:
+        e = 16 // dtype.itemsize
+        keys.view(len(keys), 1, 64 // e, 16, e)[page, 0, 1, 6, 2] = float("nan")
+    others = np.arange(200) != 70
+    case.row_end[0] = 200                              # (a row sees that token)
+    out = _call(case, k_pool=keys, row_end=cuda(case.row_end), **lists).double().cpu().numpy()
+    want, bound = case.expected(0)
+    assert np.isnan(out[0, 0, 70]) and (np.abs(out[0, :, :200] - want)[:, others] <= bound[:, others]).all()
+    for i, n in ((1, 130), (2, 70)):
+        want, bound = case.expected(i)
+        assert (np.abs(out[i, :, :n] - want) <= bound).all()
+    # the middle row of sequence 1: no number, then without a key that it saw
+    e = rows + rows // 2
+    q, lse = case.q.clone(), case.lse.clone()
+    q[case.order[e], 1, 9] = float("nan")
+    for end in (130, 50):
+        ends = case.row_end.copy()
+        ends[e] = end
+        out = _call(case, q=q, row_end=cuda(ends), **lists).double().cpu().numpy()
+        entries = [x for x in range(rows, 2 * rows) if x != e]
+        want, bound = case.expected(1, entries=entries, row_end=ends)
+        assert np.isnan(out[1, 0, :end]).all() and (np.abs(out[1, :, end:130] - want[:, end:]) <= bound[:, end:]).all()
+        for i, n in ((0, 200), (2, 70)):
+            want, bound = case.expected(i)
+            assert (np.abs(out[i, :, :n] - want) <= bound).all()
+    lse[case.order[e]] = -float("inf")
+    case.check(_call(case, q=q, lse=lse, **lists), which=[(1, 130)], entries=entries)
+
+
 def test_large_scores(gpu_lib):
     """Scores of hundreds: few tokens hold all of a row's weight."""
     case = Case([100, 300], [10, 20], (4, 2), 128, BF16, seed=12, strong=60.0)
