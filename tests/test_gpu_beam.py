@@ -169,6 +169,14 @@ def test_select_rows_past_32_bits(gpu_lib):
     check_select(view, scores, 5)
 
 
+def test_select_of_the_largest_sizes(gpu_lib):
+    """2^24 tokens, and 65535 beams."""
+    logits, scores = _random(1, 2, 2 ** 24, F32, 17)
+    check_select(logits, scores, 8)
+    logits, scores = _random(13107, 5, 9, BF16, 18)
+    check_select(logits, scores, 3)
+
+
 def test_select_of_no_items(gpu_lib):
     check_select(torch.zeros((0, 3, 10), device="cuda"), np.zeros((0, 3)), 2)
 

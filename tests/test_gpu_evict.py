@@ -229,6 +229,38 @@ def test_keep_many_pages(gpu_lib, kvq, in_place):
     case.check(want)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("kvq", [False, True])
+def test_keep_slices_of_longer_lists(gpu_lib, kvq, in_place):
+    """Old and new lists that begin inside of their arrays."""
+    case = Keep([100, 0, 33, 64], [40, 0, 33, 20], 2, 64, BF16, kvq, seed=10, in_place=in_place)
+    want = case.expected()
+    pad = torch.full((5,), -9, dtype=torch.int32, device="cuda")
+    given = {}
+    for names, lists in ((("seq_page_indptr", "page_ids"), case.src), (("dst_page_indptr", "dst_page_ids"), case.dst)):
+        indptr, ids = csr(lists)
+        given[names[0]], given[names[1]] = indptr + 5, torch.cat([pad, ids])
+    if in_place:
+        given["dst_page_indptr"], given["dst_page_ids"] = given["seq_page_indptr"], given["page_ids"]
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    case.call(error_flag=flag, **given)
+    case.check(want)
+    assert int(flag) == 0
+
+
+def test_keep_lists_that_are_refused(gpu_lib):
+    """A list of no elements, which has no address; one array for both lists with two indptr, or the other way round."""
+    case = Keep([20, 33], [0, 0], seed=11)
+    want = [case.bits(0), case.bits(1)]
+    (indptr, ids), (dst_indptr, dst_ids) = csr(case.src), csr(case.dst)
+    for given, match in ((dict(dst_page_ids=cuda([])), "dst_page_ids"), (dict(page_ids=cuda([])), "page_ids"),
+                         (dict(page_ids=ids, dst_page_ids=ids), "in place"),
+                         (dict(seq_page_indptr=indptr, dst_page_indptr=indptr), "in place")):
+        with pytest.raises(halo.HaloError, match=match):
+            case.call(**given)
+    case.check(want)
+
+
 @pytest.mark.parametrize("kvq", [False, True])
 def test_keep_nothing(gpu_lib, kvq):
     """A sequence that keeps no token, none at all, and rows of no width."""

@@ -220,6 +220,31 @@ def test_short_sequences(gpu_lib, rows, longest, kvq):
     case.check(_call(case))
 
 
+@pytest.mark.parametrize("dtype,rows", [(F32, 3), (BF16, 1), (BF16, 3), (BF16, 40), (BF16, 700)])
+def test_slices_of_longer_lists(gpu_lib, rows, dtype):
+    """Page lists and entries that begin inside of their arrays."""
+    case = Case([130, 0, 40, 257], [rows] * 4, (2, 1), 64, dtype, seed=36)
+    ids = torch.cat([torch.full((13,), -9, dtype=torch.int32, device="cuda"), case.ids])
+    given = dict(page_ids=ids, seq_page_indptr=case.indptr + 13)
+    if rows == 1:
+        given["row_indptr"] = None
+    else:
+        pad = np.full(7, 2 ** 30)
+        given.update(rows=cuda(np.concatenate([pad, case.order])), row_end=cuda(np.concatenate([pad, case.row_end])),
+                     row_indptr=cuda(case.row_indptr + 7))
+    flag = torch.zeros(1, dtype=torch.int32, device="cuda")
+    case.check(_call(case, error_flag=flag, **given))
+    assert int(flag) == 0
+
+
+def test_lists_of_no_pages_are_refused(gpu_lib):
+    """An array of no elements has no address; one of any element is taken."""
+    case = Case([0, 0], [1, 1], (2, 1), 64, BF16, seed=37, width=5)
+    with pytest.raises(halo.HaloError, match="page_ids"):
+        _call(case, page_ids=cuda([]))
+    case.check(_call(case, page_ids=cuda([0])))
+
+
 def test_lists_that_are_left_out(gpu_lib):
     case = Case([50, 20, 90], [3, 0, 20], seed=6, causal=False)
     case.check(_call(case, row_end=None))
