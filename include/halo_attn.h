@@ -573,7 +573,8 @@ typedef struct {
  * outside [0, num_pool_pages) and an entry whose row is outside [0, num_rows) by
  * itself, and one whose entries are no range of [0, num_entries) has none; 1 is then
  * written to error_flag (may be NULL; 0 never is). Entries that see no token need not be
- * looked at. */
+ * looked at. With num_seqs or width 0 no array is looked at; otherwise page_ids must not
+ * be NULL, also where no sequence has a page. */
 halo_status_t halo_kv_page_weights(const void* k_pool, const halo_attn_params_t* params,
                                    const halo_weight_sizes_t* sizes,
                                    const int32_t* page_ids, const int32_t* seq_page_indptr,
@@ -623,11 +624,13 @@ halo_status_t halo_kv_evict_select(const halo_evict_sizes_t* sizes, const float*
  * of the page list src, j < new_len[i]; any other sequence is copied whole (in
  * place: left alone). kept is [num_seqs][num_kv_heads][kept_width], ascending in a
  * row, bits are copied unchanged. dst_page_ids == page_ids with dst_page_indptr ==
- * seq_page_indptr moves in place, and no page may then be listed twice; otherwise no
- * page of dst may be a page of src or listed twice (beams that share pages are
- * evicted to pages of their own). A page
- * list holds at least the pages of its tokens; slots past new_len[i] keep what
- * they hold. Kept keys stay turned by the positions that they came with, while the
+ * seq_page_indptr moves in place, and no page may then be listed twice. With one of
+ * these pointers in both places and the other not, the call is refused (new lists
+ * behind the old ones in one array: a pointer to where they begin; one indptr for
+ * both: a copy of it). Otherwise no page of dst may be a page of src or listed twice
+ * (beams that share pages are evicted to pages of their own). A page list holds at
+ * least the pages of its tokens, and its array must not be NULL even if that is none;
+ * slots past new_len[i] keep what they hold. Kept keys stay turned by the positions that they came with, while the
  * places in the cache are counted anew: a token that comes later has its place
  * (halo_kv_step_tables' position) plus the tokens that its sequence has lost so far,
  * the sum of seq_len[i] - new_len[i], as its position for halo_rope_qk.
@@ -693,6 +696,7 @@ int64_t halo_beam_workspace_bytes(const halo_beam_sizes_t* sizes);
  * no candidate, nor is any of a beam whose score is not finite or whose logits
  * hold a NaN or +inf. A beam with ended[w] != 0 (ended may be NULL) offers its
  * end_token at its own score and nothing else. Where there are fewer candidates, the rest is -inf, -1, -1.
+ * num_items * num_beams must be at most 65535.
  * Candidates are compared in 64 bits; the exponentials, and their sums along each of the 64 or more
  * lanes that share a row, are in fp32, and the lanes' sums are joined in 64 bits. DEVICE
  * pointers; logits need only their elements' alignment; no output and no part of the
@@ -738,7 +742,8 @@ int64_t halo_beam_tables_workspace_bytes(const halo_beam_table_sizes_t* sizes);
  * free_next are left as they were.
  * The rows of one item may share pages, in the same place of their rows, as this
  * call makes them; those of different items must not. A prefix shared by several
- * items is no part of the rows (a segment of its own, see halo_forest_t).
+ * items is no part of the rows (a segment of its own, see halo_forest_t). At most
+ * 2^20 items, and 2^31 - 1 elements of block_table.
  * DEVICE arrays; none that is written may overlap another one. An item with a parent
  * outside [-1, num_beams) or a length that does not fit its row stays as it is
  * (every beam its own child, a row with such a length without pages); a call that

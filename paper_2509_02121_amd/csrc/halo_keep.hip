@@ -50,8 +50,8 @@ constexpr int kListed = 4096;    // keys of one bin that are looked at in LDS
 // holds more is counted from the row again). Then the
 // tokens are written in order: those of a larger key stay, and of those of the same
 // key the first ones. A wave knows its places from what the waves before it count.
-// Bound by the VALU of the CUs that have a row, of short rows by latency: 512 rows of 2048-2816 tokens 12.6 us, 32 rows of
-// 40000-70000 tokens 46 (a row needs 24 instructions a token and pass, as it is passed three times).
+// Bound by the VALU of the CUs that have a row, of short rows by latency: 512 rows of 2048-2816 tokens 14.9 us, 32 rows of
+// 40000-70000 tokens 47 (a row needs 24 instructions a token and pass, as it is passed three times).
 template <int W, int R>
 __global__ __launch_bounds__(64 * W) void evict_kernel(EvictArgs a) {
   constexpr int T = 64 * W, kChunk = T * R;
@@ -522,7 +522,7 @@ __global__ __launch_bounds__(256) void keep_kernel(KeepArgs a) {
 // page a wave. Kept indices are ascending, so a page reads only what lies at it or
 // behind it: the pages of one round are loaded, and stored when all are; what the next
 // round reads lies behind all of these. Bound by HBM where there are sequences enough (64 of 2500 bf16 tokens to
-// 2048: 264 us, 4-bit 86), by the rounds' waits where there are few (4 of 65000 4-bit tokens to 8192: 106 us).
+// 2048: 264 us, 4-bit 87), by the rounds' waits where there are few (4 of 65000 4-bit tokens to 8192: 107 us, bf16 413).
 constexpr int kInPlaceWaves = 16;
 template <typename T, bool KVQ, int D>
 __global__ __launch_bounds__(64 * kInPlaceWaves) void keep_in_place_kernel(KeepArgs a) {

@@ -6,8 +6,9 @@
 //
 // lse is known (attention has run), so there is no maximum to follow and no V:
 // a wave holds the keys of a few pages in registers and passes the rows by them,
-// 16 at a time, and each key is read once. A key's sum stays with its lanes from
-// the first row to the last, so it has one order and needs no atomics.
+// 16 or 32 at a time. A key's sum stays with its lanes, from the first row to the
+// last or (weights_wide, held rows) for 256 rows at a time, each of which is added
+// to weights_out by the same lanes, so it has one order and needs no atomics.
 
 #include <hip/hip_runtime.h>
 
@@ -143,8 +144,9 @@ __device__ __forceinline__ void flag_without_pages(const WeightArgs& a) {
 // sequence at a time, and passes all its rows by them. Rows are the A operand and keys the B
 // operand of 16x16x32 MFMAs, so that a lane has four rows of one key: their
 // exponentials are summed in the lane, and the four lane groups once at the end. Bound by HBM for up to 16 rows (32
-// sequences of 1000-8000 bf16 keys, a row of 4 heads on each: 75 us, 4.0 TB/s), for more of them, which are fp32 rows, by fp32
-// products (32 rows of 4 heads: 900 us, 42 TFLOP/s).
+// sequences of 1000-8000 bf16 keys, a row of 4 heads on each: 75 us, 4.0 TB/s). More rows come here as fp32 ones, 16 at a
+// time from global memory beside fp32 products (32 rows of 4 heads: 900 us, 42 TFLOP/s), and as bf16 ones where the rows of
+// weights are short (2048 sequences of 30-64 tokens, 8 rows of 4 heads: 135 us, which waits for lists and rows).
 template <typename T, bool KVQ, int D>
 __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
   using Fmt = KeyFormat<T, KVQ, D>;
@@ -784,7 +786,10 @@ __global__ __launch_bounds__(256, 2) void weights_wide_kernel(WeightArgs a) {
 // tokens, 224 us a batch at a time, 205 held; 256 tokens, 397 and 427. Short sequences do not pay for what a
 // workgroup waits for at their beginning: 2048 of 30-64 tokens with windows of 8, 16 and 32 take 135, 201 and 351 us by
 // the general kernel, 179, 217 and 293 a batch at a time, 249, 281 and 336 held; 512 of 200-300 tokens 130, 193 and 324,
-// 106, 121 and 152, 106, 115 and 134. How many tokens there are is known here by the weights' width alone.
+// 106, 121 and 152, 106, 115 and 134. What is known here are averages and capacities: how many tokens there are by the
+// weights' width alone, so that short sequences in wide rows of weights take the held kernel's times, and rows by all
+// entries, so that one prefix with the rows of a thousand requests and their private lists in one call take the general
+// kernel's; such calls are better made apart.
 constexpr int kShortWidth = 80, kHeldWidth = 129;   // five pages; more than eight
 bool many_rows(const halo_weight_sizes_t& s, bool lists, int group, int rows) {
   return (int64_t)(lists ? s.num_entries : s.num_seqs) * group >= rows * (int64_t)s.num_seqs;
