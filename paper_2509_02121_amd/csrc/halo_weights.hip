@@ -146,7 +146,7 @@ __device__ __forceinline__ void flag_without_pages(const WeightArgs& a) {
 // exponentials are summed in the lane, and the four lane groups once at the end. Bound by HBM for up to 16 rows (32
 // sequences of 1000-8000 bf16 keys, a row of 4 heads on each: 75 us, 4.0 TB/s). More rows come here as fp32 ones, 16 at a
 // time from global memory beside fp32 products (32 rows of 4 heads: 900 us, 42 TFLOP/s), and as bf16 ones where the rows of
-// weights are short (2048 sequences of 30-64 tokens, 8 rows of 4 heads: 135 us, which waits for lists and rows).
+// weights are short (2048 sequences of 30-64 tokens, 8 rows of 4 heads: 135 us).
 template <typename T, bool KVQ, int D>
 __global__ __launch_bounds__(256) void weights_kernel(WeightArgs a) {
   using Fmt = KeyFormat<T, KVQ, D>;
